@@ -306,6 +306,144 @@ int dpsgd_noise_adamw_multi(const dpsgd_layer* layers, int32_t n_layers,
                             uint32_t step, float scale, const dpsgd_adamw* opt, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Token tables (embeddings): lookup, per-example norms, clipped sum.
+ * Paper: Section 2.2, per-example gradient of the trainable parameters, for
+ * the one layer of a language model that is not of the G^T A form.
+ *
+ *   out[i][t]     = scale * table[id_it]                        (lookup)
+ *   g_i[v]        = scale * sum_{t: id_it = v} G[i][t]          (gradient of example i)
+ *
+ * table [n_rows][d], ids [B][T], out and G [B][T][d], all row-major and
+ * contiguous. An id outside [0, n_rows) is an empty position (padding): a row
+ * of zeros in out, no part of the gradient; its row of G is not read.
+ * ids is aligned to its element, table, out and G to 16 bytes.
+ * ------------------------------------------------------------------------- */
+typedef enum dpsgd_index_dtype {
+  DPSGD_I32 = 0,   /* int32 ids */
+  DPSGD_I64 = 1    /* int64 ids */
+} dpsgd_index_dtype;
+
+typedef struct dpsgd_embedding {
+  const void* ids;      /* [B][T] token ids, index_dtype                     */
+  int64_t B;            /* examples, >= 1                                    */
+  int64_t T;            /* positions per example, >= 1; B T < 2^31           */
+  int64_t n_rows;       /* rows of the table (vocabulary), 1 .. 2^31 - 1     */
+  int64_t d;            /* width of a row, 1 .. 2^30                         */
+  int32_t index_dtype;  /* dpsgd_index_dtype                                 */
+  float scale;          /* finite                                            */
+} dpsgd_embedding;
+
+/* Products are formed in float32 and rounded once to out_dtype. table and out
+ * are float32 or bf16 each on its own, and do not overlap. */
+int dpsgd_embedding_lookup(const dpsgd_embedding* emb, const void* table, int32_t table_dtype,
+                           void* out, int32_t out_dtype, void* stream);
+
+/* Scratch of the two calls below (device, 16-byte aligned); 0 for an invalid
+ * descriptor. Reads everything but ids of the descriptor. */
+size_t dpsgd_embedding_workspace_bytes(const dpsgd_embedding* emb);
+
+/* norms_sq[i] = (accumulate ? norms_sq[i] : 0) + ||g_i||_F^2 (float32 [B]):
+ * with accumulate, the table joins the norm over the linear layers. dtype is
+ * G's. Every group of equal tokens of an example is summed in float32 before
+ * its squared norm is taken. */
+int dpsgd_embedding_norms(const dpsgd_embedding* emb, const void* G, int32_t dtype,
+                          float* norms_sq, int32_t accumulate, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
+/* grad = (accumulate ? grad : 0) + sum_i c_i g_i (float32 [n_rows][d], 16-byte
+ * aligned), c_i, factors_out and mask_out as in dpsgd_clip_accumulate. norms_sq
+ * NULL: every c_i is 1 (C is not looked at, factors_out and mask_out must be
+ * NULL). Rows of examples with c_i = 0 are not read. Without accumulate every row
+ * of grad is written, rows without a token with zeros. Sums are in float32,
+ * in an order that the ids alone decide. */
+int dpsgd_embedding_clip_accumulate(const dpsgd_embedding* emb, const void* G, int32_t dtype,
+                                    const float* norms_sq, float C, float* grad,
+                                    int32_t accumulate, float* factors_out, uint8_t* mask_out,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Group norm with an activation, channels last.
+ * Paper: Section 2.2 (a model trained by per-example gradients normalises
+ * within an example).
+ *
+ *   x, y [B][S][C] (S positions: H W of an image, T of a sequence), groups of
+ *   C / groups neighbouring channels; per example and group, over its
+ *   S C / groups values:  mu = mean, rstd = 1 / sqrt(var + eps) (biased var)
+ *   xh = (x - mu) rstd;  z = gamma xh + beta;  y = act(z)
+ *
+ * gamma and beta are float32 [C] (NULL: 1 and 0). Statistics and arithmetic
+ * are float32; y is rounded once to dtype. x, y, dy, dx are contiguous and
+ * 16-byte aligned.
+ * ------------------------------------------------------------------------- */
+typedef enum dpsgd_activation {
+  DPSGD_ACT_NONE = 0,
+  DPSGD_ACT_RELU = 1,   /* max(z, 0)                                                  */
+  DPSGD_ACT_SILU = 2,   /* z / (1 + exp(-z))                                          */
+  DPSGD_ACT_GELU = 3    /* 0.5 z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))            */
+} dpsgd_activation;
+
+typedef struct dpsgd_group_norm {
+  int64_t B;            /* examples, >= 1                                    */
+  int64_t S;            /* positions, >= 1; B S < 2^31                       */
+  int64_t C;            /* channels, >= 1, a multiple of groups              */
+  int64_t groups;       /* >= 1                                              */
+  const float* gamma;   /* [C], device; may be NULL                          */
+  const float* beta;    /* [C], device; may be NULL                          */
+  int32_t dtype;        /* dpsgd_dtype of x, y, dy, dx                       */
+  int32_t act;          /* dpsgd_activation                                  */
+  float eps;            /* > 0, finite                                       */
+} dpsgd_group_norm;
+
+/* Scratch of the two calls below (device, 16-byte aligned); 0 for an invalid
+ * descriptor. Does not read the pointers of the descriptor. */
+size_t dpsgd_group_norm_workspace_bytes(const dpsgd_group_norm* gn);
+
+/* mean and rstd (float32 [B][groups]) are kept for the backward call; NULL
+ * where there is none. y may be x. */
+int dpsgd_group_norm_forward(const dpsgd_group_norm* gn, const void* x, void* y, float* mean,
+                             float* rstd, void* workspace, size_t workspace_bytes, void* stream);
+
+/* dx, and the per-example gradients of the affine parameters (float32 [B][C]):
+ *   dz = dy act'(z);  dbeta[i] = sum_s dz;  dgamma[i] = sum_s dz xh
+ *   dx = rstd (gamma dz - mean(gamma dz) - xh mean(gamma dz xh))
+ * (means over the group; act'(0) = 0 for RELU). dgamma and dbeta are linear
+ * layers' gradients with T = 1, d_in = 1, A = 1: a dpsgd_layer {A = ones [B],
+ * G = dgamma} takes them through the norm, clip, noise and step calls. dx may
+ * be dy, and may not be x. */
+int dpsgd_group_norm_backward(const dpsgd_group_norm* gn, const void* x, const void* dy,
+                              const float* mean, const float* rstd, void* dx, float* dgamma,
+                              float* dbeta, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* ---------------------------------------------------------------------------
+ * One norm over many tensors, and clipping to it.
+ * Paper: Section 2.2, g min(1, C/||g||), with the whole of n_layers gradients
+ * as one vector (one user's or one micro-batch's update; the released noisy
+ * gradient before the optimizer step).
+ *
+ *   norm = sqrt(sum_l ||g_l||_F^2);  c = norm > max_norm ? max_norm / norm : 1
+ *   outs[l] = c * grads[l]
+ *
+ * grads and outs: one float32 buffer of d_out d_in entries a layer, 16-byte
+ * aligned; outs[l] may be grads[l] (in place), and overlaps nothing else. Only
+ * d_in and d_out of a descriptor are read. Squares are summed in float64 and
+ * the norm is rounded once to float32. max_norm > 0 (+inf: no clipping). An
+ * infinite norm gives c = 0 (an infinite entry then becomes NaN, the others
+ * 0), a NaN norm c = NaN. norm_out and factor_out: float32 [1], device, either
+ * may be NULL in dpsgd_global_clip_multi.
+ * ------------------------------------------------------------------------- */
+size_t dpsgd_global_norm_workspace_bytes(const dpsgd_layer* layers, int32_t n_layers);
+
+int dpsgd_global_norm_multi(const dpsgd_layer* layers, int32_t n_layers,
+                            const float* const* grads, float* norm_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+int dpsgd_global_clip_multi(const dpsgd_layer* layers, int32_t n_layers,
+                            const float* const* grads, float* const* outs, float max_norm,
+                            float* norm_out, float* factor_out, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Inspection hooks for tests (same stream as dpsgd_add_noise).
  *   dpsgd_philox_u32: out[4*b + w] = word w of block (first_block + b), b < n_blocks.
  *   dpsgd_gaussian:   out[e] = z_e of the stream above for e < n.

@@ -316,6 +316,29 @@ int launch_philox_u32(uint32_t* out, int64_t first_block, int64_t n_blocks, uint
 int launch_gaussian(float* out, int64_t n, uint64_t seed, uint32_t tensor_id, uint32_t step,
                     hipStream_t stream);
 
+// Token tables (embedding.hip), group norm (group_norm.hip) and the norm over
+// many tensors (global_clip.hip). outs may be null in launch_global_clip: the
+// norm alone.
+size_t embedding_workspace_bytes(const dpsgd_embedding& e);
+int launch_embedding_lookup(const dpsgd_embedding& e, const void* table, int32_t table_dtype,
+                            void* out, int32_t out_dtype, hipStream_t stream);
+int launch_embedding_norms(const dpsgd_embedding& e, const void* G, int32_t dtype, float* norms_sq,
+                           int accumulate, void* workspace, hipStream_t stream);
+int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
+                         const float* norms_sq, float C, float* grad, int accumulate,
+                         float* factors_out, uint8_t* mask_out, void* workspace,
+                         hipStream_t stream);
+size_t group_norm_workspace_bytes(const dpsgd_group_norm& n);
+int launch_group_norm_forward(const dpsgd_group_norm& n, const void* x, void* y, float* mean,
+                              float* rstd, void* workspace, hipStream_t stream);
+int launch_group_norm_backward(const dpsgd_group_norm& n, const void* x, const void* dy,
+                               const float* mean, const float* rstd, void* dx, float* dgamma,
+                               float* dbeta, void* workspace, hipStream_t stream);
+size_t global_norm_workspace_bytes(const dpsgd_layer* layers, int32_t n);
+int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const* grads,
+                       float* const* outs, float max_norm, float* norm_out, float* factor_out,
+                       void* workspace, hipStream_t stream);
+
 inline int check_launch() {
   return hipGetLastError() == hipSuccess ? DPSGD_OK : DPSGD_ERR_HIP;
 }

@@ -1,0 +1,92 @@
+// Loads and stores of a few consecutive elements as float32: float or bf16
+// (uint16_t bits, rounded to nearest-even on the way out).
+#pragma once
+
+#include "common.h"
+
+namespace dpsgd {
+
+// Elements p[0..V) widened to float32. p is aligned to min(16, V sizeof(T)) bytes.
+template <int V>
+__device__ __forceinline__ void load_vec(const float* p, float (&x)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int k = 0; k < V; k += 4) {
+      const f32x4_t q = *reinterpret_cast<const f32x4_t*>(p + k);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) x[k + c] = q[c];
+    }
+  } else if constexpr (V == 2) {
+    const float2 q = *reinterpret_cast<const float2*>(p);
+    x[0] = q.x;
+    x[1] = q.y;
+  } else {
+    x[0] = *p;
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void load_vec(const uint16_t* p, float (&x)[V]) {
+  if constexpr (V == 8) {
+    const uint4 q = *reinterpret_cast<const uint4*>(p);
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      x[2 * c] = bf16_lo(w[c]);
+      x[2 * c + 1] = bf16_hi(w[c]);
+    }
+  } else if constexpr (V == 4) {
+    const uint2 q = *reinterpret_cast<const uint2*>(p);
+    x[0] = bf16_lo(q.x);
+    x[1] = bf16_hi(q.x);
+    x[2] = bf16_lo(q.y);
+    x[3] = bf16_hi(q.y);
+  } else if constexpr (V == 2) {
+    const uint32_t q = *reinterpret_cast<const uint32_t*>(p);
+    x[0] = bf16_lo(q);
+    x[1] = bf16_hi(q);
+  } else {
+    x[0] = bf16_to_f32(*p);
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void store_vec(float* p, const float (&x)[V]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int k = 0; k < V; k += 4)
+      *reinterpret_cast<f32x4_t*>(p + k) = f32x4_t{x[k], x[k + 1], x[k + 2], x[k + 3]};
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]);
+  } else {
+    *p = x[0];
+  }
+}
+
+template <int V>
+__device__ __forceinline__ void store_vec(uint16_t* p, const float (&x)[V]) {
+  if constexpr (V == 8) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                              pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  } else if constexpr (V == 4) {
+    *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]));
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<uint32_t*>(p) = pack_bf16x2(x[0], x[1]);
+  } else {
+    *p = (uint16_t)pack_bf16x2(x[0], 0.0f);
+  }
+}
+
+// Largest of 8, 4, 2, 1 (at most `most`) that divides n.
+inline int vec_width(int64_t n, int most) {
+  for (int v = most; v > 1; v >>= 1)
+    if (n % v == 0) return v;
+  return 1;
+}
+
+// n / d for n < 2^31, by the magic and shift of divide_magic.
+__device__ __forceinline__ uint32_t magic_divide(uint32_t n, uint32_t magic, int32_t shift) {
+  return shift < 0 ? n : __umulhi(n, magic) >> shift;
+}
+
+}  // namespace dpsgd

@@ -24,6 +24,16 @@ DPSGD_NORM_GHOST = 1
 DPSGD_NORM_MATERIALIZE = 2
 DPSGD_NORM_CLOSED_FORM = 3   # reported by dpsgd_select_norm_mode for T = 1 layers
 
+DPSGD_I32 = 0
+DPSGD_I64 = 1
+DPSGD_ACT_NONE = 0
+DPSGD_ACT_RELU = 1
+DPSGD_ACT_SILU = 2
+DPSGD_ACT_GELU = 3
+#: Activations of a group norm by name.
+ACTIVATIONS = {"none": DPSGD_ACT_NONE, "relu": DPSGD_ACT_RELU, "silu": DPSGD_ACT_SILU,
+               "gelu": DPSGD_ACT_GELU}
+
 DPSGD_OK = 0
 DPSGD_ERR_INVALID_ARG = -1
 DPSGD_ERR_UNSUPPORTED = -2
@@ -39,6 +49,10 @@ EXPORTED = (
     "dpsgd_clipped_sum_multi", "dpsgd_add_noise",
     "dpsgd_add_noise_multi", "dpsgd_noise_adamw", "dpsgd_noise_adamw_multi",
     "dpsgd_philox_u32", "dpsgd_gaussian", "dpsgd_status_string", "dpsgd_version",
+    "dpsgd_embedding_lookup", "dpsgd_embedding_workspace_bytes", "dpsgd_embedding_norms",
+    "dpsgd_embedding_clip_accumulate", "dpsgd_group_norm_workspace_bytes",
+    "dpsgd_group_norm_forward", "dpsgd_group_norm_backward", "dpsgd_global_norm_workspace_bytes",
+    "dpsgd_global_norm_multi", "dpsgd_global_clip_multi",
 )
 
 
@@ -72,12 +86,39 @@ class dpsgd_adamw(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
     ]
 
 
+class dpsgd_embedding(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
+    _fields_ = [
+        ("ids", ctypes.c_void_p),
+        ("B", ctypes.c_int64),
+        ("T", ctypes.c_int64),
+        ("n_rows", ctypes.c_int64),
+        ("d", ctypes.c_int64),
+        ("index_dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class dpsgd_group_norm(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
+    _fields_ = [
+        ("B", ctypes.c_int64),
+        ("S", ctypes.c_int64),
+        ("C", ctypes.c_int64),
+        ("groups", ctypes.c_int64),
+        ("gamma", ctypes.c_void_p),
+        ("beta", ctypes.c_void_p),
+        ("dtype", ctypes.c_int32),
+        ("act", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+    ]
+
+
 _lib = None
 
 
 def _declare(lib):
     P = ctypes.POINTER
     L = P(dpsgd_layer)
+    E, N = P(dpsgd_embedding), P(dpsgd_group_norm)
     vp, i32, i64, u32, u64, f32, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                        ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
                                        ctypes.c_size_t)
@@ -103,6 +144,17 @@ def _declare(lib):
                                                    f32, f32, u64, u32, f32, P(dpsgd_adamw), vp]),
         "dpsgd_philox_u32": (ctypes.c_int, [vp, i64, i64, u64, u32, u32, vp]),
         "dpsgd_gaussian": (ctypes.c_int, [vp, i64, u64, u32, u32, vp]),
+        "dpsgd_embedding_lookup": (ctypes.c_int, [E, vp, i32, vp, i32, vp]),
+        "dpsgd_embedding_workspace_bytes": (sz, [E]),
+        "dpsgd_embedding_norms": (ctypes.c_int, [E, vp, i32, vp, i32, vp, sz, vp]),
+        "dpsgd_embedding_clip_accumulate": (ctypes.c_int, [E, vp, i32, vp, f32, vp, i32, vp, vp,
+                                                           vp, sz, vp]),
+        "dpsgd_group_norm_workspace_bytes": (sz, [N]),
+        "dpsgd_group_norm_forward": (ctypes.c_int, [N, vp, vp, vp, vp, vp, sz, vp]),
+        "dpsgd_group_norm_backward": (ctypes.c_int, [N, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "dpsgd_global_norm_workspace_bytes": (sz, [L, i32]),
+        "dpsgd_global_norm_multi": (ctypes.c_int, [L, i32, P(vp), vp, vp, sz, vp]),
+        "dpsgd_global_clip_multi": (ctypes.c_int, [L, i32, P(vp), P(vp), f32, vp, vp, vp, sz, vp]),
         "dpsgd_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "dpsgd_version": (ctypes.c_int, []),
     }
@@ -343,6 +395,215 @@ def dpsgd_gaussian(out, n, seed, tensor_id, step, stream=None):
     load()
     st = _lib.dpsgd_gaussian(_ptr(out), n, seed, tensor_id, step, _stream(stream))
     _check("dpsgd_gaussian", st)
+
+
+# ----------------------------------------- around the linear layers
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return DPSGD_F32
+    if t.dtype == torch.bfloat16:
+        return DPSGD_BF16
+    raise ValueError(f"float32 or bfloat16 expected, not {t.dtype}")
+
+
+def _want(name, t, shape, dtype=None):
+    """Raises ValueError unless t is a contiguous device tensor of this shape (and dtype)."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+
+
+def _workspace(workspace):
+    return _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def make_embedding(ids, table_shape, scale: float = 1.0) -> dpsgd_embedding:
+    """Descriptor of a table [n_rows, d] and the ids [B, T] (int32 or int64, on the
+    device) that look into it. An id outside the table is an empty position. The
+    descriptor keeps ids alive."""
+    import torch
+    if ids.dim() != 2 or ids.dtype not in (torch.int32, torch.int64):
+        raise ValueError("ids must be [B, T], int32 or int64")
+    if not ids.is_cuda or not ids.is_contiguous():
+        raise ValueError("ids must be a contiguous device tensor")
+    n_rows, d = table_shape
+    emb = dpsgd_embedding(ids.data_ptr(), ids.shape[0], ids.shape[1], n_rows, d,
+                          DPSGD_I64 if ids.dtype == torch.int64 else DPSGD_I32, scale)
+    emb.keep = ids
+    return emb
+
+
+def dpsgd_embedding_lookup(emb: dpsgd_embedding, table, out, stream=None):
+    load()
+    _want("table", table, (emb.n_rows, emb.d))
+    _want("out", out, (emb.B, emb.T, emb.d))
+    st = _lib.dpsgd_embedding_lookup(ctypes.byref(emb), _ptr(table), _dtype_of(table), _ptr(out),
+                                     _dtype_of(out), _stream(stream))
+    _check("dpsgd_embedding_lookup", st)
+
+
+def dpsgd_embedding_workspace_bytes(emb: dpsgd_embedding) -> int:
+    load()
+    return int(_lib.dpsgd_embedding_workspace_bytes(ctypes.byref(emb)))
+
+
+def dpsgd_embedding_norms(emb: dpsgd_embedding, G, norms_sq, accumulate=False, workspace=None,
+                          stream=None):
+    import torch
+    load()
+    _want("G", G, (emb.B, emb.T, emb.d))
+    _want("norms_sq", norms_sq, (emb.B,), torch.float32)
+    st = _lib.dpsgd_embedding_norms(ctypes.byref(emb), _ptr(G), _dtype_of(G), _ptr(norms_sq),
+                                    int(accumulate), *_workspace(workspace), _stream(stream))
+    _check("dpsgd_embedding_norms", st)
+
+
+def dpsgd_embedding_clip_accumulate(emb: dpsgd_embedding, G, norms_sq, C, grad, accumulate=False,
+                                    factors_out=None, mask_out=None, workspace=None, stream=None):
+    """norms_sq None: the plain sum over the batch (C is not looked at)."""
+    import torch
+    load()
+    _want("G", G, (emb.B, emb.T, emb.d))
+    _want("grad", grad, (emb.n_rows, emb.d), torch.float32)
+    if norms_sq is not None:
+        _want("norms_sq", norms_sq, (emb.B,), torch.float32)
+    if factors_out is not None:
+        _want("factors_out", factors_out, (emb.B,), torch.float32)
+    if mask_out is not None:
+        _want("mask_out", mask_out, (emb.B,), torch.uint8)
+    st = _lib.dpsgd_embedding_clip_accumulate(
+        ctypes.byref(emb), _ptr(G), _dtype_of(G), _ptr(norms_sq), C, _ptr(grad), int(accumulate),
+        _ptr(factors_out), _ptr(mask_out), *_workspace(workspace), _stream(stream))
+    _check("dpsgd_embedding_clip_accumulate", st)
+
+
+def make_group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
+                    act: str = "none") -> dpsgd_group_norm:
+    """Descriptor of a group norm over channels-last rows x [B, ..., C] (every axis
+    between the first and the last is a position: [B, S, C], [B, H, W, C]; a
+    channels_last tensor [B, C, H, W] is x.permute(0, 2, 3, 1)). act: a name of
+    ACTIVATIONS. The descriptor keeps gamma and beta alive."""
+    import torch
+    if x.dim() < 2 or x.numel() == 0:
+        raise ValueError("x must be [B, ..., C] with no empty axis")
+    if act not in ACTIVATIONS:
+        raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
+    B, C = x.shape[0], x.shape[-1]
+    for name, t in (("gamma", gamma), ("beta", beta)):
+        if t is not None:
+            _want(name, t, (C,), torch.float32)
+    gn = dpsgd_group_norm(B, x.numel() // (B * C), C, groups,
+                          None if gamma is None else gamma.data_ptr(),
+                          None if beta is None else beta.data_ptr(), _dtype_of(x),
+                          ACTIVATIONS[act], eps)
+    gn.keep = (gamma, beta)
+    return gn
+
+
+def _want_rows(name, t, gn: dpsgd_group_norm):
+    _want(name, t, t.shape)
+    if t.shape[0] != gn.B or t.shape[-1] != gn.C or t.numel() != gn.B * gn.S * gn.C:
+        raise ValueError(f"{name} must be [{gn.B}, ({gn.S} positions), {gn.C}], not {list(t.shape)}")
+    if _dtype_of(t) != gn.dtype:
+        raise ValueError(f"{name} has another dtype than the descriptor")
+
+
+def dpsgd_group_norm_workspace_bytes(gn: dpsgd_group_norm) -> int:
+    load()
+    return int(_lib.dpsgd_group_norm_workspace_bytes(ctypes.byref(gn)))
+
+
+def dpsgd_group_norm_forward(gn: dpsgd_group_norm, x, y, mean=None, rstd=None, workspace=None,
+                             stream=None):
+    import torch
+    load()
+    _want_rows("x", x, gn)
+    _want_rows("y", y, gn)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        if t is not None:
+            _want(name, t, (gn.B, gn.groups), torch.float32)
+    st = _lib.dpsgd_group_norm_forward(ctypes.byref(gn), _ptr(x), _ptr(y), _ptr(mean), _ptr(rstd),
+                                       *_workspace(workspace), _stream(stream))
+    _check("dpsgd_group_norm_forward", st)
+
+
+def dpsgd_group_norm_backward(gn: dpsgd_group_norm, x, dy, mean, rstd, dx, dgamma, dbeta,
+                              workspace=None, stream=None):
+    """dgamma and dbeta are per example ([B, C]); affine_layer makes layers of them."""
+    import torch
+    load()
+    for name, t in (("x", x), ("dy", dy), ("dx", dx)):
+        _want_rows(name, t, gn)
+    for name, t in (("mean", mean), ("rstd", rstd)):
+        _want(name, t, (gn.B, gn.groups), torch.float32)
+    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
+        _want(name, t, (gn.B, gn.C), torch.float32)
+    st = _lib.dpsgd_group_norm_backward(ctypes.byref(gn), _ptr(x), _ptr(dy), _ptr(mean),
+                                        _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
+                                        *_workspace(workspace), _stream(stream))
+    _check("dpsgd_group_norm_backward", st)
+
+
+def affine_layer(ones, grad, tensor_id: int) -> dpsgd_layer:
+    """The per-example gradients [B, C] of a vector of parameters as a layer (T = 1,
+    d_in = 1, activations ones [B]): the norm, clip, noise and step calls take it like
+    any other float32 layer. The parameter's own buffers are [C, 1]."""
+    B, C = grad.shape
+    return make_layer(ones.view(B, 1, 1), grad.view(B, 1, C), tensor_id)
+
+
+def dpsgd_global_norm_workspace_bytes(layers) -> int:
+    load()
+    arr, n = _array(layers)
+    return int(_lib.dpsgd_global_norm_workspace_bytes(arr, n))
+
+
+def _want_gradients(name, tensors, layers):
+    import torch
+    if len(tensors) != len(layers):
+        raise ValueError(f"{name}: {len(layers)} tensors expected, not {len(tensors)}")
+    for t, L in zip(tensors, layers):
+        if (t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous()
+                or t.numel() != L.d_in * L.d_out):
+            raise ValueError(f"{name} must be contiguous float32 device tensors of d_out d_in entries")
+
+
+def _want_scalar(name, t):
+    import torch
+    if t is not None and (t.dtype != torch.float32 or not t.is_cuda or t.numel() != 1):
+        raise ValueError(f"{name} must be one float32 value on the device")
+
+
+def dpsgd_global_norm_multi(layers, grads, norm_out, workspace=None, stream=None):
+    load()
+    _want_gradients("grads", grads, layers)
+    _want_scalar("norm_out", norm_out)
+    arr, n = _array(layers)
+    st = _lib.dpsgd_global_norm_multi(arr, n, _ptr_array(grads), _ptr(norm_out),
+                                      *_workspace(workspace), _stream(stream))
+    _check("dpsgd_global_norm_multi", st)
+
+
+def dpsgd_global_clip_multi(layers, grads, outs, max_norm: float, norm_out=None, factor_out=None,
+                            workspace=None, stream=None):
+    """outs may be grads (in place)."""
+    load()
+    _want_gradients("grads", grads, layers)
+    if outs is not grads:
+        _want_gradients("outs", outs, layers)
+    _want_scalar("norm_out", norm_out)
+    _want_scalar("factor_out", factor_out)
+    arr, n = _array(layers)
+    st = _lib.dpsgd_global_clip_multi(arr, n, _ptr_array(grads), _ptr_array(outs), max_norm,
+                                      _ptr(norm_out), _ptr(factor_out), *_workspace(workspace),
+                                      _stream(stream))
+    _check("dpsgd_global_clip_multi", st)
 
 
 # ------------------------------------------------------------ whole step
