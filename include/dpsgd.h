@@ -326,9 +326,9 @@ typedef enum dpsgd_index_dtype {
 typedef struct dpsgd_embedding {
   const void* ids;      /* [B][T] token ids, index_dtype                     */
   int64_t B;            /* examples, >= 1                                    */
-  int64_t T;            /* positions per example, >= 1; B T < 2^31           */
+  int64_t T;            /* positions per example, >= 1; B T <= 2^30          */
   int64_t n_rows;       /* rows of the table (vocabulary), 1 .. 2^31 - 1     */
-  int64_t d;            /* width of a row, 1 .. 2^30                         */
+  int64_t d;            /* width of a row, 1 .. 2^20                         */
   int32_t index_dtype;  /* dpsgd_index_dtype                                 */
   float scale;          /* finite                                            */
 } dpsgd_embedding;
@@ -353,7 +353,8 @@ int dpsgd_embedding_norms(const dpsgd_embedding* emb, const void* G, int32_t dty
 /* grad = (accumulate ? grad : 0) + sum_i c_i g_i (float32 [n_rows][d], 16-byte
  * aligned), c_i, factors_out and mask_out as in dpsgd_clip_accumulate. norms_sq
  * NULL: every c_i is 1 (C is not looked at, factors_out and mask_out must be
- * NULL). Rows of examples with c_i = 0 are not read. Without accumulate every row
+ * NULL). norms_sq, grad, factors_out and mask_out do not overlap
+ * (DPSGD_ERR_INVALID_ARG). Rows of examples with c_i = 0 are not read. Without accumulate every row
  * of grad is written, rows without a token with zeros. Sums are in float32,
  * in an order that the ids alone decide. */
 int dpsgd_embedding_clip_accumulate(const dpsgd_embedding* emb, const void* G, int32_t dtype,

@@ -14,12 +14,18 @@ constexpr int64_t kMostEntries = INT64_C(1) << 40;   // of one tensor
 bool valid_dtype(int32_t d) { return d == DPSGD_F32 || d == DPSGD_BF16; }
 bool aligned(const void* p, size_t n) { return p && reinterpret_cast<uintptr_t>(p) % n == 0; }
 
+bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
+  const char *p = static_cast<const char*>(a), *q = static_cast<const char*>(b);
+  return p && q && p < q + nb && q < p + na;
+}
+
 int check_embedding(const dpsgd_embedding* e, bool data) {
   if (!e) return DPSGD_ERR_INVALID_ARG;
   if (e->index_dtype != DPSGD_I32 && e->index_dtype != DPSGD_I64) return DPSGD_ERR_UNSUPPORTED;
   if (e->B < 1 || e->T < 1 || e->n_rows < 1 || e->d < 1) return DPSGD_ERR_INVALID_ARG;
-  if (e->B > kI32Max || e->T > kI32Max / e->B || e->n_rows > kI32Max) return DPSGD_ERR_INVALID_ARG;
-  if (e->d > (INT64_C(1) << 30) || e->d > kMostEntries / (e->B * e->T) ||
+  if (e->B > (INT64_C(1) << 30) || e->T > (INT64_C(1) << 30) / e->B || e->n_rows > kI32Max)
+    return DPSGD_ERR_INVALID_ARG;
+  if (e->d > (INT64_C(1) << 20) || e->d > kMostEntries / (e->B * e->T) ||
       e->d > kMostEntries / e->n_rows)
     return DPSGD_ERR_INVALID_ARG;
   if (!isfinite(e->scale)) return DPSGD_ERR_INVALID_ARG;
@@ -107,6 +113,13 @@ int dpsgd_embedding_clip_accumulate(const dpsgd_embedding* emb, const void* G, i
   if (norms_sq) {
     if (!aligned(norms_sq, 4) || !(C > 0.0f)) return DPSGD_ERR_INVALID_ARG;   // NaN too
     if (factors_out && !aligned(factors_out, 4)) return DPSGD_ERR_INVALID_ARG;
+    // The factors are formed from the norms while they, and grad, are written.
+    const size_t n = (size_t)emb->B * sizeof(float);
+    const size_t ng = (size_t)(emb->n_rows * emb->d) * sizeof(float);
+    if (overlaps(norms_sq, n, grad, ng) || overlaps(norms_sq, n, factors_out, n) ||
+        overlaps(norms_sq, n, mask_out, (size_t)emb->B) || overlaps(grad, ng, factors_out, n) ||
+        overlaps(grad, ng, mask_out, (size_t)emb->B))
+      return DPSGD_ERR_INVALID_ARG;
   } else if (factors_out || mask_out) {
     return DPSGD_ERR_INVALID_ARG;
   }

@@ -7,14 +7,15 @@
 // An id outside [0, V) is an empty position: a row of zeros out, and a row of G
 // that is never read.
 //
-// The gradient is formed by sorted tokens, without floating-point atomics: a
-// counting sort gives the positions of every token in ascending order
-// (order, and offsets[v] into it), one wave sums the rows of one table row in
-// that order, and rows with more than `chunk` positions are summed in chunks of
-// the sorted list that a last pass joins in order. For the norms the list is
-// sorted once more by example, so that equal tokens of an example are
-// neighbours: a lane adds rows until the token changes, then adds the square of
-// its sum, and the cross-lane sum is taken once at the end.
+// The gradient is formed by sorted tokens, without floating-point atomics. For the
+// sum, a counting sort gives the positions of every token in ascending order
+// (order, and offsets into it); a wave takes kChunk consecutive entries of that
+// list and a block of columns and adds rows until the token changes, so that
+// the work is even whatever the frequencies of the tokens are. A token whose
+// entries lie in several chunks leaves partial rows that a last pass joins in
+// order; rows without a token are filled by waves of their own in the same
+// launch. For the norms every example's tokens are sorted in LDS, and equal
+// tokens, then neighbours, are added before they are squared.
 #include <math.h>
 
 #include "vec.h"
@@ -26,23 +27,49 @@ namespace {
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
+constexpr int kSortBuckets = 256;    // one workgroup a bucket, one round on the chip
 constexpr int kMaxKeysPerWg = 512;   // LDS: kSortWaves counters a key
+constexpr int kSortList = 256;       // matches that a wave keeps in LDS
+constexpr int kSortBatch = 8;        // loads that a lane has in flight
 
-// Keys of the list to sort; a key outside [0, n_keys) is left out.
-struct TokenKey {   // key of position p: its token
-  const void* ids;
-  int32_t wide;     // int64 ids
-  uint32_t n_keys;
-  int64_t n;
-  __device__ int64_t count() const { return n; }
-  __device__ uint32_t key(int64_t k) const {
-    if (wide) {
-      const uint64_t v = static_cast<const uint64_t*>(ids)[k];
-      return v < n_keys ? (uint32_t)v : 0xFFFFFFFFu;
-    }
-    return static_cast<const uint32_t*>(ids)[k];
+// Order of the keys [0, n) in a sorted list: by the low bits first (the bucket),
+// then by the others. Frequent words have small ids, so neighbouring ids go to
+// different buckets. slot() is a key's place among all, and the index of its
+// first entry in `offsets`.
+struct Buckets {
+  uint32_t n, R;   // keys, keys of a bucket
+  int32_t log;     // log2 of the number of buckets
+  __host__ __device__ uint32_t slot(uint32_t key) const {
+    return (key & ((1u << log) - 1u)) * R + (key >> log);
   }
-  __device__ int32_t value(int64_t k) const { return (int32_t)k; }
+  int64_t slots() const { return (int64_t)R << log; }
+};
+
+Buckets buckets_of(int64_t n_keys) {
+  Buckets b{(uint32_t)n_keys, 1, 0};
+  while ((INT64_C(1) << b.log) < n_keys &&
+         ((1 << b.log) < kSortBuckets || n_keys > (int64_t)kMaxKeysPerWg << b.log))
+    ++b.log;
+  b.R = (uint32_t)ceil_div(n_keys, INT64_C(1) << b.log);
+  return b;
+}
+
+// Keys of the list to sort; a key of n or more is left out. key(k) is for any
+// k < count().
+template <class Id>
+struct TokenKey {   // key of position p: its token
+  const Id* ids;
+  int32_t n;
+  __device__ int32_t count() const { return n; }
+  __device__ __forceinline__ uint32_t key(int32_t k) const {
+    if constexpr (sizeof(Id) == 8) {
+      const uint2 v = reinterpret_cast<const uint2*>(ids)[k];
+      return v.y ? 0xFFFFFFFFu : v.x;
+    } else {
+      return (uint32_t)ids[k];
+    }
+  }
+  __device__ __forceinline__ int32_t value(int32_t k) const { return k; }
 };
 
 struct ExampleKey {   // key of entry k of a list of positions: its example
@@ -50,41 +77,88 @@ struct ExampleKey {   // key of entry k of a list of positions: its example
   const int32_t* end;   // entries of the list
   uint32_t magic;       // division by T
   int32_t shift;
-  uint32_t n_keys;
-  __device__ int64_t count() const { return *end; }
-  __device__ uint32_t key(int64_t k) const { return magic_divide((uint32_t)order[k], magic, shift); }
-  __device__ int32_t value(int64_t k) const { return order[k]; }
+  __device__ int32_t count() const { return *end; }
+  __device__ __forceinline__ uint32_t key(int32_t k) const {
+    return magic_divide((uint32_t)order[k], magic, shift);
+  }
+  __device__ __forceinline__ int32_t value(int32_t k) const { return order[k]; }
 };
 
-// Stable counting sort in one launch: workgroup w owns the keys [w R, (w + 1) R)
-// and reads the whole list twice. The first pass counts, wave by wave (each wave
-// has one contiguous range of the list), its own keys and the entries with a
-// smaller key; a prefix over keys and waves then gives every wave its place, and
-// the second pass writes the entries there in list order. No entry depends on
-// the order of an atomic (the counts are integers).
+// Writes the entries of one group of 64 (at most) to their places: entry `value`
+// of key m for the lanes of `left`, in lane order; one round a distinct key.
+__device__ __forceinline__ void place_group(uint64_t left, uint32_t m, int32_t value,
+                                            volatile int32_t* place, int32_t* order) {
+  const int lane = threadIdx.x & 63;
+  while (left) {
+    const int first = __ffsll((unsigned long long)left) - 1;
+    const uint32_t m0 = (uint32_t)__builtin_amdgcn_readlane((int)m, first);
+    const uint64_t same = __ballot(m == m0) & left;
+    const int32_t at = place[m0];
+    if (same >> lane & 1) order[at + __popcll(same & ((UINT64_C(1) << lane) - 1))] = value;
+    if (lane == first) place[m0] = at + __popcll(same);
+    left &= ~same;
+  }
+}
+
+// Stable counting sort in one launch: workgroup w owns bucket w and reads the
+// whole list. Its waves have one contiguous range of the list each. They count
+// the entries of the smaller buckets and, key by key, those of their own, which
+// they keep in LDS in list order (kSortList of them; a wave that finds more
+// reads the rest of its range again). A prefix over keys and waves gives every
+// wave its places. No entry's place depends on the order of an atomic (the
+// counts are integers).
 template <class Key>
-__global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, uint32_t R,
-                                                            int32_t* order, int32_t* offsets) {
-  extern __shared__ int32_t lds[];
+__global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk, int32_t* order,
+                                                            int32_t* offsets) {
+  extern __shared__ __align__(16) int32_t lds[];
+  __shared__ int32_t kept_value[kSortWaves][kSortList];
+  __shared__ uint16_t kept_key[kSortWaves][kSortList];
+  __shared__ int32_t less_of[kSortWaves];
+  const uint32_t R = bk.R, w = blockIdx.x, mask = (1u << bk.log) - 1u;
   int32_t* table = lds;                       // [kSortWaves][R]
   int32_t* total = lds + kSortWaves * R;      // [R]
-  int32_t* less_of = total + R;               // [kSortWaves]
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const uint32_t lo = blockIdx.x * R;
-  const uint32_t n_here = keys.n_keys - lo < R ? keys.n_keys - lo : R;
-  const int64_t N = keys.count();
-  const int64_t per = ((N + kSortThreads - 1) / kSortThreads) * 64;   // entries of a wave
-  const int64_t begin = per * wave < N ? per * wave : N;
-  const int64_t end = begin + per < N ? begin + per : N;
+  const int32_t N = keys.count();
+  const int32_t groups = (N >> 6) + ((N & 63) != 0), per = (groups + kSortWaves - 1) / kSortWaves;
+  // Groups of 64 entries of this wave.
+  const int32_t first = per * wave < groups ? per * wave : groups;
+  const int32_t last = first + per < groups ? first + per : groups;
 
   for (uint32_t k = threadIdx.x; k < kSortWaves * R; k += kSortThreads) table[k] = 0;
   __syncthreads();
-  int32_t less = 0;
-  for (int64_t k = begin + lane; k < end; k += 64) {
-    const uint32_t key = keys.key(k);
-    if (key < lo) ++less;
-    const uint32_t m = key - lo;
-    if (key >= lo && m < n_here) atomicAdd(&table[wave * R + m], 1);
+  int32_t less = 0, kept = 0;
+  int32_t again = last;   // first group whose matches were not kept
+  for (int32_t g = first; g < last; g += kSortBatch) {
+    uint32_t key[kSortBatch];
+    if (g + kSortBatch <= last && (g + kSortBatch) <= N >> 6) {   // every entry is there
+#pragma unroll
+      for (int u = 0; u < kSortBatch; ++u) key[u] = keys.key((g << 6) + lane + u * 64);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kSortBatch; ++u)
+        key[u] = g + u < last && (((g + u) << 6) + lane) < N ? keys.key(((g + u) << 6) + lane) : 0xFFFFFFFFu;
+    }
+#pragma unroll
+    for (int u = 0; u < kSortBatch; ++u) {
+      const uint32_t b = key[u] < bk.n ? key[u] & mask : 0xFFFFFFFFu;
+      less += b < w;
+      const uint64_t hits = __ballot(b == w);
+      if (hits) {
+        const uint32_t m = key[u] >> bk.log;
+        if (b == w) atomicAdd(&table[wave * R + m], 1);
+        const int32_t more = __popcll(hits);
+        if (again == last && kept + more <= kSortList) {
+          if (b == w) {
+            const int at = kept + __popcll(hits & ((UINT64_C(1) << lane) - 1));
+            kept_value[wave][at] = keys.value(((g + u) << 6) + lane);
+            kept_key[wave][at] = (uint16_t)m;
+          }
+          kept += more;
+        } else if (again == last) {
+          again = g + u;
+        }
+      }
+    }
   }
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) less += __shfl_xor(less, off, 64);
@@ -92,13 +166,15 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, uint32_t R
   __syncthreads();
   if (threadIdx.x < R) {
     int32_t t = 0;
-    for (int w = 0; w < kSortWaves; ++w) t += table[w * R + threadIdx.x];
+    for (int v = 0; v < kSortWaves; ++v) t += table[v * R + threadIdx.x];
     total[threadIdx.x] = t;
   }
   __syncthreads();
   if (threadIdx.x < 64) {   // exclusive prefix of total[], 64 keys at a time
-    int32_t run = 0;
-    for (int w = 0; w < kSortWaves; ++w) run += less_of[w];
+    int32_t run = lane < kSortWaves ? less_of[lane] : 0;
+#pragma unroll
+    for (int off = kSortWaves / 2; off >= 1; off >>= 1) run += __shfl_xor(run, off, 64);
+    run = __shfl(run, 0, 64);
     for (uint32_t base = 0; base < R; base += 64) {
       const int32_t t = base + lane < R ? total[base + lane] : 0;
       int32_t s = t;
@@ -110,51 +186,39 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, uint32_t R
       if (base + lane < R) total[base + lane] = run + s - t;
       run += __shfl(s, 63, 64);
     }
-    if (lane == 0 && lo + n_here == keys.n_keys) offsets[keys.n_keys] = run;
+    if (lane == 0 && w == mask) offsets[bk.R << bk.log] = run;
   }
   __syncthreads();
-  if (threadIdx.x < n_here) {
+  if (threadIdx.x < R) {
     int32_t at = total[threadIdx.x];
-    offsets[lo + threadIdx.x] = at;
-    for (int w = 0; w < kSortWaves; ++w) {
-      const int32_t t = table[w * R + threadIdx.x];
-      table[w * R + threadIdx.x] = at;
+    offsets[w * R + threadIdx.x] = at;
+    for (int v = 0; v < kSortWaves; ++v) {
+      const int32_t t = table[v * R + threadIdx.x];
+      table[v * R + threadIdx.x] = at;
       at += t;
     }
   }
   __syncthreads();
   volatile int32_t* place = table + wave * R;   // written by one lane, read by the others of its wave
-  for (int64_t base = begin; base < end; base += 64) {
-    const int64_t k = base + lane;
-    const uint32_t key = k < end ? keys.key(k) : 0xFFFFFFFFu;
-    const uint32_t m = key - lo;
-    uint64_t left = __ballot(key >= lo && m < n_here);
-    while (left) {   // one round for each distinct key among the 64 entries
-      const int first = __ffsll((unsigned long long)left) - 1;
-      const uint32_t m0 = (uint32_t)__builtin_amdgcn_readlane((int)m, first);
-      const uint64_t same = __ballot(m == m0) & left;
-      const int32_t at = place[m0];
-      if (same >> lane & 1) {
-        const int rank = __popcll(same & ((UINT64_C(1) << lane) - 1));
-        order[at + rank] = keys.value(k);
-      }
-      if (lane == first) place[m0] = at + __popcll(same);
-      left &= ~same;
-    }
+  for (int32_t base = 0; base < kept; base += 64) {
+    const bool here = base + lane < kept;
+    const int at = here ? base + lane : 0;
+    place_group(__ballot(here), kept_key[wave][at], kept_value[wave][at], place, order);
+  }
+  for (int32_t g = again; g < last; ++g) {
+    const int32_t k = (g << 6) + lane;
+    const uint32_t key = k < N ? keys.key(k) : 0xFFFFFFFFu;
+    const bool match = key < bk.n && (key & mask) == w;
+    place_group(__ballot(match), key >> bk.log, match ? keys.value(k) : 0, place, order);
   }
 }
 
-uint32_t keys_per_wg(int64_t n_keys) {
-  const int64_t r = ceil_div(n_keys, 256);
-  return (uint32_t)(r < kMaxKeysPerWg ? r : kMaxKeysPerWg);
-}
-
 template <class Key>
-int launch_sort(const Key& keys, int32_t* order, int32_t* offsets, hipStream_t stream) {
-  const uint32_t R = keys_per_wg(keys.n_keys);
-  const size_t lds = ((size_t)(kSortWaves + 1) * R + kSortWaves) * sizeof(int32_t);
-  hipLaunchKernelGGL(sort_kernel<Key>, dim3((uint32_t)ceil_div(keys.n_keys, R)), dim3(kSortThreads),
-                     lds, stream, keys, R, order, offsets);
+int launch_sort(const Key& keys, const Buckets& bk, int32_t* order, int32_t* offsets,
+                hipStream_t stream) {
+  const size_t lds = (size_t)(kSortWaves + 1) * bk.R * sizeof(int32_t);
+  hipLaunchKernelGGL(sort_kernel<Key>, dim3(1u << bk.log), dim3(kSortThreads), lds, stream, keys, bk,
+                     order, offsets);
   return check_launch();
 }
 
@@ -218,108 +282,318 @@ int launch_lookup_of(const LookupArgs& a, hipStream_t stream) {
 
 // --------------------------------------------------------------------- norms
 
+constexpr int kNormThreads = 1024;
+constexpr int kNormWaves = kNormThreads / 64;
+constexpr int kSortedInLds = 4096;   // longest example whose tokens are sorted in LDS
+constexpr int kLdsGroups = kSortedInLds / kNormThreads;   // groups of 64 tokens of a wave
+constexpr int kMostParts = 16;
+constexpr int kRowBatch = 8;         // rows of G that a thread has in flight
+
 struct NormArgs {
   const void* ids;
   const void* G;
-  const int32_t* order;     // positions by example, token, position
-  const int32_t* offsets;   // [B + 1]
-  float* partials;          // [B][parts * blocks]
-  int64_t jobs;             // B * parts * blocks
-  int32_t d, wide, parts, blocks;
+  const int32_t* order;     // T > kSortedInLds: positions by example, token, position
+  const int32_t* offsets;   // by example slot
+  Buckets examples, tokens;
+  float* partials;          // [B][wgs * blocks], or norms_sq itself where that is 1
+  int32_t T, n_rows, d;
+  int32_t wide, accumulate;
+  int32_t wgs, blocks;      // workgroups and column blocks of an example
+  int32_t units, parts;     // column vectors of a block, parts of a workgroup's entries
+  int32_t digits;           // of 8 bits, of a token
   float scale;
 };
 
-// First entry at or after s (of n) whose token differs from the entry before it.
-__device__ __forceinline__ int32_t group_start(const NormArgs& a, const int32_t* list, int32_t n,
-                                               int32_t s) {
-  const int lane = threadIdx.x & 63;
-  if (s <= 0) return 0;
-  for (; s < n; s += 64) {
-    const int32_t k = s + lane;
-    const bool starts = k < n && read_id(a.ids, a.wide, list[k]) != read_id(a.ids, a.wide, list[k - 1]);
-    const uint64_t b = __ballot(starts);
-    if (b) return s + __ffsll((unsigned long long)b) - 1;
+// An example's entries by token, in LDS ...
+struct LdsList {
+  const uint32_t* id;
+  const uint16_t* t;
+  __device__ __forceinline__ uint32_t group(int32_t k) const { return id[k]; }
+  __device__ __forceinline__ uint32_t row(int32_t k) const { return t[k]; }
+};
+
+// ... or its part of the list of all positions, groups in slot order.
+struct GlobalList {
+  const int32_t* order;
+  const void* ids;
+  Buckets tokens;
+  int32_t first;   // position of the example's first token
+  int32_t wide;
+  __device__ uint32_t group(int32_t k) const {
+    return tokens.slot((uint32_t)read_id(ids, wide, order[k]));
+  }
+  __device__ uint32_t row(int32_t k) const { return (uint32_t)(order[k] - first); }
+};
+
+// LDS of the sort: two buffers of tokens and of their places t, and the counters
+// of the digits.
+struct SortLds {
+  uint32_t* id[2];
+  uint16_t* t[2];
+  uint32_t* count;   // [kNormWaves][256]
+  uint32_t* sums;    // [4]
+};
+
+// Sorts the tokens of one example by (token, t), digit by digit, and returns how
+// many there are (empty positions are dropped); they end up in buffer
+// digits & 1. Every wave has a contiguous range of the list. Lanes with the same
+// digit find each other with eight ballots; the first of them adds their number
+// to the wave's counter, so a pass is stable and needs no atomics.
+__device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first, const SortLds& l) {
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const uint64_t below = (UINT64_C(1) << lane) - 1;
+  int32_t n = a.T;
+  for (int digit = 0; digit < a.digits; ++digit) {
+    const int from = digit & 1;
+    for (int k = threadIdx.x; k < kNormWaves * 256; k += kNormThreads) l.count[k] = 0;
+    __syncthreads();
+    const int32_t groups = (n + 63) >> 6, per = (groups + kNormWaves - 1) / kNormWaves;
+    uint32_t id[kLdsGroups], at[kLdsGroups], t[kLdsGroups];   // at: digit | rank << 8, ~0: none
+    volatile uint32_t* mine = l.count + wave * 256;
+#pragma unroll
+    for (int u = 0; u < kLdsGroups; ++u) {
+      at[u] = ~0u;
+      if (u >= per) continue;
+      const int32_t k = ((wave * per + u) << 6) + lane;
+      bool there = k < n;
+      id[u] = 0;
+      if (there) {
+        if (digit == 0) {
+          const int64_t v = read_id(a.ids, a.wide, first + k);
+          there = (uint64_t)v < (uint64_t)a.n_rows;
+          id[u] = (uint32_t)v;
+          t[u] = (uint32_t)k;
+        } else {
+          id[u] = l.id[from][k];
+          t[u] = l.t[from][k];
+        }
+      }
+      const uint32_t d = (id[u] >> (8 * digit)) & 255u;
+      uint64_t same = __ballot(there);
+#pragma unroll
+      for (int b = 0; b < 8; ++b) {
+        const bool set = d >> b & 1;
+        const uint64_t ones = __ballot(set);
+        same &= set ? ones : ~ones;
+      }
+      if (there) {
+        const uint32_t before = mine[d];
+        at[u] = d | (before + (uint32_t)__popcll(same & below)) << 8;
+        if ((same & below) == 0) mine[d] = before + (uint32_t)__popcll(same);
+      }
+    }
+    __syncthreads();
+    uint32_t total = 0, scan = 0;
+    if (threadIdx.x < 256) {
+#pragma unroll
+      for (int w = 0; w < kNormWaves; ++w) total += l.count[w * 256 + threadIdx.x];
+      scan = total;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) {
+        const uint32_t o = __shfl_up(scan, off, 64);
+        if (lane >= off) scan += o;
+      }
+      if (lane == 63) l.sums[wave] = scan;
+    }
+    __syncthreads();
+    if (threadIdx.x < 256) {
+      uint32_t place = scan - total;
+      for (int w = 0; w < wave; ++w) place += l.sums[w];
+#pragma unroll
+      for (int w = 0; w < kNormWaves; ++w) {
+        const uint32_t c = l.count[w * 256 + threadIdx.x];
+        l.count[w * 256 + threadIdx.x] = place;
+        place += c;
+      }
+    }
+    n = (int32_t)(l.sums[0] + l.sums[1] + l.sums[2] + l.sums[3]);
+    __syncthreads();
+#pragma unroll
+    for (int u = 0; u < kLdsGroups; ++u) {
+      if (at[u] == ~0u) continue;
+      const uint32_t to = l.count[wave * 256 + (at[u] & 255u)] + (at[u] >> 8);
+      l.id[from ^ 1][to] = id[u];
+      l.t[from ^ 1][to] = (uint16_t)t[u];
+    }
+    __syncthreads();
   }
   return n;
 }
 
-// One wave: the column block `blk` of the groups that start in part `part` of
-// example i's list.
-template <class T, int V>
-__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
-  const int64_t job = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  if (job >= a.jobs) return;
-  const int lane = threadIdx.x & 63;
-  const int64_t i = job / (a.parts * a.blocks);
-  const int rest = (int)(job - i * (a.parts * a.blocks));
-  const int part = rest / a.blocks, blk = rest - part * a.blocks;
-  const int32_t* list = a.order + a.offsets[i];
-  const int32_t n = a.offsets[i + 1] - a.offsets[i];
-  const int32_t s = group_start(a, list, n, (int32_t)((int64_t)n * part / a.parts));
-  const int32_t e = group_start(a, list, n, (int32_t)((int64_t)n * (part + 1) / a.parts));
-  const int col = (blk * 64 + lane) * V;
+// First entry at or after s (of n) that begins a group.
+template <class List>
+__device__ __forceinline__ int32_t group_start(const List& list, int32_t n, int32_t s) {
+  if (s <= 0 || s >= n) return s <= 0 ? 0 : n;
+  const uint32_t g = list.group(s - 1);
+  if (list.group(s) != g) return s;
+  int32_t lo = s, hi = n;   // lo is of group g, hi is not
+  while (hi - lo > 1) {
+    const int32_t mid = lo + (hi - lo) / 2;
+    if (list.group(mid) == g) lo = mid; else hi = mid;
+  }
+  return hi;
+}
+
+// Sum of squares of the group sums of the groups that start in one workgroup's
+// share of an example's list. A thread owns V columns and one part of the
+// share; parts are cut without regard to groups (one token may be most of an
+// example), so a part hands on the sum of its first and of its last group, and
+// part 0's threads join those in order.
+template <class T, int V, class List>
+__device__ __forceinline__ float group_squares(const NormArgs& a, const List& list, int32_t n,
+                                               int wg, int blk, const T* G, float* edges) {
+  const int part = threadIdx.x / a.units, u = threadIdx.x - part * a.units;
+  const int col = (blk * a.units + u) * V;
+  const bool mine = part < a.parts && col < a.d;
+  const int32_t of_wg = (n + a.wgs - 1) / a.wgs;
+  const int32_t S = a.wgs == 1 ? 0 : group_start(list, n, of_wg * wg < n ? of_wg * wg : n);
+  const int32_t E = a.wgs == 1 || n - of_wg * wg <= of_wg ? n : group_start(list, n, of_wg * (wg + 1));
+  const int32_t of_part = (E - S + a.parts - 1) / a.parts;
+  const auto cut = [&](int q) { return E - S - q * of_part < 0 ? E : S + q * of_part; };
   float ss = 0.0f;
-  if (col < a.d) {
+  if (mine) {
+    const int32_t s = cut(part), e = cut(part + 1);
     float acc[V] = {};
-    int64_t last = -1;
-    for (int32_t k = s; k < e; ++k) {
-      const int32_t p = list[k];
-      const int64_t id = read_id(a.ids, a.wide, p);
-      float x[V];
-      load_vec<V>(static_cast<const T*>(a.G) + (int64_t)p * a.d + col, x);
-      if (id != last) {
+    float* head = edges + (part * a.units + u) * V;
+    float* tail = head + a.parts * a.units * V;
+    bool first = true;
+    uint32_t last = s < e ? list.group(s) : 0;
+    for (int32_t k0 = s; k0 < e; k0 += kRowBatch) {
+      Raw<T, V> raw[kRowBatch];
+      uint32_t g[kRowBatch];
+#pragma unroll
+      for (int k = 0; k < kRowBatch; ++k) {
+        const int32_t at = k0 + k < e ? k0 + k : e - 1;
+        g[k] = list.group(at);
+        raw[k].load(G + (int64_t)list.row(at) * a.d + col);
+      }
+#pragma unroll
+      for (int k = 0; k < kRowBatch; ++k) {
+        if (k0 + k >= e) break;
+        float x[V];
+        raw[k].widen(x);
+        if (g[k] != last) {
+          if (first) {
+            store_vec<V>(head, acc);
+            first = false;
+          } else {
+#pragma unroll
+            for (int c = 0; c < V; ++c) ss = fmaf(acc[c], acc[c], ss);
+          }
+#pragma unroll
+          for (int c = 0; c < V; ++c) acc[c] = x[c];
+          last = g[k];
+        } else {
+#pragma unroll
+          for (int c = 0; c < V; ++c) acc[c] += x[c];
+        }
+      }
+    }
+    store_vec<V>(first ? head : tail, acc);
+  }
+  __syncthreads();
+  if (mine && part == 0) {
+    float acc[V] = {};
+    for (int q = 0; q < a.parts; ++q) {
+      const int32_t s = cut(q), e = cut(q + 1);
+      if (s >= e) break;
+      float x[V], y[V];
+      load_vec<V>(edges + (q * a.units + u) * V, x);
+      load_vec<V>(edges + ((a.parts + q) * a.units + u) * V, y);
+      if (s > S && list.group(s) != list.group(s - 1)) {
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           ss = fmaf(acc[c], acc[c], ss);
-          acc[c] = x[c];
+          acc[c] = 0.0f;
         }
-        last = id;
-      } else {
+      }
 #pragma unroll
-        for (int c = 0; c < V; ++c) acc[c] += x[c];
+      for (int c = 0; c < V; ++c) acc[c] += x[c];
+      if (list.group(s) != list.group(e - 1)) {   // otherwise y was not written
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          ss = fmaf(acc[c], acc[c], ss);
+          acc[c] = y[c];
+        }
       }
     }
 #pragma unroll
     for (int c = 0; c < V; ++c) ss = fmaf(acc[c], acc[c], ss);
   }
+  return ss;
+}
+
+// Bytes of LDS for the sort of an example of T tokens.
+__host__ __device__ inline int sort_lds_bytes(int T) {
+  const int padded = (T + 7) & ~7;
+  return padded * 12 + kNormWaves * 256 * 4 + 16;
+}
+
+template <class T, int V, bool IN_LDS>
+__global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
+  extern __shared__ __align__(16) char norm_lds[];
+  __shared__ float red[kNormWaves];
+  const uint32_t per = (uint32_t)(a.wgs * a.blocks);
+  const uint32_t i = blockIdx.x / per, rest = blockIdx.x - i * per;
+  const int wg = (int)(rest / (uint32_t)a.blocks), blk = (int)rest - wg * a.blocks;
+  const T* G = static_cast<const T*>(a.G) + (int64_t)i * a.T * a.d;
+  float ss;
+  if constexpr (IN_LDS) {
+    const int padded = (a.T + 7) & ~7;
+    SortLds l;
+    l.count = reinterpret_cast<uint32_t*>(norm_lds);
+    l.sums = l.count + kNormWaves * 256;
+    l.id[0] = l.sums + 4;
+    l.id[1] = l.id[0] + padded;
+    l.t[0] = reinterpret_cast<uint16_t*>(l.id[1] + padded);
+    l.t[1] = l.t[0] + padded;
+    const int32_t n = sort_example(a, (int64_t)i * a.T, l);
+    const int at = a.digits & 1;
+    ss = group_squares<T, V>(a, LdsList{l.id[at], l.t[at]}, n, wg, blk, G,
+                             reinterpret_cast<float*>(norm_lds + sort_lds_bytes(a.T)));
+  } else {
+    const uint32_t slot = a.examples.slot(i);
+    const int32_t s = a.offsets[slot], n = a.offsets[slot + 1] - s;
+    ss = group_squares<T, V>(a, GlobalList{a.order + s, a.ids, a.tokens, (int32_t)i * a.T, a.wide}, n, wg,
+                             blk, G, reinterpret_cast<float*>(norm_lds));
+  }
   ss = wave_sum(ss);
-  if (lane == 0) a.partials[job] = ss * a.scale * a.scale;
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = ss;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    float t = 0.0f;
+    for (int k = 0; k < kNormWaves; ++k) t += red[k];
+    t *= a.scale * a.scale;
+    a.partials[blockIdx.x] = a.accumulate ? a.partials[blockIdx.x] + t : t;
+  }
 }
 
 // --------------------------------------------------------------- clipped sum
 
+constexpr int kChunk = 32;         // entries of a chunk (one a lane, and one on each side)
+constexpr int kRowsPerWave = 16;   // table rows that a wave looks through for empty ones
+constexpr int kJoinThreads = 512;
+
 struct SumArgs {
+  const void* ids;
   const void* G;
   const int32_t* order;     // positions by token, position
-  const int32_t* offsets;   // [V + 1]
-  const float* factors;     // [B], NULL: all 1
+  const int32_t* offsets;   // by token slot
+  const float* norms_sq;    // [B], NULL: all factors 1
   float* grad;
   float* partials;          // [chunks][2][d]
-  int64_t V;
-  int64_t chunk_wgs;        // workgroups of the chunks, before those of the rows
-  int32_t chunks, chunk;    // chunks of the sorted list, entries of one
-  int32_t d, accumulate;
+  float* factors_out;
+  uint8_t* mask_out;
+  Buckets tokens;
+  int64_t V, B;
+  // Workgroups of the chunks, then of the empty rows, then of the factors.
+  uint32_t chunk_wgs, row_wgs;
+  int32_t chunks, blocks;   // chunks of the sorted list, column blocks of a row
+  int32_t d, accumulate, wide;
   uint32_t magic;           // division by T
   int32_t shift;
-  float scale;
+  float scale, C;
 };
-
-// Sum of factor * G over the entries [s, e) of the sorted list, V columns a lane.
-template <class T, int V>
-__device__ __forceinline__ void sum_rows(const SumArgs& a, int32_t s, int32_t e, int col,
-                                         float (&acc)[V]) {
-#pragma unroll
-  for (int c = 0; c < V; ++c) acc[c] = 0.0f;
-  for (int32_t k = s; k < e; ++k) {
-    const int32_t p = a.order[k];
-    const float f = a.factors ? a.factors[magic_divide((uint32_t)p, a.magic, a.shift)] : 1.0f;
-    if (f == 0.0f) continue;   // factor 0: the example's rows are not read
-    float x[V];
-    load_vec<V>(static_cast<const T*>(a.G) + (int64_t)p * a.d + col, x);
-#pragma unroll
-    for (int c = 0; c < V; ++c) acc[c] = fmaf(f, x[c], acc[c]);
-  }
-}
 
 template <int V>
 __device__ __forceinline__ void write_row(const SumArgs& a, int64_t v, int col, float (&acc)[V]) {
@@ -336,126 +610,209 @@ __device__ __forceinline__ void write_row(const SumArgs& a, int64_t v, int col, 
   store_vec<V>(out, acc);
 }
 
-// Token whose entries hold list position k: the last v with offsets[v] <= k.
-__device__ __forceinline__ int64_t token_at(const SumArgs& a, int32_t k) {
-  int64_t lo = 0, hi = a.V - 1;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi + 1) >> 1;
-    if (a.offsets[mid] <= k) lo = mid; else hi = mid - 1;
+// One chunk of the sorted list and one block of 64 V columns. Lane l holds entry
+// s - 1 + l: its position, token and factor. A token's sum goes to its row of
+// grad if all of its entries are in the chunk, to partial row 0 of the chunk if
+// entries of it come before, and to partial row 1 otherwise.
+template <class T, int V>
+__device__ __forceinline__ void sum_chunk(const SumArgs& a, int32_t q, int blk) {
+  const int lane = threadIdx.x & 63;
+  const int32_t total = a.offsets[a.tokens.R << a.tokens.log];
+  const int32_t s = q * kChunk;
+  if (s >= total) return;
+  const int32_t n = total - s < kChunk ? total - s : kChunk;
+  const int32_t k = s - 1 + lane;
+  int32_t p = 0, token = -1;
+  float f = 0.0f;
+  if (lane <= n + 1 && k >= 0 && k < total) {
+    p = a.order[k];
+    token = (int32_t)read_id(a.ids, a.wide, p);
+    f = 1.0f;
+    if (a.norms_sq) f = clip_factor(a.norms_sq[magic_divide((uint32_t)p, a.magic, a.shift)], a.C);
   }
-  return lo;
+  const int32_t before = __shfl_up(token, 1, 64);
+  const uint64_t starts = __ballot(lane == 0 || token != before);
+  const int col = (blk * 64 + lane) * V;
+  const bool mine = col < a.d;
+  const T* G = static_cast<const T*>(a.G) + col;
+  float acc[V] = {};
+  bool open = !(starts >> 1 & 1);   // the sum at hand began in an earlier chunk
+  const auto flush = [&](int last, bool more) {   // `last`: lane of its last entry
+    const int32_t v = __builtin_amdgcn_readlane(token, last);
+    if (mine) {
+      if (!open && !more)
+        write_row<V>(a, v, col, acc);
+      else
+        store_vec<V>(a.partials + ((int64_t)q * 2 + (open ? 0 : 1)) * a.d + col, acc);
+    }
+    open = false;
+#pragma unroll
+    for (int c = 0; c < V; ++c) acc[c] = 0.0f;
+  };
+  for (int j0 = 1; j0 <= n; j0 += kRowBatch) {
+    Raw<T, V> raw[kRowBatch];
+    float fj[kRowBatch];
+#pragma unroll
+    for (int j = 0; j < kRowBatch; ++j) {
+      // An example of factor 0 is not read.
+      fj[j] = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), j0 + j));
+      const int32_t pj = __builtin_amdgcn_readlane(p, j0 + j);
+      raw[j].zero();
+      if (mine && j0 + j <= n && fj[j] != 0.0f) raw[j].load(G + (int64_t)pj * a.d);
+    }
+#pragma unroll
+    for (int j = 0; j < kRowBatch; ++j) {
+      if (j0 + j > n) break;
+      if (j0 + j > 1 && (starts >> (j0 + j) & 1)) flush(j0 + j - 1, false);
+      float x[V];
+      raw[j].widen(x);
+#pragma unroll
+      for (int c = 0; c < V; ++c) acc[c] = fmaf(fj[j], x[c], acc[c]);
+    }
+  }
+  flush(n, !(starts >> (n + 1) & 1));
 }
 
-// A wave per row of the table; rows with more than `chunk` entries are left to
-// the waves of the chunks, each of which sums the entries of its chunk that
-// belong to such a row: at most two of them, one that began before or at the
-// chunk's start (slot 0) and one that begins inside it (slot 1).
 template <class T, int V>
 __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   const int lane = threadIdx.x & 63;
-  const int wave = threadIdx.x >> 6;
-  if (blockIdx.x < a.chunk_wgs) {
-    const int64_t q = (int64_t)blockIdx.x * (kThreads / 64) + wave;
-    if (q >= a.chunks) return;
-    const int32_t total = a.offsets[a.V];
-    const int32_t s = (int32_t)q * a.chunk;
-    if (s >= total) return;
-    const int32_t e = s + a.chunk < total ? s + a.chunk : total;
-    const int64_t v0 = token_at(a, s), v1 = token_at(a, e - 1);
-    for (int slot = 0; slot < 2; ++slot) {
-      const int64_t v = slot == 0 ? v0 : v1;
-      if (slot == 1 && v1 == v0) break;
-      const int32_t vs = a.offsets[v], ve = a.offsets[v + 1];
-      if (ve - vs <= a.chunk) continue;
-      float* out = a.partials + (q * 2 + slot) * a.d;
-      for (int col = lane * V; col < a.d; col += 64 * V) {
-        float acc[V];
-        sum_rows<T, V>(a, vs > s ? vs : s, ve < e ? ve : e, col, acc);
-        store_vec<V>(out + col, acc);
-      }
-    }
+  const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t wg = blockIdx.x;
+  if (wg < a.chunk_wgs) {
+    const uint32_t job = wg * (kThreads / 64) + wave, q = job / (uint32_t)a.blocks;
+    if (q < (uint32_t)a.chunks) sum_chunk<T, V>(a, (int32_t)q, (int)(job - q * a.blocks));
     return;
   }
-  const int64_t v = ((int64_t)blockIdx.x - a.chunk_wgs) * (kThreads / 64) + wave;
-  if (v >= a.V) return;
-  const int32_t s = a.offsets[v], e = a.offsets[v + 1];
-  if ((s == e && a.accumulate) || (a.chunks > 0 && e - s > a.chunk)) return;
-  for (int col = lane * V; col < a.d; col += 64 * V) {
-    float acc[V];
-    sum_rows<T, V>(a, s, e, col, acc);
-    write_row<V>(a, v, col, acc);
+  wg -= a.chunk_wgs;
+  if (wg >= a.row_wgs) {   // the factors and the mask, where they are asked for
+    const int64_t i = (int64_t)(wg - a.row_wgs) * kThreads + threadIdx.x;
+    if (i < a.B) write_factor(a.norms_sq[i], a.C, i, nullptr, a.factors_out, a.mask_out);
+    return;
+  }
+  // Rows without a token.
+  const int64_t v0 = ((int64_t)wg * (kThreads / 64) + wave) * kRowsPerWave;
+  bool empty = false;
+  if (lane < kRowsPerWave && v0 + lane < a.V) {
+    const uint32_t slot = a.tokens.slot((uint32_t)(v0 + lane));
+    empty = a.offsets[slot] == a.offsets[slot + 1];
+  }
+  float zero[V] = {};
+  for (uint64_t left = __ballot(empty); left; left &= left - 1) {
+    float* row = a.grad + (v0 + __ffsll((unsigned long long)left) - 1) * a.d;
+    for (int col = lane * V; col < a.d; col += 64 * V) store_vec<V>(row + col, zero);
   }
 }
 
-// Joins the partial sums of each row with more than `chunk` entries: the
-// workgroups of the chunk in which the row begins add them in order.
+// Joins the partial rows of the token that begins in chunk q and goes on after
+// it, if there is one: row 1 of chunk q, rows 0 of the chunks after it. Each wave
+// adds a range of them in order, then wave 0 the waves' sums.
 template <int V>
-__global__ __launch_bounds__(kThreads) void join_kernel(SumArgs a) {
+__global__ __launch_bounds__(kJoinThreads) void join_kernel(SumArgs a) {
+  __shared__ float sums[kJoinThreads / 64][64 * V];
   const int32_t q = blockIdx.x;
-  const int32_t total = a.offsets[a.V];
-  const int32_t s = q * a.chunk;
-  if (s >= total) return;
-  const int32_t e = s + a.chunk < total ? s + a.chunk : total;
-  for (int slot = 0; slot < 2; ++slot) {
-    const int64_t v = token_at(a, slot == 0 ? s : e - 1);
-    const int32_t vs = a.offsets[v], ve = a.offsets[v + 1];
-    if (vs < s || ve - vs <= a.chunk) continue;
-    if (slot == 1 && vs == s) break;   // the row of slot 0
-    const int32_t last = (ve - 1) / a.chunk;
-    for (int col = ((int)blockIdx.y * kThreads + (int)threadIdx.x) * V; col < a.d;
-         col += (int)gridDim.y * kThreads * V) {
-      float acc[V];
-      load_vec<V>(a.partials + ((int64_t)q * 2 + slot) * a.d + col, acc);
-      for (int32_t k = q + 1; k <= last; ++k) {
-        float x[V];
-        load_vec<V>(a.partials + (int64_t)k * 2 * a.d + col, x);
+  const int32_t total = a.offsets[a.tokens.R << a.tokens.log];
+  const int32_t s = q * kChunk;
+  if (total - s <= kChunk) return;   // nothing comes after this chunk
+  const int32_t token = (int32_t)read_id(a.ids, a.wide, a.order[s + kChunk - 1]);
+  const uint32_t slot = a.tokens.slot((uint32_t)token);
+  const int32_t begin = a.offsets[slot], end = a.offsets[slot + 1];
+  if (begin < s || end <= s + kChunk) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int col = ((int)blockIdx.y * 64 + lane) * V;
+  const int32_t n = (end - 1) / kChunk - q + 1;   // partial rows
+  const int32_t per = (n + kJoinThreads / 64 - 1) / (kJoinThreads / 64);
+  const int32_t from = wave * per, to = from + per < n ? from + per : n;
+  float acc[V] = {};
+  if (col < a.d) {
+#pragma unroll 4
+    for (int32_t k = from; k < to; ++k) {
+      float x[V];
+      load_vec<V>(a.partials + ((int64_t)(q + k) * 2 + (k == 0 ? 1 : 0)) * a.d + col, x);
 #pragma unroll
-        for (int c = 0; c < V; ++c) acc[c] += x[c];
-      }
-      write_row<V>(a, v, col, acc);
+      for (int c = 0; c < V; ++c) acc[c] += x[c];
     }
   }
+#pragma unroll
+  for (int c = 0; c < V; ++c) sums[wave][c * 64 + lane] = acc[c];
+  __syncthreads();
+  if (wave == 0 && col < a.d) {
+    for (int w = 1; w < kJoinThreads / 64 && w * per < n; ++w)
+#pragma unroll
+      for (int c = 0; c < V; ++c) acc[c] += sums[w][c * 64 + lane];
+    write_row<V>(a, token, col, acc);
+  }
 }
 
-// Entries of one chunk of the sorted list: at least 64, at most about 1024 chunks.
-int32_t chunk_entries(int64_t N) {
-  const int64_t c = ceil_div(N, 1024);
-  return (int32_t)(c < 64 ? 64 : c);
+// Chunks of the sorted list.
+int64_t chunk_count(int64_t N) { return ceil_div(N, kChunk); }
+
+// Split of the norms' work: column vectors over the threads of `blocks` blocks,
+// what is left of a workgroup over `parts` parts of its entries (at least 8
+// each), and, for few examples, several workgroups an example, so that about 256
+// run. From 96 examples on one workgroup each has enough loads in flight to
+// fill the memory system, and no launch is needed to add up partial sums.
+struct NormPlan {
+  int vec, blocks, units, parts, wgs;
+  bool in_lds;
+};
+
+NormPlan norm_plan(const dpsgd_embedding& e, int32_t dtype) {
+  NormPlan p;
+  p.vec = vec_width(e.d, dtype == DPSGD_BF16 ? 8 : 4);
+  const int64_t units = e.d / p.vec;
+  p.blocks = (int)ceil_div(units, kNormThreads);
+  p.units = (int)ceil_div(units, p.blocks);
+  int64_t parts = kNormThreads / p.units;
+  if (parts > kMostParts) parts = kMostParts;
+  if (parts > ceil_div(e.T, 8)) parts = ceil_div(e.T, 8);
+  p.parts = (int)parts;
+  int64_t wgs = e.B * p.blocks >= 96 ? 1 : ceil_div(256, e.B * p.blocks);
+  const int64_t most = ceil_div(e.T, 8 * parts);
+  p.wgs = (int)(wgs < most ? wgs : most);
+  p.in_lds = e.T <= kSortedInLds;
+  return p;
 }
 
-// Chunks of the sorted list; none where no row can have more than one.
-int32_t chunk_count(int64_t N) {
-  const int64_t c = chunk_entries(N);
-  return N <= c ? 0 : (int32_t)ceil_div(N, c);
+size_t order_bytes(int64_t N) { return round_up((size_t)N * sizeof(int32_t), 256); }
+size_t list_bytes(int64_t N, const Buckets& b) {
+  return order_bytes(N) + round_up((size_t)(b.slots() + 1) * sizeof(int32_t), 256);
 }
 
-// Column blocks (of one wave) and parts of an example's list.
-void norm_jobs(int64_t B, int64_t T, int64_t d, int* vec, int* blocks, int* parts) {
-  *vec = vec_width(d, 4);
-  *blocks = (int)ceil_div(d, 64 * *vec);
-  int64_t p = ceil_div(8192, B * *blocks);
-  const int64_t most = ceil_div(T, 8);
-  *parts = (int)(p < most ? p : most);
+int sort_tokens(const dpsgd_embedding& e, const Buckets& b, int32_t* order, int32_t* offsets,
+                hipStream_t stream) {
+  if (e.index_dtype == DPSGD_I64)
+    return launch_sort(TokenKey<int64_t>{static_cast<const int64_t*>(e.ids), (int32_t)(e.B * e.T)}, b, order, offsets,
+                       stream);
+  return launch_sort(TokenKey<int32_t>{static_cast<const int32_t*>(e.ids), (int32_t)(e.B * e.T)}, b, order, offsets,
+                     stream);
 }
 
-size_t list_bytes(int64_t N, int64_t keys) {
-  return round_up((size_t)N * sizeof(int32_t), 256) + round_up((size_t)(keys + 1) * sizeof(int32_t), 256);
-}
-
-TokenKey token_key(const dpsgd_embedding& e) {
-  return TokenKey{e.ids, e.index_dtype == DPSGD_I64, (uint32_t)e.n_rows, e.B * e.T};
+template <class T, int V>
+void launch_norm_kernel(const NormPlan& p, const NormArgs& a, uint32_t wgs, hipStream_t stream) {
+  const size_t edges = 2 * (size_t)p.parts * p.units * V * sizeof(float);
+  if (p.in_lds)
+    hipLaunchKernelGGL((norm_kernel<T, V, true>), dim3(wgs), dim3(kNormThreads),
+                       (size_t)sort_lds_bytes(a.T) + edges, stream, a);
+  else
+    hipLaunchKernelGGL((norm_kernel<T, V, false>), dim3(wgs), dim3(kNormThreads), edges, stream, a);
 }
 
 }  // namespace
 
+// Workspace: the list by token (order, offsets); then, for the norms, the list by
+// example (T > kSortedInLds) and the partial sums, or, for the sum, the chunks'
+// partial rows.
 size_t embedding_workspace_bytes(const dpsgd_embedding& e) {
   const int64_t N = e.B * e.T;
-  int vec, blocks, parts;
-  norm_jobs(e.B, e.T, e.d, &vec, &blocks, &parts);
-  const size_t norms = list_bytes(N, e.B) + (size_t)(e.B * blocks * parts) * sizeof(float);
-  const size_t sum = round_up((size_t)e.B * sizeof(float), 256) +
-                     (size_t)chunk_count(N) * 2 * (size_t)e.d * sizeof(float);
-  return list_bytes(N, e.n_rows) + (norms > sum ? norms : sum);
+  size_t partials = 0;
+  for (int32_t dtype : {DPSGD_F32, DPSGD_BF16}) {
+    const NormPlan p = norm_plan(e, dtype);
+    const size_t n = (size_t)(e.B * p.wgs * p.blocks) * sizeof(float);
+    partials = n > partials ? n : partials;
+  }
+  const size_t norms = (e.T > kSortedInLds ? list_bytes(N, buckets_of(e.B)) : 0) + partials;
+  const size_t sum = (size_t)chunk_count(N) * 2 * (size_t)e.d * sizeof(float);
+  return list_bytes(N, buckets_of(e.n_rows)) + (norms > sum ? norms : sum);
 }
 
 int launch_embedding_lookup(const dpsgd_embedding& e, const void* table, int32_t table_dtype,
@@ -470,49 +827,64 @@ int launch_embedding_lookup(const dpsgd_embedding& e, const void* table, int32_t
 int launch_embedding_norms(const dpsgd_embedding& e, const void* G, int32_t dtype, float* norms_sq,
                            int accumulate, void* workspace, hipStream_t stream) {
   const int64_t N = e.B * e.T;
-  char* ws = static_cast<char*>(workspace);
-  int32_t* order = reinterpret_cast<int32_t*>(ws);
-  int32_t* offsets = reinterpret_cast<int32_t*>(ws + round_up((size_t)N * sizeof(int32_t), 256));
-  ws += list_bytes(N, e.n_rows);
-  int32_t* by_example = reinterpret_cast<int32_t*>(ws);
-  int32_t* starts = reinterpret_cast<int32_t*>(ws + round_up((size_t)N * sizeof(int32_t), 256));
-  float* partials = reinterpret_cast<float*>(ws + list_bytes(N, e.B));
-  int st = launch_sort(token_key(e), order, offsets, stream);
-  if (st != DPSGD_OK) return st;
-  ExampleKey ex{order, offsets + e.n_rows, 0, 0, (uint32_t)e.B};
-  divide_magic(e.T, &ex.magic, &ex.shift);
-  st = launch_sort(ex, by_example, starts, stream);
-  if (st != DPSGD_OK) return st;
+  const NormPlan p = norm_plan(e, dtype);
+  const int64_t wgs = e.B * p.wgs * p.blocks;
+  if (wgs > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
   NormArgs a{};
   a.ids = e.ids;
   a.G = G;
-  a.order = by_example;
-  a.offsets = starts;
-  a.partials = partials;
+  a.T = (int32_t)e.T;
+  a.n_rows = (int32_t)e.n_rows;
+  a.digits = 1;
+  while (a.digits < 4 && (e.n_rows - 1) >> (8 * a.digits)) ++a.digits;
   a.d = (int32_t)e.d;
   a.wide = e.index_dtype == DPSGD_I64;
+  a.wgs = p.wgs;
+  a.blocks = p.blocks;
+  a.units = p.units;
+  a.parts = p.parts;
   a.scale = e.scale;
-  int vec;
-  norm_jobs(e.B, e.T, e.d, &vec, &a.blocks, &a.parts);
-  a.jobs = e.B * a.parts * a.blocks;
-  const int64_t wgs = ceil_div(a.jobs, kThreads / 64);
-  if (wgs > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
-  const dim3 grid((uint32_t)wgs), block(kThreads);
-#define DPSGD_NORMS(T)                                                                              \
-  switch (vec) {                                                                                    \
-    case 4: hipLaunchKernelGGL((norm_kernel<T, 4>), grid, block, 0, stream, a); break;              \
-    case 2: hipLaunchKernelGGL((norm_kernel<T, 2>), grid, block, 0, stream, a); break;              \
-    default: hipLaunchKernelGGL((norm_kernel<T, 1>), grid, block, 0, stream, a); break;             \
+  a.tokens = buckets_of(e.n_rows);
+  char* ws = static_cast<char*>(workspace);
+  char* partials = ws + list_bytes(N, a.tokens);
+  int st = DPSGD_OK;
+  if (!p.in_lds) {
+    int32_t* order = reinterpret_cast<int32_t*>(ws);
+    int32_t* offsets = reinterpret_cast<int32_t*>(ws + order_bytes(N));
+    a.examples = buckets_of(e.B);
+    int32_t* by_example = reinterpret_cast<int32_t*>(partials);
+    int32_t* starts = reinterpret_cast<int32_t*>(partials + order_bytes(N));
+    partials += list_bytes(N, a.examples);
+    st = sort_tokens(e, a.tokens, order, offsets, stream);
+    if (st != DPSGD_OK) return st;
+    ExampleKey ex{order, offsets + a.tokens.slots(), 0, 0};
+    divide_magic(e.T, &ex.magic, &ex.shift);
+    st = launch_sort(ex, a.examples, by_example, starts, stream);
+    if (st != DPSGD_OK) return st;
+    a.order = by_example;
+    a.offsets = starts;
   }
+  const bool whole = p.wgs * p.blocks == 1;   // one workgroup an example: no partial sums
+  a.partials = whole ? norms_sq : reinterpret_cast<float*>(partials);
+  a.accumulate = whole && accumulate;
+  const uint32_t w = (uint32_t)wgs;
   if (dtype == DPSGD_BF16) {
-    DPSGD_NORMS(uint16_t)
+    switch (p.vec) {
+      case 8: launch_norm_kernel<uint16_t, 8>(p, a, w, stream); break;
+      case 4: launch_norm_kernel<uint16_t, 4>(p, a, w, stream); break;
+      case 2: launch_norm_kernel<uint16_t, 2>(p, a, w, stream); break;
+      default: launch_norm_kernel<uint16_t, 1>(p, a, w, stream); break;
+    }
   } else {
-    DPSGD_NORMS(float)
+    switch (p.vec) {
+      case 4: launch_norm_kernel<float, 4>(p, a, w, stream); break;
+      case 2: launch_norm_kernel<float, 2>(p, a, w, stream); break;
+      default: launch_norm_kernel<float, 1>(p, a, w, stream); break;
+    }
   }
-#undef DPSGD_NORMS
   st = check_launch();
-  if (st != DPSGD_OK) return st;
-  return launch_norms_reduce(partials, (int64_t)a.parts * a.blocks, e.B, norms_sq, accumulate, stream);
+  if (st != DPSGD_OK || whole) return st;
+  return launch_norms_reduce(a.partials, (int64_t)p.wgs * p.blocks, e.B, norms_sq, accumulate, stream);
 }
 
 int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
@@ -521,44 +893,46 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
                          hipStream_t stream) {
   const int64_t N = e.B * e.T;
   char* ws = static_cast<char*>(workspace);
-  int32_t* order = reinterpret_cast<int32_t*>(ws);
-  int32_t* offsets = reinterpret_cast<int32_t*>(ws + round_up((size_t)N * sizeof(int32_t), 256));
-  ws += list_bytes(N, e.n_rows);
-  float* factors = reinterpret_cast<float*>(ws);
-  int st = DPSGD_OK;
-  if (norms_sq) {
-    st = launch_clip_factors(norms_sq, e.B, C, factors, factors_out, mask_out, stream);
-    if (st != DPSGD_OK) return st;
-  }
-  st = launch_sort(token_key(e), order, offsets, stream);
-  if (st != DPSGD_OK) return st;
   SumArgs a{};
+  a.tokens = buckets_of(e.n_rows);
+  int32_t* order = reinterpret_cast<int32_t*>(ws);
+  int32_t* offsets = reinterpret_cast<int32_t*>(ws + order_bytes(N));
+  const int st = sort_tokens(e, a.tokens, order, offsets, stream);
+  if (st != DPSGD_OK) return st;
+  a.ids = e.ids;
   a.G = G;
   a.order = order;
   a.offsets = offsets;
-  a.factors = norms_sq ? factors : nullptr;
+  a.norms_sq = norms_sq;
   a.grad = grad;
-  a.partials = reinterpret_cast<float*>(ws + round_up((size_t)e.B * sizeof(float), 256));
+  a.partials = reinterpret_cast<float*>(ws + list_bytes(N, a.tokens));
+  a.factors_out = factors_out;
+  a.mask_out = mask_out;
   a.V = e.n_rows;
-  a.chunk = chunk_entries(N);
-  a.chunks = chunk_count(N);
-  a.chunk_wgs = ceil_div(a.chunks, kThreads / 64);
+  a.B = e.B;
   a.d = (int32_t)e.d;
   a.accumulate = accumulate;
+  a.wide = e.index_dtype == DPSGD_I64;
   a.scale = e.scale;
+  a.C = C;
   divide_magic(e.T, &a.magic, &a.shift);
-  const int64_t wgs = a.chunk_wgs + ceil_div(a.V, kThreads / 64);
-  if (wgs > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
   const int vec = vec_width(e.d, 4);
-  const dim3 grid((uint32_t)wgs), block(kThreads);
-  const dim3 jgrid((uint32_t)a.chunks, (uint32_t)ceil_div(e.d, (int64_t)kThreads * vec));
+  a.chunks = (int32_t)chunk_count(N);
+  a.blocks = (int32_t)ceil_div(e.d, 64 * vec);
+  const int64_t chunk_wgs = ceil_div((int64_t)a.chunks * a.blocks, kThreads / 64);
+  const int64_t row_wgs = accumulate ? 0 : ceil_div(a.V, kThreads / 64 * kRowsPerWave);
+  const int64_t wgs = chunk_wgs + row_wgs + (factors_out || mask_out ? ceil_div(e.B, kThreads) : 0);
+  if (wgs > 0x1FFFFFFF) return DPSGD_ERR_INVALID_ARG;   // jobs stay below 2^31
+  a.chunk_wgs = (uint32_t)chunk_wgs;
+  a.row_wgs = (uint32_t)row_wgs;
+  const dim3 grid((uint32_t)wgs), block(kThreads), jgrid((uint32_t)a.chunks, (uint32_t)a.blocks);
 #define DPSGD_SUM(V)                                                                                \
   if (dtype == DPSGD_BF16) {                                                                        \
     hipLaunchKernelGGL((sum_kernel<uint16_t, V>), grid, block, 0, stream, a);                       \
   } else {                                                                                          \
     hipLaunchKernelGGL((sum_kernel<float, V>), grid, block, 0, stream, a);                          \
   }                                                                                                 \
-  if (a.chunks > 0) hipLaunchKernelGGL(join_kernel<V>, jgrid, block, 0, stream, a);
+  if (a.chunks > 1) hipLaunchKernelGGL(join_kernel<V>, jgrid, dim3(kJoinThreads), 0, stream, a);
   switch (vec) {
     case 4: DPSGD_SUM(4) break;
     case 2: DPSGD_SUM(2) break;

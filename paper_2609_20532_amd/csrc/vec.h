@@ -77,6 +77,50 @@ __device__ __forceinline__ void store_vec(uint16_t* p, const float (&x)[V]) {
   }
 }
 
+// The same elements as they lie in memory, in registers: for loads that stay in
+// flight while others are issued.
+template <class T, int V>
+struct Raw {
+  static constexpr int kBytes = V * (int)sizeof(T);
+  uint32_t w[kBytes >= 4 ? kBytes / 4 : 1];
+
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int k = 0; k < kBytes / 16; ++k) {
+        const uint4 q = reinterpret_cast<const uint4*>(p)[k];
+        w[4 * k] = q.x;
+        w[4 * k + 1] = q.y;
+        w[4 * k + 2] = q.z;
+        w[4 * k + 3] = q.w;
+      }
+    } else if constexpr (kBytes == 8) {
+      const uint2 q = *reinterpret_cast<const uint2*>(p);
+      w[0] = q.x;
+      w[1] = q.y;
+    } else if constexpr (kBytes == 4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else {
+      w[0] = *reinterpret_cast<const uint16_t*>(p);
+    }
+  }
+
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (uint32_t& x : w) x = 0;
+  }
+
+  __device__ __forceinline__ void widen(float (&x)[V]) const {
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      if constexpr (sizeof(T) == 4)
+        x[c] = __uint_as_float(w[c]);
+      else
+        x[c] = c & 1 ? bf16_hi(w[c / 2]) : bf16_lo(w[c / 2]);
+    }
+  }
+};
+
 // Largest of 8, 4, 2, 1 (at most `most`) that divides n.
 inline int vec_width(int64_t n, int most) {
   for (int v = most; v > 1; v >>= 1)

@@ -75,6 +75,9 @@ SHAPES = [   # B, T, V, d, ids
     (2, 1100, 40, 520, "words"),
     (300, 4, 33, 8, "padded"),          # more examples than workgroups of the sort
     (1, 4500, 700, 24, "words"),        # one long example
+    (1, 4096, 900, 128, "words"),       # the longest that is sorted in LDS, and the most of it
+    (2, 4097, 3, 72, "uniform"),        # the shortest that is not; few tokens, each most of a part
+    (3, 2500, 2, 136, "padded"),
 ]
 
 

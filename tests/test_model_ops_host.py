@@ -31,7 +31,7 @@ def _gn(**kw):
 BAD_EMB = [
     (dict(B=0), INVALID), (dict(T=0), INVALID), (dict(n_rows=0), INVALID), (dict(d=0), INVALID),
     (dict(B=1 << 20, T=1 << 12), INVALID), (dict(n_rows=1 << 31), INVALID),
-    (dict(d=(1 << 30) + 1), INVALID), (dict(n_rows=1 << 30, d=1 << 20), INVALID),
+    (dict(d=(1 << 20) + 1), INVALID), (dict(B=1 << 15, T=(1 << 15) + 1), INVALID), (dict(n_rows=1 << 30, d=1 << 20), INVALID),
     (dict(ids=None), INVALID), (dict(ids=66), INVALID), (dict(ids=68, index_dtype=1), INVALID),
     (dict(index_dtype=2), UNSUPPORTED), (dict(scale=float("nan")), INVALID),
     (dict(scale=float("inf")), INVALID),
