@@ -23,13 +23,25 @@
 namespace dpsgd {
 namespace {
 
+// Inclusive sum over the lanes of a wave: shifts within rows of 16 lanes, then
+// the rows' last lanes to the rows after them (six adds, no LDS).
+__device__ __forceinline__ int32_t wave_scan(int32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr 1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast 15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast 31
+  return x;
+}
+
 // ------------------------------------------------------------------- sorting
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWaves = kSortThreads / 64;
 constexpr int kSortBuckets = 256;    // one workgroup a bucket, one round on the chip
 constexpr int kMaxKeysPerWg = 512;   // LDS: kSortWaves counters a key
-constexpr int kSortList = 256;       // matches that a wave keeps in LDS
+constexpr int kSortList = 384;       // matches that a wave keeps in LDS
 constexpr int kSortBatch = 8;        // loads that a lane has in flight
 
 // Order of the keys [0, n) in a sorted list: by the low bits first (the bucket),
@@ -84,107 +96,91 @@ struct ExampleKey {   // key of entry k of a list of positions: its example
   __device__ __forceinline__ int32_t value(int32_t k) const { return order[k]; }
 };
 
-// Writes the entries of one group of 64 (at most) to their places: entry `value`
-// of key m for the lanes of `left`, in lane order; one round a distinct key.
-__device__ __forceinline__ void place_group(uint64_t left, uint32_t m, int32_t value,
-                                            volatile int32_t* place, int32_t* order) {
-  const int lane = threadIdx.x & 63;
-  while (left) {
-    const int first = __ffsll((unsigned long long)left) - 1;
-    const uint32_t m0 = (uint32_t)__builtin_amdgcn_readlane((int)m, first);
-    const uint64_t same = __ballot(m == m0) & left;
-    const int32_t at = place[m0];
-    if (same >> lane & 1) order[at + __popcll(same & ((UINT64_C(1) << lane) - 1))] = value;
-    if (lane == first) place[m0] = at + __popcll(same);
-    left &= ~same;
-  }
-}
-
 // Stable counting sort in one launch: workgroup w owns bucket w and reads the
 // whole list. Its waves have one contiguous range of the list each. They count
-// the entries of the smaller buckets and, key by key, those of their own, which
-// they keep in LDS in list order (kSortList of them; a wave that finds more
-// reads the rest of its range again). A prefix over keys and waves gives every
-// wave its places. No entry's place depends on the order of an atomic (the
-// counts are integers).
+// the entries of the smaller buckets, and keep their own bucket's in LDS, in
+// list order (kSortList of them; a wave that finds more reads the rest of its
+// range again). Key by key counts of those and a prefix over keys and waves
+// give every wave its places. No entry's place depends on the order of an
+// atomic (the counts are integers).
 template <class Key>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk, int32_t* order,
                                                             int32_t* offsets) {
   extern __shared__ __align__(16) int32_t lds[];
-  __shared__ int32_t kept_value[kSortWaves][kSortList];
-  __shared__ uint16_t kept_key[kSortWaves][kSortList];
+  __shared__ uint2 kept_of[kSortWaves][kSortList];   // value, key within the bucket
   __shared__ int32_t less_of[kSortWaves];
   const uint32_t R = bk.R, w = blockIdx.x, mask = (1u << bk.log) - 1u;
   int32_t* table = lds;                       // [kSortWaves][R]
   int32_t* total = lds + kSortWaves * R;      // [R]
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const uint64_t below = (UINT64_C(1) << lane) - 1;
   const int32_t N = keys.count();
   const int32_t groups = (N >> 6) + ((N & 63) != 0), per = (groups + kSortWaves - 1) / kSortWaves;
-  // Groups of 64 entries of this wave.
+  // Groups of 64 entries of this wave, and the end of its entries.
   const int32_t first = per * wave < groups ? per * wave : groups;
   const int32_t last = first + per < groups ? first + per : groups;
+  const int32_t end = last == groups ? N : last << 6;
 
   for (uint32_t k = threadIdx.x; k < kSortWaves * R; k += kSortThreads) table[k] = 0;
-  __syncthreads();
+  uint2* list = kept_of[wave];
   int32_t less = 0, kept = 0;
   int32_t again = last;   // first group whose matches were not kept
   for (int32_t g = first; g < last; g += kSortBatch) {
+    const int32_t k0 = (g << 6) + lane;
     uint32_t key[kSortBatch];
-    if (g + kSortBatch <= last && (g + kSortBatch) <= N >> 6) {   // every entry is there
+    if (g + kSortBatch <= last && (g + kSortBatch) << 6 <= end) {   // every entry is there
 #pragma unroll
-      for (int u = 0; u < kSortBatch; ++u) key[u] = keys.key((g << 6) + lane + u * 64);
+      for (int u = 0; u < kSortBatch; ++u) key[u] = keys.key(k0 + u * 64);
     } else {
 #pragma unroll
-      for (int u = 0; u < kSortBatch; ++u)
-        key[u] = g + u < last && (((g + u) << 6) + lane) < N ? keys.key(((g + u) << 6) + lane) : 0xFFFFFFFFu;
+      for (int u = 0; u < kSortBatch; ++u) {
+        const int32_t k = k0 + u * 64;
+        key[u] = keys.key(k < end ? k : end - 1);
+        if (k >= end) key[u] = 0xFFFFFFFFu;
+      }
     }
 #pragma unroll
     for (int u = 0; u < kSortBatch; ++u) {
       const uint32_t b = key[u] < bk.n ? key[u] & mask : 0xFFFFFFFFu;
       less += b < w;
       const uint64_t hits = __ballot(b == w);
-      if (hits) {
-        const uint32_t m = key[u] >> bk.log;
-        if (b == w) atomicAdd(&table[wave * R + m], 1);
+      if (hits && again == last) {
         const int32_t more = __popcll(hits);
-        if (again == last && kept + more <= kSortList) {
-          if (b == w) {
-            const int at = kept + __popcll(hits & ((UINT64_C(1) << lane) - 1));
-            kept_value[wave][at] = keys.value(((g + u) << 6) + lane);
-            kept_key[wave][at] = (uint16_t)m;
-          }
+        if (kept + more <= kSortList) {
+          if (b == w) list[kept + __popcll(hits & below)] = make_uint2((uint32_t)keys.value(k0 + u * 64),
+                                                                       key[u] >> bk.log);
           kept += more;
-        } else if (again == last) {
+        } else {
           again = g + u;
         }
       }
     }
   }
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) less += __shfl_xor(less, off, 64);
-  if (lane == 0) less_of[wave] = less;
+  less = wave_scan(less);
+  if (lane == 63) less_of[wave] = less;
   __syncthreads();
+  for (int32_t k = lane; k < kept; k += 64) atomicAdd(&table[wave * R + list[k].y], 1);
+  for (int32_t g = again; g < last; ++g) {
+    const int32_t k = (g << 6) + lane;
+    const uint32_t key = k < end ? keys.key(k) : 0xFFFFFFFFu;
+    if (key < bk.n && (key & mask) == w) atomicAdd(&table[wave * R + (key >> bk.log)], 1);
+  }
+  __syncthreads();
+  int32_t count[kSortWaves];   // of key threadIdx.x, wave by wave
   if (threadIdx.x < R) {
     int32_t t = 0;
-    for (int v = 0; v < kSortWaves; ++v) t += table[v * R + threadIdx.x];
+#pragma unroll
+    for (int v = 0; v < kSortWaves; ++v) t += count[v] = table[v * R + threadIdx.x];
     total[threadIdx.x] = t;
   }
   __syncthreads();
-  if (threadIdx.x < 64) {   // exclusive prefix of total[], 64 keys at a time
-    int32_t run = lane < kSortWaves ? less_of[lane] : 0;
-#pragma unroll
-    for (int off = kSortWaves / 2; off >= 1; off >>= 1) run += __shfl_xor(run, off, 64);
-    run = __shfl(run, 0, 64);
+  if (wave == 0) {   // exclusive prefix of total[], 64 keys at a time
+    int32_t run = __builtin_amdgcn_readlane(wave_scan(lane < kSortWaves ? less_of[lane] : 0), 63);
     for (uint32_t base = 0; base < R; base += 64) {
       const int32_t t = base + lane < R ? total[base + lane] : 0;
-      int32_t s = t;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int32_t u = __shfl_up(s, off, 64);
-        if (lane >= off) s += u;
-      }
+      const int32_t s = wave_scan(t);
       if (base + lane < R) total[base + lane] = run + s - t;
-      run += __shfl(s, 63, 64);
+      run += __builtin_amdgcn_readlane(s, 63);
     }
     if (lane == 0 && w == mask) offsets[bk.R << bk.log] = run;
   }
@@ -192,24 +188,39 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk
   if (threadIdx.x < R) {
     int32_t at = total[threadIdx.x];
     offsets[w * R + threadIdx.x] = at;
+#pragma unroll
     for (int v = 0; v < kSortWaves; ++v) {
-      const int32_t t = table[v * R + threadIdx.x];
       table[v * R + threadIdx.x] = at;
-      at += t;
+      at += count[v];
     }
   }
   __syncthreads();
-  volatile int32_t* place = table + wave * R;   // written by one lane, read by the others of its wave
+  // Places: lanes with the same key find each other bit by bit; the first of
+  // them moves the wave's place of that key on.
+  volatile int32_t* place = table + wave * R;
+  const auto put = [&](bool here, uint32_t m, int32_t value) {
+    uint64_t same = __ballot(here);
+    for (uint32_t bit = 1; bit < R; bit <<= 1) {
+      const bool set = (m & bit) != 0;
+      const uint64_t ones = __ballot(set);
+      same &= set ? ones : ~ones;
+    }
+    if (here) {
+      const int32_t at = place[m];
+      order[at + __popcll(same & below)] = value;
+      if ((same & below) == 0) place[m] = at + __popcll(same);
+    }
+  };
   for (int32_t base = 0; base < kept; base += 64) {
     const bool here = base + lane < kept;
-    const int at = here ? base + lane : 0;
-    place_group(__ballot(here), kept_key[wave][at], kept_value[wave][at], place, order);
+    const uint2 e = list[here ? base + lane : 0];
+    put(here, e.y, (int32_t)e.x);
   }
   for (int32_t g = again; g < last; ++g) {
     const int32_t k = (g << 6) + lane;
-    const uint32_t key = k < N ? keys.key(k) : 0xFFFFFFFFu;
+    const uint32_t key = k < end ? keys.key(k) : 0xFFFFFFFFu;
     const bool match = key < bk.n && (key & mask) == w;
-    place_group(__ballot(match), key >> bk.log, match ? keys.value(k) : 0, place, order);
+    put(match, match ? key >> bk.log : 0, match ? keys.value(k) : 0);
   }
 }
 
@@ -340,7 +351,7 @@ struct SortLds {
 // digit find each other with eight ballots; the first of them adds their number
 // to the wave's counter, so a pass is stable and needs no atomics.
 __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first, const SortLds& l) {
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const uint64_t below = (UINT64_C(1) << lane) - 1;
   int32_t n = a.T;
   for (int digit = 0; digit < a.digits; ++digit) {
@@ -383,16 +394,11 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
       }
     }
     __syncthreads();
-    uint32_t total = 0, scan = 0;
+    uint32_t count[kNormWaves], total = 0, scan = 0;   // of digit threadIdx.x, wave by wave
     if (threadIdx.x < 256) {
 #pragma unroll
-      for (int w = 0; w < kNormWaves; ++w) total += l.count[w * 256 + threadIdx.x];
-      scan = total;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const uint32_t o = __shfl_up(scan, off, 64);
-        if (lane >= off) scan += o;
-      }
+      for (int w = 0; w < kNormWaves; ++w) total += count[w] = l.count[w * 256 + threadIdx.x];
+      scan = (uint32_t)wave_scan((int32_t)total);
       if (lane == 63) l.sums[wave] = scan;
     }
     __syncthreads();
@@ -401,9 +407,8 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
       for (int w = 0; w < wave; ++w) place += l.sums[w];
 #pragma unroll
       for (int w = 0; w < kNormWaves; ++w) {
-        const uint32_t c = l.count[w * 256 + threadIdx.x];
         l.count[w * 256 + threadIdx.x] = place;
-        place += c;
+        place += count[w];
       }
     }
     n = (int32_t)(l.sums[0] + l.sums[1] + l.sums[2] + l.sums[3]);
@@ -492,15 +497,24 @@ __device__ __forceinline__ float group_squares(const NormArgs& a, const List& li
     store_vec<V>(first ? head : tail, acc);
   }
   __syncthreads();
-  if (mine && part == 0) {
+  if (threadIdx.x / 64 * 64 >= a.units) return ss;   // waves without a thread of part 0
+  // Bit q: part q has entries; its first group began in the part before; all of
+  // its entries are of one group.
+  const int q = threadIdx.x & 63;
+  const int32_t qs = cut(q < a.parts ? q : 0), qe = cut(q < a.parts ? q + 1 : 1);
+  const bool any = q < a.parts && qs < qe;
+  const uint64_t there = __ballot(any);
+  const uint64_t goes_on = __ballot(any && qs > S && list.group(qs) == list.group(qs - 1));
+  const uint64_t single = __ballot(any && list.group(qs) == list.group(qe - 1));
+  if (mine && part == 0 && there) {
     float acc[V] = {};
-    for (int q = 0; q < a.parts; ++q) {
-      const int32_t s = cut(q), e = cut(q + 1);
-      if (s >= e) break;
-      float x[V], y[V];
-      load_vec<V>(edges + (q * a.units + u) * V, x);
-      load_vec<V>(edges + ((a.parts + q) * a.units + u) * V, y);
-      if (s > S && list.group(s) != list.group(s - 1)) {
+    const int n_parts = 64 - __clzll((long long)there);   // parts with entries come first
+#pragma unroll 4
+    for (int p = 0; p < n_parts; ++p) {
+      float x[V], y[V];   // y is not written where the part is of one group
+      load_vec<V>(edges + (p * a.units + u) * V, x);
+      load_vec<V>(edges + ((a.parts + p) * a.units + u) * V, y);
+      if (!(goes_on >> p & 1)) {
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           ss = fmaf(acc[c], acc[c], ss);
@@ -509,7 +523,7 @@ __device__ __forceinline__ float group_squares(const NormArgs& a, const List& li
       }
 #pragma unroll
       for (int c = 0; c < V; ++c) acc[c] += x[c];
-      if (list.group(s) != list.group(e - 1)) {   // otherwise y was not written
+      if (!(single >> p & 1)) {
 #pragma unroll
         for (int c = 0; c < V; ++c) {
           ss = fmaf(acc[c], acc[c], ss);
