@@ -35,6 +35,13 @@ __device__ __forceinline__ int32_t wave_scan(int32_t x) {
   return x;
 }
 
+// What one lane has written to LDS, the others of its wave read after this (a
+// wave's LDS accesses are done in order: this holds the compiler to it).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // ------------------------------------------------------------------- sorting
 
 constexpr int kSortThreads = 1024;
@@ -197,7 +204,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk
   __syncthreads();
   // Places: lanes with the same key find each other bit by bit; the first of
   // them moves the wave's place of that key on.
-  volatile int32_t* place = table + wave * R;
+  int32_t* place = table + wave * R;
   const auto put = [&](bool here, uint32_t m, int32_t value) {
     uint64_t same = __ballot(here);
     for (uint32_t bit = 1; bit < R; bit <<= 1) {
@@ -210,6 +217,7 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk
       order[at + __popcll(same & below)] = value;
       if ((same & below) == 0) place[m] = at + __popcll(same);
     }
+    wave_fence();
   };
   for (int32_t base = 0; base < kept; base += 64) {
     const bool here = base + lane < kept;
@@ -339,10 +347,11 @@ struct GlobalList {
 // LDS of the sort: two buffers of tokens and of their places t, and the counters
 // of the digits.
 struct SortLds {
-  uint32_t* id[2];
-  uint16_t* t[2];
+  uint32_t* id;      // [2][padded]
+  uint16_t* t;       // [2][padded]
   uint32_t* count;   // [kNormWaves][256]
   uint32_t* sums;    // [4]
+  int padded;
 };
 
 // Sorts the tokens of one example by (token, t), digit by digit, and returns how
@@ -355,12 +364,12 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
   const uint64_t below = (UINT64_C(1) << lane) - 1;
   int32_t n = a.T;
   for (int digit = 0; digit < a.digits; ++digit) {
-    const int from = digit & 1;
+    const int from = digit & 1 ? l.padded : 0, to = l.padded - from;
     for (int k = threadIdx.x; k < kNormWaves * 256; k += kNormThreads) l.count[k] = 0;
     __syncthreads();
     const int32_t groups = (n + 63) >> 6, per = (groups + kNormWaves - 1) / kNormWaves;
     uint32_t id[kLdsGroups], at[kLdsGroups], t[kLdsGroups];   // at: digit | rank << 8, ~0: none
-    volatile uint32_t* mine = l.count + wave * 256;
+    uint32_t* mine = l.count + wave * 256;
 #pragma unroll
     for (int u = 0; u < kLdsGroups; ++u) {
       at[u] = ~0u;
@@ -375,8 +384,8 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
           id[u] = (uint32_t)v;
           t[u] = (uint32_t)k;
         } else {
-          id[u] = l.id[from][k];
-          t[u] = l.t[from][k];
+          id[u] = l.id[from + k];
+          t[u] = l.t[from + k];
         }
       }
       const uint32_t d = (id[u] >> (8 * digit)) & 255u;
@@ -392,6 +401,7 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
         at[u] = d | (before + (uint32_t)__popcll(same & below)) << 8;
         if ((same & below) == 0) mine[d] = before + (uint32_t)__popcll(same);
       }
+      wave_fence();
     }
     __syncthreads();
     uint32_t count[kNormWaves], total = 0, scan = 0;   // of digit threadIdx.x, wave by wave
@@ -416,9 +426,9 @@ __device__ __forceinline__ int32_t sort_example(const NormArgs& a, int64_t first
 #pragma unroll
     for (int u = 0; u < kLdsGroups; ++u) {
       if (at[u] == ~0u) continue;
-      const uint32_t to = l.count[wave * 256 + (at[u] & 255u)] + (at[u] >> 8);
-      l.id[from ^ 1][to] = id[u];
-      l.t[from ^ 1][to] = (uint16_t)t[u];
+      const uint32_t place = l.count[wave * 256 + (at[u] & 255u)] + (at[u] >> 8);
+      l.id[to + place] = id[u];
+      l.t[to + place] = (uint16_t)t[u];
     }
     __syncthreads();
   }
@@ -553,17 +563,15 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
   const T* G = static_cast<const T*>(a.G) + (int64_t)i * a.T * a.d;
   float ss;
   if constexpr (IN_LDS) {
-    const int padded = (a.T + 7) & ~7;
     SortLds l;
+    l.padded = (a.T + 7) & ~7;
     l.count = reinterpret_cast<uint32_t*>(norm_lds);
     l.sums = l.count + kNormWaves * 256;
-    l.id[0] = l.sums + 4;
-    l.id[1] = l.id[0] + padded;
-    l.t[0] = reinterpret_cast<uint16_t*>(l.id[1] + padded);
-    l.t[1] = l.t[0] + padded;
+    l.id = l.sums + 4;
+    l.t = reinterpret_cast<uint16_t*>(l.id + 2 * l.padded);
     const int32_t n = sort_example(a, (int64_t)i * a.T, l);
-    const int at = a.digits & 1;
-    ss = group_squares<T, V>(a, LdsList{l.id[at], l.t[at]}, n, wg, blk, G,
+    const int at = a.digits & 1 ? l.padded : 0;
+    ss = group_squares<T, V>(a, LdsList{l.id + at, l.t + at}, n, wg, blk, G,
                              reinterpret_cast<float*>(norm_lds + sort_lds_bytes(a.T)));
   } else {
     const uint32_t slot = a.examples.slot(i);
