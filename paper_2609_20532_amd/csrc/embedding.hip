@@ -473,21 +473,25 @@ __device__ __forceinline__ float group_squares(const NormArgs& a, const List& li
     float* tail = head + a.parts * a.units * V;
     bool first = true;
     uint32_t last = s < e ? list.group(s) : 0;
-    for (int32_t k0 = s; k0 < e; k0 += kRowBatch) {
-      Raw<T, V> raw[kRowBatch];
-      uint32_t g[kRowBatch];
+    // Two batches in turn: one is loaded while the other is added.
+    constexpr int kHalf = kRowBatch / 2;
+    Raw<T, V> raw[2][kHalf];
+    uint32_t g[2][kHalf];
+    const auto load = [&](int b, int32_t k0) {
 #pragma unroll
-      for (int k = 0; k < kRowBatch; ++k) {
+      for (int k = 0; k < kHalf; ++k) {
         const int32_t at = k0 + k < e ? k0 + k : e - 1;
-        g[k] = list.group(at);
-        raw[k].load(G + (int64_t)list.row(at) * a.d + col);
+        g[b][k] = list.group(at);
+        raw[b][k].load(G + (int64_t)list.row(at) * a.d + col);
       }
+    };
+    const auto add = [&](int b, int32_t k0) {
 #pragma unroll
-      for (int k = 0; k < kRowBatch; ++k) {
+      for (int k = 0; k < kHalf; ++k) {
         if (k0 + k >= e) break;
         float x[V];
-        raw[k].widen(x);
-        if (g[k] != last) {
+        raw[b][k].widen(x);
+        if (g[b][k] != last) {
           if (first) {
             store_vec<V>(head, acc);
             first = false;
@@ -497,12 +501,19 @@ __device__ __forceinline__ float group_squares(const NormArgs& a, const List& li
           }
 #pragma unroll
           for (int c = 0; c < V; ++c) acc[c] = x[c];
-          last = g[k];
+          last = g[b][k];
         } else {
 #pragma unroll
           for (int c = 0; c < V; ++c) acc[c] += x[c];
         }
       }
+    };
+    if (s < e) load(0, s);
+    for (int32_t k0 = s; k0 < e; k0 += kRowBatch) {
+      if (k0 + kHalf < e) load(1, k0 + kHalf);
+      add(0, k0);
+      if (k0 + kRowBatch < e) load(0, k0 + kRowBatch);
+      add(1, k0 + kHalf);
     }
     store_vec<V>(first ? head : tail, acc);
   }
