@@ -386,7 +386,7 @@ typedef enum dpsgd_activation {
 typedef struct dpsgd_group_norm {
   int64_t B;            /* examples, >= 1                                    */
   int64_t S;            /* positions, >= 1; B S < 2^31                       */
-  int64_t C;            /* channels, >= 1, a multiple of groups              */
+  int64_t C;            /* channels, 1 .. 2^20, a multiple of groups         */
   int64_t groups;       /* >= 1                                              */
   const float* gamma;   /* [C], device; may be NULL                          */
   const float* beta;    /* [C], device; may be NULL                          */

@@ -38,7 +38,7 @@ int check_group_norm(const dpsgd_group_norm* n) {
   if (!valid_dtype(n->dtype)) return DPSGD_ERR_UNSUPPORTED;
   if (n->act < DPSGD_ACT_NONE || n->act > DPSGD_ACT_GELU) return DPSGD_ERR_UNSUPPORTED;
   if (n->B < 1 || n->S < 1 || n->C < 1 || n->groups < 1) return DPSGD_ERR_INVALID_ARG;
-  if (n->B > kI32Max || n->S > kI32Max / n->B || n->C > kI32Max) return DPSGD_ERR_INVALID_ARG;
+  if (n->B > kI32Max || n->S > kI32Max / n->B || n->C > (INT64_C(1) << 20)) return DPSGD_ERR_INVALID_ARG;
   if (n->C > kMostEntries / (n->B * n->S)) return DPSGD_ERR_INVALID_ARG;
   if (n->groups > n->C || n->C % n->groups != 0) return DPSGD_ERR_INVALID_ARG;
   if (!isfinite(n->eps) || !(n->eps > 0.0f)) return DPSGD_ERR_INVALID_ARG;

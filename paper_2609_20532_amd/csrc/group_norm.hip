@@ -6,12 +6,17 @@
 //   dx = rstd (gamma dz - m1 - xh m2),  m1 = mean(gamma dz), m2 = mean(gamma dz xh)
 //
 // with mu, rstd, m1 and m2 per example and group of C / groups neighbouring
-// channels. Both directions sum over the positions channel by channel (a
-// thread keeps a fixed set of channels, so that any group width works), which
-// for the gradient are dgamma_i and dbeta_i themselves, and then over the
-// channels of a group. The statistics are means and sums of squared deviations
-// (no difference of large sums): each thread takes eight rows at a time, in two
-// passes over registers, and results are merged by their counts.
+// channels. Bound by memory traffic. A workgroup takes a tile, some rows and a
+// block of channels of one example, into registers; a thread keeps a fixed set of
+// channels, so that any group width works. Where all rows of whole groups fit one
+// tile, x (and dy) are read once, and the result is written from the registers
+// in the same launch. Otherwise a first pass leaves the tiles' statistics, a
+// second one joins them, and a third reads x (and dy) again, from the last-level
+// cache where it holds them.
+//
+// Statistics are taken in two passes over the registers, the mean and then the
+// deviations from it, and tiles are merged by their counts: no difference of
+// large sums is formed.
 #include <math.h>
 
 #include "vec.h"
@@ -19,35 +24,60 @@
 namespace dpsgd {
 namespace {
 
+constexpr int kTile = 1024;    // most threads of a tile's workgroup
+constexpr int kGradRows = 8;   // rows of a thread in a backward tile
+
+// Rows of a thread in a forward tile: 32 registers of 4 elements each.
+template <class T>
+constexpr int kTileRows = 32 / (int)sizeof(T);
+
+// 1 / (1 + exp(-z)) to a few units in the last place, by the hardware's
+// exponential and reciprocal.
+__device__ __forceinline__ float sigmoid(float z) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
+}
+
 constexpr float kGelu0 = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGelu1 = 0.044715f;
 
-template <int ACT>
-__device__ __forceinline__ float act_of(float z) {
-  if constexpr (ACT == DPSGD_ACT_RELU) return z < 0.0f ? 0.0f : z;   // a NaN stays
-  if constexpr (ACT == DPSGD_ACT_SILU) return z / (1.0f + expf(-z));
-  if constexpr (ACT == DPSGD_ACT_GELU) {
-    const float u = kGelu0 * fmaf(kGelu1 * z * z, z, z);
-    return z / (1.0f + expf(-2.0f * u));   // 0.5 z (1 + tanh u)
+// x = act(x), or slope = act'(x), for V values. 0.5 (1 + tanh u) = sigmoid(2 u).
+template <int V>
+__device__ __forceinline__ void activate(int act, float (&x)[V]) {
+  if (act == DPSGD_ACT_RELU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) x[c] = x[c] < 0.0f ? 0.0f : x[c];   // a NaN stays
+  } else if (act == DPSGD_ACT_SILU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) x[c] *= sigmoid(x[c]);
+  } else if (act == DPSGD_ACT_GELU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c)
+      x[c] *= sigmoid(2.0f * kGelu0 * fmaf(kGelu1 * x[c] * x[c], x[c], x[c]));
   }
-  return z;
 }
 
-// act'(z).
-template <int ACT>
-__device__ __forceinline__ float slope_of(float z) {
-  if constexpr (ACT == DPSGD_ACT_RELU) return z > 0.0f ? 1.0f : (z == z ? 0.0f : z);
-  if constexpr (ACT == DPSGD_ACT_SILU) {
-    const float p = 1.0f / (1.0f + expf(-z));
-    return p * fmaf(z, 1.0f - p, 1.0f);
+template <int V>
+__device__ __forceinline__ void slopes(int act, const float (&z)[V], float (&slope)[V]) {
+  if (act == DPSGD_ACT_RELU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) slope[c] = z[c] > 0.0f ? 1.0f : (z[c] == z[c] ? 0.0f : z[c]);
+  } else if (act == DPSGD_ACT_SILU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const float p = sigmoid(z[c]);
+      slope[c] = p * fmaf(z[c], 1.0f - p, 1.0f);
+    }
+  } else if (act == DPSGD_ACT_GELU) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const float p = sigmoid(2.0f * kGelu0 * fmaf(kGelu1 * z[c] * z[c], z[c], z[c]));
+      const float du = kGelu0 * fmaf(3.0f * kGelu1 * z[c], z[c], 1.0f);
+      slope[c] = fmaf(2.0f * z[c] * p * (1.0f - p), du, p);
+    }
+  } else {
+#pragma unroll
+    for (int c = 0; c < V; ++c) slope[c] = 1.0f;
   }
-  if constexpr (ACT == DPSGD_ACT_GELU) {
-    const float u = kGelu0 * fmaf(kGelu1 * z * z, z, z);
-    const float p = 1.0f / (1.0f + expf(-2.0f * u));
-    const float du = kGelu0 * fmaf(3.0f * kGelu1 * z, z, 1.0f);
-    return p + 2.0f * z * p * (1.0f - p) * du;
-  }
-  return 1.0f;
 }
 
 struct GnArgs {
@@ -60,38 +90,15 @@ struct GnArgs {
   float* rstd;
   float* dgamma;         // [B][C]
   float* dbeta;
-  float* partials;       // [B][chunks][C][3]: a channel's Stat (backward: [2], its sums)
+  float* partials;       // forward: [B][chunks][blocks][segs][3]; backward: [B][chunks][C][2]
   float2* sums;          // [B][groups] m1, m2
-  int64_t S;
-  int64_t rows;          // rows of a chunk
+  int32_t S, rows;       // rows of an example, of a tile
   int32_t B, C, groups, width;
-  int32_t chunks, blocks;   // chunks of an example's rows, blocks of its channels
-  int32_t units;         // channel vectors of a block
+  int32_t chunks, blocks;   // tiles of an example: row chunks, channel blocks
+  int32_t units, segs;   // channel vectors of a block; most groups that a block has a part of
+  int32_t act;
   float eps;
 };
-
-// Where a workgroup of the passes over the rows is.
-struct Place {
-  int64_t b, r0, r1;
-  int32_t chunk, c, r, step;   // first channel, first row and row step of the thread
-  bool active;
-};
-
-template <int V>
-__device__ __forceinline__ Place place_of(const GnArgs& a) {
-  Place p;
-  const int64_t w = blockIdx.x;
-  const int32_t blk = (int32_t)(w % a.blocks);
-  p.chunk = (int32_t)(w / a.blocks % a.chunks);
-  p.b = w / a.blocks / a.chunks;
-  p.step = kThreads / a.units;
-  p.r = threadIdx.x / a.units;
-  p.c = (blk * a.units + threadIdx.x % a.units) * V;
-  p.active = p.r < p.step && p.c < a.C;
-  p.r0 = p.chunk * a.rows;
-  p.r1 = p.r0 + a.rows < a.S ? p.r0 + a.rows : a.S;
-  return p;
-}
 
 // n values: their mean as an unevaluated sum hi + lo (lo at most a rounding of
 // hi), and the sum of squared deviations from it. The second word keeps the
@@ -100,6 +107,13 @@ __device__ __forceinline__ Place place_of(const GnArgs& a) {
 struct Stat {
   float n, hi, lo, m2;
 };
+
+// Sum of squares about the mean of n values from that about a point which is
+// `lo` below it; at least 0 (and NaN stays NaN).
+__device__ __forceinline__ float about_mean(float m2, float n, float lo) {
+  const float m = fmaf(-n * lo, lo, m2);
+  return m < 0.0f ? 0.0f : m;
+}
 
 __device__ __forceinline__ void merge(Stat& a, const Stat& b) {
   const float t = a.n + b.n;
@@ -113,221 +127,440 @@ __device__ __forceinline__ void merge(Stat& a, const Stat& b) {
   a.n = t;
 }
 
-template <class T, int V>
-__global__ __launch_bounds__(kThreads) void gn_stats_kernel(GnArgs a) {
-  __shared__ float lds[kThreads][3 * V + 1];
-  const Place p = place_of<V>(a);
-  const T* x = static_cast<const T*>(a.x) + p.b * a.S * a.C + p.c;
-  Stat st[V] = {};
-  if (p.active) {
-    for (int64_t r = p.r0 + p.r; r < p.r1; r += 8 * p.step) {
-      float v[8][V];
-      int m = 0;
+// Where a thread is: tile (example b, chunk, block), rows r0 + r + k step < r1,
+// channels c .. c + V - 1 (in the block: unit V ...). first: first group of the
+// block, of which it has a part.
+struct Place {
+  int32_t b, chunk, blk, r, r0, r1, step, unit, c, c0, c1, first, here;
+  bool active;
+};
+
+template <int V>
+__device__ __forceinline__ Place place_of(const GnArgs& a) {
+  Place p;
+  const uint32_t w = blockIdx.x, per = (uint32_t)a.blocks * (uint32_t)a.chunks;
+  p.b = (int32_t)(w / per);
+  const uint32_t rest = w - (uint32_t)p.b * per;
+  p.chunk = (int32_t)(rest / (uint32_t)a.blocks);
+  p.blk = (int32_t)(rest - (uint32_t)p.chunk * (uint32_t)a.blocks);
+  p.step = (int32_t)blockDim.x / a.units;
+  p.r = (int32_t)threadIdx.x / a.units;
+  p.unit = (int32_t)threadIdx.x - p.r * a.units;
+  p.c0 = p.blk * a.units * V;
+  p.c1 = p.c0 + a.units * V < a.C ? p.c0 + a.units * V : a.C;
+  p.c = p.c0 + p.unit * V;
+  p.active = p.r < p.step && p.c < a.C;
+  p.r0 = p.chunk * a.rows;
+  p.r1 = a.S - p.r0 < a.rows ? a.S : p.r0 + a.rows;
+  p.first = p.c0 / a.width;
+  p.here = (p.c1 - 1) / a.width - p.first + 1;
+  return p;
+}
+
+// LDS of a tile's sums: one partial sum a thread and channel (each channel of
+// the vector padded by `units`, which keeps the reads below apart), then one a
+// helper and channel in the channels' own order.
+template <int V>
+__host__ __device__ constexpr int sums_floats(int threads, int units) {
+  return V * (threads + units) + (threads > units * V ? threads : units * V);
+}
+
+__device__ __forceinline__ int helpers_of(int channels) {
+  const int h = (int)blockDim.x / channels;
+  return h < 1 ? 1 : h;
+}
+
+// Sums each channel of the block over the threads that hold rows of it, to `h`
+// values [h][channels] in LDS; h is helpers_of(channels). Ends with a barrier.
+template <int V>
+__device__ __forceinline__ const float* sum_rows(const float (&v)[V], const Place& p, int units,
+                                                 float* lds) {
+  const int stride = (int)blockDim.x + units, channels = units * V, h = helpers_of(channels);
+  float* out = lds + V * stride;
+  if (p.r < p.step) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const int64_t at = r + k * p.step;
-        if (at < p.r1) {
-          load_vec<V>(x + at * a.C, v[k]);
-          m = k + 1;
-        } else {
-#pragma unroll
-          for (int c = 0; c < V; ++c) v[k][c] = 0.0f;
-        }
-      }
-      const float n = (float)m;
-#pragma unroll
-      for (int c = 0; c < V; ++c) {
-        float s = 0.0f, e = 0.0f, q = 0.0f;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) s += v[k][c];
-        s /= n;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float d = k < m ? v[k][c] - s : 0.0f;
-          e += d;
-          q = fmaf(d, d, q);
-        }
-        e /= n;
-        merge(st[c], Stat{n, s, e, fmaf(-n * e, e, q)});
-      }
-    }
+    for (int c = 0; c < V; ++c) lds[c * stride + threadIdx.x] = v[c];
   }
-  float* mine = lds[threadIdx.x];
+  __syncthreads();
+  for (int t = threadIdx.x; t < h * channels; t += blockDim.x) {
+    const int j = t / channels, k = t - j * channels, c = k / units, unit = k - c * units;
+    float s = 0.0f;
+#pragma unroll 4
+    for (int r = j; r < p.step; r += h) s += lds[c * stride + r * units + unit];
+    out[j * channels + unit * V + c] = s;
+  }
+  __syncthreads();
+  return out;
+}
+
+// The sum over the block's part of each group, to seg[] in LDS, one wave a
+// group. Ends with a barrier.
+__device__ __forceinline__ void sum_groups(const float* from, int channels, int h, const Place& p,
+                                           int width, float* seg) {
+  const int lane = threadIdx.x & 63;
+  for (int j = threadIdx.x >> 6; j < p.here; j += blockDim.x >> 6) {
+    const int g0 = (p.first + j) * width;
+    const int a = (g0 > p.c0 ? g0 : p.c0) - p.c0, b = (g0 + width < p.c1 ? g0 + width : p.c1) - p.c0;
+    float s = 0.0f;
+    for (int i = 0; i < h; ++i)
+      for (int k = a + lane; k < b; k += 64) s += from[i * channels + k];
+    s = wave_sum(s);
+    if (lane == 0) seg[j] = s;
+  }
+  __syncthreads();
+}
+
+// Statistics of a tile; with WHOLE (all rows, whole groups) the output too.
+template <class T, int V, bool WHOLE>
+__global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
+  extern __shared__ __align__(16) float gn_lds[];
+  const Place p = place_of<V>(a);
+  const int channels = a.units * V, h = helpers_of(channels);
+  float* seg_mean = gn_lds;                // [segs]
+  float* seg_lo = seg_mean + a.segs;       // [segs]
+  float* seg_m2 = seg_lo + a.segs;         // [segs]
+  float* lds = seg_m2 + a.segs;
+  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  const T* x = static_cast<const T*>(a.x) + at;
+  const int32_t n_rows = p.r1 - p.r0;
+
+  Raw<T, V> raw[kTileRows<T>];
+  float v[V] = {};
+#pragma unroll
+  for (int k = 0; k < kTileRows<T>; ++k) {
+    raw[k].zero();
+    const int32_t r = p.r + k * p.step;
+    if (p.active && r < n_rows) raw[k].load(x + (int64_t)r * a.C);
+  }
+#pragma unroll
+  for (int k = 0; k < kTileRows<T>; ++k) {
+    float f[V];
+    raw[k].widen(f);
+#pragma unroll
+    for (int c = 0; c < V; ++c) v[c] += f[c];
+  }
+  sum_groups(sum_rows<V>(v, p, a.units, lds), channels, h, p, a.width, seg_mean);
+
+  // The mean of the tile's part of a group, and the deviations from it.
+  float mu[V];
+  int32_t j[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    mine[3 * c] = st[c].hi;
-    mine[3 * c + 1] = st[c].lo;
-    mine[3 * c + 2] = st[c].m2;
+    const int32_t ch = p.c + c < a.C ? p.c + c : a.C - 1;
+    j[c] = ch / a.width - p.first;
+    const int32_t g0 = (p.first + j[c]) * a.width;
+    const int32_t n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
+    mu[c] = p.active ? seg_mean[j[c]] / ((float)n_rows * (float)n) : 0.0f;
   }
-  mine[3 * V] = st[0].n;
-  int half = 1;
-  while (half < p.step) half <<= 1;
-  for (half >>= 1; half >= 1; half >>= 1) {
-    __syncthreads();
-    if (p.active && p.r < half && p.r + half < p.step) {
-      const float* other = lds[threadIdx.x + half * a.units];
+  float q[V];
+#pragma unroll
+  for (int c = 0; c < V; ++c) v[c] = q[c] = 0.0f;
+#pragma unroll
+  for (int k = 0; k < kTileRows<T>; ++k) {
+    if (p.r + k * p.step < n_rows) {
+      float f[V];
+      raw[k].widen(f);
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        merge(st[c], Stat{other[3 * V], other[3 * c], other[3 * c + 1], other[3 * c + 2]});
-        mine[3 * c] = st[c].hi;
-        mine[3 * c + 1] = st[c].lo;
-        mine[3 * c + 2] = st[c].m2;
+        const float d = f[c] - mu[c];
+        v[c] += d;
+        q[c] = fmaf(d, d, q[c]);
       }
-      mine[3 * V] = st[0].n;
     }
   }
-  if (p.active && p.r == 0) {
-    float* out = a.partials + ((p.b * a.chunks + p.chunk) * a.C + p.c) * 3;
+  if (!p.active) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) v[c] = q[c] = 0.0f;
+  }
+  sum_groups(sum_rows<V>(v, p, a.units, lds), channels, h, p, a.width, seg_lo);
+  sum_groups(sum_rows<V>(q, p, a.units, lds), channels, h, p, a.width, seg_m2);
+
+  if constexpr (!WHOLE) {
+    for (int s = threadIdx.x; s < p.here; s += blockDim.x) {
+      const int32_t g0 = (p.first + s) * a.width;
+      const int32_t n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
+      const float count = (float)n_rows * (float)n, lo = seg_lo[s] / count;
+      float* to = a.partials + (((int64_t)blockIdx.x) * a.segs + s) * 3;
+      to[0] = seg_mean[s] / count;
+      to[1] = lo;
+      to[2] = about_mean(seg_m2[s], count, lo);
+    }
+  } else {
+    const float count = (float)a.S * (float)a.width;
+    for (int s = threadIdx.x; s < p.here; s += blockDim.x) {
+      const float lo = seg_lo[s] / count;
+      const int64_t g = (int64_t)p.b * a.groups + p.first + s;
+      a.mean[g] = seg_mean[s] / count + lo;
+      a.rstd[g] = 1.0f / sqrtf(about_mean(seg_m2[s], count, lo) / count + a.eps);
+    }
+    if (!p.active) return;
+    float rs[V], ga[V], be[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      out[3 * c] = st[c].hi;
-      out[3 * c + 1] = st[c].lo;
-      out[3 * c + 2] = st[c].m2;
+      const float lo = seg_lo[j[c]] / count;
+      rs[c] = 1.0f / sqrtf(about_mean(seg_m2[j[c]], count, lo) / count + a.eps);
+      mu[c] += lo;
+      ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
+      be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
+    }
+    T* y = static_cast<T*>(a.out) + at;
+#pragma unroll
+    for (int k = 0; k < kTileRows<T>; ++k) {
+      const int32_t r = p.r + k * p.step;
+      if (r < n_rows) {
+        float f[V];
+        raw[k].widen(f);
+#pragma unroll
+        for (int c = 0; c < V; ++c) f[c] = fmaf((f[c] - mu[c]) * rs[c], ga[c], be[c]);
+        activate<V>(a.act, f);
+        store_vec<V>(y + (int64_t)r * a.C, f);
+      }
     }
   }
 }
 
-// One wave per example and group: its chunks' and channels' statistics merged.
+// One workgroup per example and group: the tiles' statistics merged, each
+// thread a range of them, then pairwise.
 __global__ __launch_bounds__(kThreads) void gn_finish_kernel(GnArgs a) {
-  const int64_t job = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (job >= (int64_t)a.B * a.groups) return;
-  const int64_t b = job / a.groups, g = job - b * a.groups;
+  __shared__ float lds[kThreads][4];
+  const uint32_t b = blockIdx.x / (uint32_t)a.groups;
+  const int32_t g = (int32_t)(blockIdx.x - b * (uint32_t)a.groups);
+  // Blocks that have a part of the group (channels of a block: `per`).
+  const int32_t per = a.units, g0 = g * a.width, g1 = g0 + a.width;
+  const int32_t k0 = g0 / per, n_blocks = (g1 - 1) / per - k0 + 1;
   Stat st{};
-  const int64_t items = (int64_t)a.chunks * a.width;
-  for (int64_t k = lane; k < items; k += 64) {
-    const int64_t chunk = k / a.width;
-    const float* s = a.partials + ((b * a.chunks + chunk) * a.C + g * a.width + (k - chunk * a.width)) * 3;
-    const int64_t left = a.S - chunk * a.rows;
-    merge(st, Stat{(float)(left < a.rows ? left : a.rows), s[0], s[1], s[2]});
+  for (int32_t k = threadIdx.x; k < a.chunks * n_blocks; k += kThreads) {
+    const int32_t chunk = k / n_blocks, blk = k0 + k - chunk * n_blocks;
+    const int32_t c0 = blk * per, c1 = c0 + per < a.C ? c0 + per : a.C;
+    const float* s = a.partials + ((((int64_t)b * a.chunks + chunk) * a.blocks + blk) * a.segs +
+                                   (g - c0 / a.width)) * 3;
+    const int32_t rows = a.S - chunk * a.rows < a.rows ? a.S - chunk * a.rows : a.rows;
+    const int32_t n = (g1 < c1 ? g1 : c1) - (g0 > c0 ? g0 : c0);
+    merge(st, Stat{(float)rows * (float)n, s[0], s[1], s[2]});
   }
-  for (int off = 32; off >= 1; off >>= 1) {
-    const Stat other{__shfl_down(st.n, off, 64), __shfl_down(st.hi, off, 64),
-                     __shfl_down(st.lo, off, 64), __shfl_down(st.m2, off, 64)};
-    if (lane < off) merge(st, other);
+  float* mine = lds[threadIdx.x];
+  for (int half = kThreads / 2; half >= 1; half >>= 1) {
+    mine[0] = st.n;
+    mine[1] = st.hi;
+    mine[2] = st.lo;
+    mine[3] = st.m2;
+    __syncthreads();
+    if ((int)threadIdx.x < half) {
+      const float* o = lds[threadIdx.x + half];
+      merge(st, Stat{o[0], o[1], o[2], o[3]});
+    }
+    __syncthreads();
   }
-  if (lane == 0) {
-    a.mean[job] = st.hi;
-    a.rstd[job] = 1.0f / sqrtf(st.m2 / ((float)a.S * (float)a.width) + a.eps);
+  if (threadIdx.x == 0) {
+    a.mean[blockIdx.x] = st.hi;
+    a.rstd[blockIdx.x] = 1.0f / sqrtf(st.m2 / ((float)a.S * (float)a.width) + a.eps);
   }
 }
 
-template <class T, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_apply_kernel(GnArgs a) {
+template <class T, int V>
+__global__ __launch_bounds__(kTile) void gn_apply_kernel(GnArgs a) {
   const Place p = place_of<V>(a);
   if (!p.active) return;
-  const T* x = static_cast<const T*>(a.x) + p.b * a.S * a.C + p.c;
-  T* y = static_cast<T*>(a.out) + p.b * a.S * a.C + p.c;
+  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  const T* x = static_cast<const T*>(a.x) + at;
+  T* y = static_cast<T*>(a.out) + at;
   float mu[V], rs[V], ga[V], be[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const int64_t g = p.b * a.groups + (p.c + c) / a.width;
+    const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
     mu[c] = a.mean[g];
     rs[c] = a.rstd[g];
     ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
     be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
   }
-  for (int64_t r = p.r0 + p.r; r < p.r1; r += p.step) {
+  const int32_t n_rows = p.r1 - p.r0;
+#pragma unroll 4
+  for (int32_t r = p.r; r < n_rows; r += p.step) {
     float v[V];
-    load_vec<V>(x + r * a.C, v);
+    load_vec<V>(x + (int64_t)r * a.C, v);
 #pragma unroll
-    for (int c = 0; c < V; ++c) v[c] = act_of<ACT>(fmaf((v[c] - mu[c]) * rs[c], ga[c], be[c]));
-    store_vec<V>(y + r * a.C, v);
+    for (int c = 0; c < V; ++c) v[c] = fmaf((v[c] - mu[c]) * rs[c], ga[c], be[c]);
+    activate<V>(a.act, v);
+    store_vec<V>(y + (int64_t)r * a.C, v);
   }
 }
 
-template <class T, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_grad_sums_kernel(GnArgs a) {
-  __shared__ float lds[kThreads][2 * V + 1];
+// Sums of a tile's dz and dz xh; with WHOLE dgamma_i, dbeta_i and dx too.
+template <class T, int V, bool WHOLE>
+__global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
+  extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
-  const T* x = static_cast<const T*>(a.x) + p.b * a.S * a.C + p.c;
-  const T* dy = static_cast<const T*>(a.dy) + p.b * a.S * a.C + p.c;
+  const int channels = a.units * V, h = helpers_of(channels);
+  float* seg1 = gn_lds;                       // [segs]
+  float* seg2 = seg1 + a.segs;                // [segs]
+  float* weighted = seg2 + a.segs;            // [channels] gamma times a channel's sum
+  float* lds = weighted + channels;
+  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  const T* x = static_cast<const T*>(a.x) + at;
+  const T* dy = static_cast<const T*>(a.dy) + at;
+  const int32_t n_rows = p.r1 - p.r0;
+
+  Raw<T, V> rx[kGradRows], rd[kGradRows];
+#pragma unroll
+  for (int k = 0; k < kGradRows; ++k) {
+    rx[k].zero();
+    rd[k].zero();
+    const int32_t r = p.r + k * p.step;
+    if (p.active && r < n_rows) {
+      rx[k].load(x + (int64_t)r * a.C);
+      rd[k].load(dy + (int64_t)r * a.C);
+    }
+  }
+  float rs[V], mu[V], ga[V], be[V];
+#pragma unroll
+  for (int c = 0; c < V; ++c) {
+    rs[c] = mu[c] = be[c] = 0.0f;
+    ga[c] = 1.0f;
+    if (p.active) {
+      const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
+      rs[c] = a.rstd[g];
+      mu[c] = a.mean[g];
+      if (a.gamma) ga[c] = a.gamma[p.c + c];
+      if (a.beta) be[c] = a.beta[p.c + c];
+    }
+  }
   float sb[V] = {}, sg[V] = {};
-  if (p.active) {
-    float mu[V], rs[V], ga[V], be[V];
+  float dz[kGradRows][V];
+#pragma unroll
+  for (int k = 0; k < kGradRows; ++k) {
+    float xv[V], z[V], slope[V];
+    rx[k].widen(xv);
+    rd[k].widen(dz[k]);
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const int64_t g = p.b * a.groups + (p.c + c) / a.width;
-      mu[c] = a.mean[g];
-      rs[c] = a.rstd[g];
-      ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
-      be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
+      xv[c] = (xv[c] - mu[c]) * rs[c];
+      z[c] = fmaf(xv[c], ga[c], be[c]);
     }
-    for (int64_t r = p.r0 + p.r; r < p.r1; r += p.step) {
-      float v[V], d[V];
-      load_vec<V>(x + r * a.C, v);
-      load_vec<V>(dy + r * a.C, d);
+    slopes<V>(a.act, z, slope);
+    const bool there = p.active && p.r + k * p.step < n_rows;
 #pragma unroll
-      for (int c = 0; c < V; ++c) {
-        const float xh = (v[c] - mu[c]) * rs[c];
-        const float dz = d[c] * slope_of<ACT>(fmaf(xh, ga[c], be[c]));
-        sb[c] += dz;
-        sg[c] = fmaf(dz, xh, sg[c]);
+    for (int c = 0; c < V; ++c) {
+      dz[k][c] = there ? dz[k][c] * slope[c] : 0.0f;
+      sb[c] += dz[k][c];
+      sg[c] += there ? dz[k][c] * xv[c] : 0.0f;
+    }
+  }
+  // One value a channel, to its place in the tile's or the example's sums.
+  const int64_t out_at = WHOLE ? (int64_t)p.b * a.C + p.c0
+                               : (((int64_t)p.b * a.chunks + p.chunk) * a.C + p.c0) * 2;
+  const float* from = sum_rows<V>(sb, p, a.units, lds);
+  for (int k = threadIdx.x; k < p.c1 - p.c0; k += blockDim.x) {
+    float s = 0.0f;
+    for (int i = 0; i < h; ++i) s += from[i * channels + k];
+    if constexpr (WHOLE) {
+      a.dbeta[out_at + k] = s;
+      weighted[k] = a.gamma ? a.gamma[p.c0 + k] * s : s;
+    } else {
+      a.partials[out_at + 2 * k] = s;
+    }
+  }
+  if constexpr (WHOLE) {
+    __syncthreads();
+    sum_groups(weighted, channels, 1, p, a.width, seg1);
+  } else {
+    __syncthreads();
+  }
+  from = sum_rows<V>(sg, p, a.units, lds);
+  for (int k = threadIdx.x; k < p.c1 - p.c0; k += blockDim.x) {
+    float s = 0.0f;
+    for (int i = 0; i < h; ++i) s += from[i * channels + k];
+    if constexpr (WHOLE) {
+      a.dgamma[out_at + k] = s;
+      weighted[k] = a.gamma ? a.gamma[p.c0 + k] * s : s;
+    } else {
+      a.partials[out_at + 2 * k + 1] = s;
+    }
+  }
+  if constexpr (WHOLE) {
+    __syncthreads();
+    sum_groups(weighted, channels, 1, p, a.width, seg2);
+    if (!p.active) return;
+    const float inv = 1.0f / ((float)a.S * (float)a.width);
+    float m1[V], m2[V];
+#pragma unroll
+    for (int c = 0; c < V; ++c) {
+      const int32_t g = (p.c + c) / a.width - p.first;
+      m1[c] = seg1[g] * inv;
+      m2[c] = seg2[g] * inv;
+    }
+    T* dx = static_cast<T*>(a.out) + at;
+#pragma unroll
+    for (int k = 0; k < kGradRows; ++k) {
+      const int32_t r = p.r + k * p.step;
+      if (r < n_rows) {
+        float xv[V];
+        rx[k].widen(xv);
+#pragma unroll
+        for (int c = 0; c < V; ++c) {
+          const float xh = (xv[c] - mu[c]) * rs[c];
+          dz[k][c] = rs[c] * (fmaf(dz[k][c], ga[c], -m1[c]) - xh * m2[c]);
+        }
+        store_vec<V>(dx + (int64_t)r * a.C, dz[k]);
       }
     }
   }
-  float* mine = lds[threadIdx.x];
-#pragma unroll
-  for (int c = 0; c < V; ++c) {
-    mine[2 * c] = sb[c];
-    mine[2 * c + 1] = sg[c];
-  }
-  int half = 1;
-  while (half < p.step) half <<= 1;
-  for (half >>= 1; half >= 1; half >>= 1) {
-    __syncthreads();
-    if (p.active && p.r < half && p.r + half < p.step) {
-      const float* other = lds[threadIdx.x + half * a.units];
-#pragma unroll
-      for (int c = 0; c < 2 * V; ++c) mine[c] += other[c];
-    }
-  }
-  if (p.active && p.r == 0) {
-    float* out = a.partials + ((p.b * a.chunks + p.chunk) * a.C + p.c) * 2;
-#pragma unroll
-    for (int c = 0; c < 2 * V; ++c) out[c] = mine[c];
-  }
 }
 
-// One wave per example and group: dgamma_i and dbeta_i of its channels, and the
-// means m1 and m2.
+// One workgroup per example and group: dgamma_i and dbeta_i of its channels, and
+// the means m1 and m2. Up to kThreads / width threads add a channel's tiles.
 __global__ __launch_bounds__(kThreads) void gn_grad_finish_kernel(GnArgs a) {
-  const int64_t job = (int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (job >= (int64_t)a.B * a.groups) return;
-  const int64_t b = job / a.groups, g = job - b * a.groups;
+  __shared__ float2 lds[kThreads];
+  __shared__ float red[kThreads / 64];
+  const uint32_t b = blockIdx.x / (uint32_t)a.groups;
+  const int32_t g = (int32_t)(blockIdx.x - b * (uint32_t)a.groups);
+  const int32_t wide = a.width < kThreads ? a.width : kThreads, h = kThreads / wide;
+  const int32_t j = threadIdx.x / wide, k0 = threadIdx.x - j * wide;
   float s1 = 0.0f, s2 = 0.0f;
-  for (int32_t k = lane; k < a.width; k += 64) {
-    const int64_t c = g * a.width + k;
-    float sb = 0.0f, sg = 0.0f;
-    for (int32_t chunk = 0; chunk < a.chunks; ++chunk) {
-      const float* s = a.partials + ((b * a.chunks + chunk) * a.C + c) * 2;
-      sb += s[0];
-      sg += s[1];
+  for (int32_t base = 0; base < a.width; base += wide) {
+    const int32_t k = base + k0;
+    const int64_t c = (int64_t)g * a.width + k;
+    float2 s = make_float2(0.0f, 0.0f);
+    if (j < h && k < a.width) {
+#pragma unroll 4
+      for (int32_t chunk = j; chunk < a.chunks; chunk += h) {
+        const float2 q = reinterpret_cast<const float2*>(a.partials)[((int64_t)b * a.chunks + chunk) * a.C + c];
+        s.x += q.x;
+        s.y += q.y;
+      }
     }
-    a.dbeta[b * a.C + c] = sb;
-    a.dgamma[b * a.C + c] = sg;
-    const float ga = a.gamma ? a.gamma[c] : 1.0f;
-    s1 = fmaf(ga, sb, s1);
-    s2 = fmaf(ga, sg, s2);
+    lds[threadIdx.x] = s;
+    __syncthreads();
+    if (j == 0 && k < a.width) {
+      for (int32_t i = 1; i < h; ++i) {
+        s.x += lds[i * wide + k0].x;
+        s.y += lds[i * wide + k0].y;
+      }
+      a.dbeta[(int64_t)b * a.C + c] = s.x;
+      a.dgamma[(int64_t)b * a.C + c] = s.y;
+      const float ga = a.gamma ? a.gamma[c] : 1.0f;
+      s1 = fmaf(ga, s.x, s1);
+      s2 = fmaf(ga, s.y, s2);
+    }
+    __syncthreads();
   }
-  s1 = wave_sum(s1);
-  s2 = wave_sum(s2);
+  s1 = block_sum(s1, red);
+  s2 = block_sum(s2, red);
   const float inv = 1.0f / ((float)a.S * (float)a.width);
-  if (lane == 0) a.sums[job] = make_float2(s1 * inv, s2 * inv);
+  if (threadIdx.x == 0) a.sums[blockIdx.x] = make_float2(s1 * inv, s2 * inv);
 }
 
-template <class T, int V, int ACT>
-__global__ __launch_bounds__(kThreads) void gn_grad_apply_kernel(GnArgs a) {
+template <class T, int V>
+__global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
   const Place p = place_of<V>(a);
   if (!p.active) return;
-  const T* x = static_cast<const T*>(a.x) + p.b * a.S * a.C + p.c;
-  const T* dy = static_cast<const T*>(a.dy) + p.b * a.S * a.C + p.c;
-  T* dx = static_cast<T*>(a.out) + p.b * a.S * a.C + p.c;
+  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  const T* x = static_cast<const T*>(a.x) + at;
+  const T* dy = static_cast<const T*>(a.dy) + at;
+  T* dx = static_cast<T*>(a.out) + at;
   float mu[V], rs[V], ga[V], be[V], m1[V], m2[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const int64_t g = p.b * a.groups + (p.c + c) / a.width;
+    const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
     mu[c] = a.mean[g];
     rs[c] = a.rstd[g];
     ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
@@ -335,40 +568,74 @@ __global__ __launch_bounds__(kThreads) void gn_grad_apply_kernel(GnArgs a) {
     m1[c] = a.sums[g].x;
     m2[c] = a.sums[g].y;
   }
-  for (int64_t r = p.r0 + p.r; r < p.r1; r += p.step) {
-    float v[V], d[V];
-    load_vec<V>(x + r * a.C, v);
-    load_vec<V>(dy + r * a.C, d);
+  const int32_t n_rows = p.r1 - p.r0;
+#pragma unroll 4
+  for (int32_t r = p.r; r < n_rows; r += p.step) {
+    float v[V], d[V], z[V], slope[V];
+    load_vec<V>(x + (int64_t)r * a.C, v);
+    load_vec<V>(dy + (int64_t)r * a.C, d);
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const float xh = (v[c] - mu[c]) * rs[c];
-      const float dz = d[c] * slope_of<ACT>(fmaf(xh, ga[c], be[c]));
-      d[c] = rs[c] * (fmaf(dz, ga[c], -m1[c]) - xh * m2[c]);
+      v[c] = (v[c] - mu[c]) * rs[c];
+      z[c] = fmaf(v[c], ga[c], be[c]);
     }
-    store_vec<V>(dx + r * a.C, d);
+    slopes<V>(a.act, z, slope);
+#pragma unroll
+    for (int c = 0; c < V; ++c) d[c] = rs[c] * (fmaf(d[c] * slope[c], ga[c], -m1[c]) - v[c] * m2[c]);
+    store_vec<V>(dx + (int64_t)r * a.C, d);
   }
 }
 
-// Split of the passes over the rows: blocks of channel vectors, and chunks of
-// rows so that about 2048 workgroups run, each thread with at least eight rows.
+// Tiles of one direction: `per_thread` rows of a thread.
 struct GnPlan {
-  int vec, units, blocks;
+  int vec, threads, units, blocks, segs;
   int64_t chunks, rows;
+  bool whole;
 };
 
-GnPlan plan_of(const dpsgd_group_norm& n) {
+// Channels of a block that are whole groups and whole vectors: the smallest
+// number, then as many as make a row of the block 128 bytes.
+int64_t block_channels(const dpsgd_group_norm& n, int vec, int64_t bytes) {
+  const int64_t width = n.C / n.groups;
+  int64_t least = width;
+  while (least % vec != 0) least += width;   // at most vec steps
+  int64_t cb = least * ceil_div(bytes, least * (n.dtype == DPSGD_BF16 ? 2 : 4));
+  return cb < n.C ? cb : n.C;
+}
+
+GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
   GnPlan p;
-  p.vec = vec_width(n.C, n.dtype == DPSGD_BF16 ? 8 : 4);
+  p.vec = vec_width(n.C, 4);
+  const int64_t width = n.C / n.groups;
+  // All rows of a block of whole groups in one tile, where that fits.
+  for (int64_t bytes : {128, 64}) {
+    const int64_t cb = block_channels(n, p.vec, bytes), units = ceil_div(cb, p.vec);
+    if (units > kTile || ceil_div(n.S, kTile / units) > per_thread) continue;
+    p.whole = true;
+    p.units = (int)units;
+    p.blocks = (int)ceil_div(n.C, cb);
+    // As many threads as one row each takes, within a workgroup.
+    const int64_t threads = round_up((size_t)(units * n.S), 64);
+    p.threads = (int)(threads < kTile ? threads : kTile);
+    p.chunks = 1;
+    p.rows = n.S;
+    p.segs = (int)(cb / width);
+    return p;
+  }
+  p.whole = false;
+  p.threads = kTile;
   const int64_t units = n.C / p.vec;
-  p.blocks = (int)ceil_div(units, kThreads);
+  p.blocks = (int)ceil_div(units, kTile);
   p.units = (int)ceil_div(units, p.blocks);
-  const int64_t least = 8 * (kThreads / p.units);
-  int64_t chunks = ceil_div(2048, n.B * p.blocks);
-  const int64_t most = ceil_div(n.S, least);
-  if (chunks > most) chunks = most;
-  p.rows = ceil_div(n.S, chunks);
+  p.rows = (int64_t)per_thread * (kTile / p.units);
+  if (p.rows > n.S) p.rows = n.S;
   p.chunks = ceil_div(n.S, p.rows);
+  p.segs = (int)((int64_t)p.units * p.vec / width + 2);
   return p;
+}
+
+int rows_of(const dpsgd_group_norm& n, bool backward) {
+  return backward ? kGradRows : n.dtype == DPSGD_BF16 ? kTileRows<uint16_t> : kTileRows<float>;
 }
 
 size_t stat_bytes(const dpsgd_group_norm& n) {
@@ -385,8 +652,8 @@ GnArgs args_of(const dpsgd_group_norm& n, const GnPlan& p, const void* x, void* 
   a.rstd = reinterpret_cast<float*>(static_cast<char*>(ws) + stat_bytes(n));
   a.sums = static_cast<float2*>(ws);   // the backward pass is given mean and rstd
   a.partials = reinterpret_cast<float*>(static_cast<char*>(ws) + 2 * stat_bytes(n));
-  a.S = n.S;
-  a.rows = p.rows;
+  a.S = (int32_t)n.S;
+  a.rows = (int32_t)p.rows;
   a.B = (int32_t)n.B;
   a.C = (int32_t)n.C;
   a.groups = (int32_t)n.groups;
@@ -394,75 +661,72 @@ GnArgs args_of(const dpsgd_group_norm& n, const GnPlan& p, const void* x, void* 
   a.chunks = (int32_t)p.chunks;
   a.blocks = p.blocks;
   a.units = p.units;
+  a.segs = p.segs;
+  a.act = n.act;
   a.eps = n.eps;
   return a;
 }
 
-template <class T, int V, int ACT>
-int run_forward(const GnArgs& a, uint32_t wgs, uint32_t finish, hipStream_t stream) {
-  hipLaunchKernelGGL((gn_stats_kernel<T, V>), dim3(wgs), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL(gn_finish_kernel, dim3(finish), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL((gn_apply_kernel<T, V, ACT>), dim3(wgs), dim3(kThreads), 0, stream, a);
-  return check_launch();
-}
-
-template <class T, int V, int ACT>
-int run_backward(const GnArgs& a, uint32_t wgs, uint32_t finish, hipStream_t stream) {
-  hipLaunchKernelGGL((gn_grad_sums_kernel<T, V, ACT>), dim3(wgs), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL(gn_grad_finish_kernel, dim3(finish), dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL((gn_grad_apply_kernel<T, V, ACT>), dim3(wgs), dim3(kThreads), 0, stream, a);
-  return check_launch();
-}
-
 template <class T, int V>
-int run_act(int act, bool backward, const GnArgs& a, uint32_t wgs, uint32_t finish,
-            hipStream_t stream) {
-  switch (act) {
-#define DPSGD_ACT(A)                                                      \
-  case A:                                                                 \
-    return backward ? run_backward<T, V, A>(a, wgs, finish, stream)       \
-                    : run_forward<T, V, A>(a, wgs, finish, stream);
-    DPSGD_ACT(DPSGD_ACT_RELU)
-    DPSGD_ACT(DPSGD_ACT_SILU)
-    DPSGD_ACT(DPSGD_ACT_GELU)
-    DPSGD_ACT(DPSGD_ACT_NONE)
-#undef DPSGD_ACT
-    default: return DPSGD_ERR_UNSUPPORTED;
+int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hipStream_t stream) {
+  const int64_t tiles = n.B * p.chunks * p.blocks, groups = n.B * n.groups;
+  if (tiles > 0x7FFFFFFF || groups > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
+  const dim3 grid((uint32_t)tiles), block((uint32_t)p.threads), by_group((uint32_t)groups);
+  const size_t sums = (size_t)sums_floats<V>(p.threads, p.units);
+  if (!backward) {
+    const size_t lds = (sums + 3 * (size_t)p.segs) * sizeof(float);
+    if (p.whole) {
+      hipLaunchKernelGGL((gn_tile_kernel<T, V, true>), grid, block, lds, stream, a);
+      return check_launch();
+    }
+    hipLaunchKernelGGL((gn_tile_kernel<T, V, false>), grid, block, lds, stream, a);
+    GnArgs f = a;
+    f.units = p.units * V;   // channels of a block
+    hipLaunchKernelGGL(gn_finish_kernel, by_group, dim3(kThreads), 0, stream, f);
+    hipLaunchKernelGGL((gn_apply_kernel<T, V>), grid, block, 0, stream, a);
+    return check_launch();
   }
+  const size_t lds = (sums + 2 * (size_t)p.segs + (size_t)p.units * V) * sizeof(float);
+  if (p.whole) {
+    hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, true>), grid, block, lds, stream, a);
+    return check_launch();
+  }
+  hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, false>), grid, block, lds, stream, a);
+  hipLaunchKernelGGL(gn_grad_finish_kernel, by_group, dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL((gn_grad_apply_kernel<T, V>), grid, block, 0, stream, a);
+  return check_launch();
 }
 
 int run_group_norm(const dpsgd_group_norm& n, const GnPlan& p, bool backward, const GnArgs& a,
                    hipStream_t stream) {
-  const int64_t wgs = n.B * p.chunks * p.blocks, finish = ceil_div(n.B * n.groups, kThreads / 64);
-  if (wgs > 0x7FFFFFFF || finish > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
-  const uint32_t w = (uint32_t)wgs, f = (uint32_t)finish;
   if (n.dtype == DPSGD_BF16) {
     switch (p.vec) {
-      case 8: return run_act<uint16_t, 8>(n.act, backward, a, w, f, stream);
-      case 4: return run_act<uint16_t, 4>(n.act, backward, a, w, f, stream);
-      case 2: return run_act<uint16_t, 2>(n.act, backward, a, w, f, stream);
-      default: return run_act<uint16_t, 1>(n.act, backward, a, w, f, stream);
+      case 4: return run<uint16_t, 4>(n, p, backward, a, stream);
+      case 2: return run<uint16_t, 2>(n, p, backward, a, stream);
+      default: return run<uint16_t, 1>(n, p, backward, a, stream);
     }
   }
   switch (p.vec) {
-    case 4: return run_act<float, 4>(n.act, backward, a, w, f, stream);
-    case 2: return run_act<float, 2>(n.act, backward, a, w, f, stream);
-    default: return run_act<float, 1>(n.act, backward, a, w, f, stream);
+    case 4: return run<float, 4>(n, p, backward, a, stream);
+    case 2: return run<float, 2>(n, p, backward, a, stream);
+    default: return run<float, 1>(n, p, backward, a, stream);
   }
 }
 
 }  // namespace
 
 // Workspace: mean and rstd where the caller does not take them (backward: m1 and
-// m2), then the chunks' statistics of every channel.
+// m2), then the tiles' statistics.
 size_t group_norm_workspace_bytes(const dpsgd_group_norm& n) {
-  const GnPlan p = plan_of(n);
-  return 2 * stat_bytes(n) + (size_t)(n.B * p.chunks * n.C) * 3 * sizeof(float);
+  const GnPlan f = plan_of(n, rows_of(n, false)), b = plan_of(n, rows_of(n, true));
+  const size_t forward = f.whole ? 0 : (size_t)(n.B * f.chunks * f.blocks * f.segs) * 3 * sizeof(float);
+  const size_t backward = b.whole ? 0 : (size_t)(n.B * b.chunks * n.C) * 2 * sizeof(float);
+  return 2 * stat_bytes(n) + (forward > backward ? forward : backward);
 }
 
 int launch_group_norm_forward(const dpsgd_group_norm& n, const void* x, void* y, float* mean,
                               float* rstd, void* workspace, hipStream_t stream) {
-  const GnPlan p = plan_of(n);
+  const GnPlan p = plan_of(n, rows_of(n, false));
   GnArgs a = args_of(n, p, x, y, workspace);
   if (mean) a.mean = mean;
   if (rstd) a.rstd = rstd;
@@ -472,7 +736,7 @@ int launch_group_norm_forward(const dpsgd_group_norm& n, const void* x, void* y,
 int launch_group_norm_backward(const dpsgd_group_norm& n, const void* x, const void* dy,
                                const float* mean, const float* rstd, void* dx, float* dgamma,
                                float* dbeta, void* workspace, hipStream_t stream) {
-  const GnPlan p = plan_of(n);
+  const GnPlan p = plan_of(n, rows_of(n, true));
   GnArgs a = args_of(n, p, x, dx, workspace);
   a.dy = dy;
   a.mean = const_cast<float*>(mean);   // read only in the backward kernels

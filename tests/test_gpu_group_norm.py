@@ -45,6 +45,12 @@ SHAPES = [   # B, S, C, groups
     (70, 3, 8, 2),
     (1, 2048, 320, 32),
     (2, 40, 2, 1),
+    (2, 3, 4100, 1),        # one group wider than a tile's block of channels
+    (1, 9, 2051, 1),        # the same, no vectors
+    (1, 40, 6200, 2),       # groups that straddle blocks
+    (2, 1023, 33, 3),       # whole groups in one tile, rows not a multiple of its step
+    (1, 5000, 12, 4),       # several tiles of narrow rows
+    (3, 300, 144, 9),       # blocks of several groups, the last one smaller
 ]
 
 

@@ -82,7 +82,7 @@ def test_embedding_refuses_bad_arguments(lib):
 BAD_GN = [
     (dict(B=0), INVALID), (dict(S=0), INVALID), (dict(C=0), INVALID), (dict(groups=0), INVALID),
     (dict(groups=5), INVALID), (dict(groups=24), INVALID), (dict(B=1 << 16, S=1 << 16), INVALID),
-    (dict(C=1 << 32, groups=1), INVALID), (dict(eps=0.0), INVALID), (dict(eps=-1.0), INVALID),
+    (dict(C=1 << 32, groups=1), INVALID), (dict(C=(1 << 20) + 1, groups=1), INVALID), (dict(eps=0.0), INVALID), (dict(eps=-1.0), INVALID),
     (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(dtype=2), UNSUPPORTED), (dict(act=4), UNSUPPORTED), (dict(act=-1), UNSUPPORTED),
 ]
