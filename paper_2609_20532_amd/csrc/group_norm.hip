@@ -96,6 +96,9 @@ struct GnArgs {
   int32_t B, C, groups, width;
   int32_t chunks, blocks;   // tiles of an example: row chunks, channel blocks
   int32_t units, segs;   // channel vectors of a block; most groups that a block has a part of
+  int32_t lanes, log;    // threads of a row, a power of two (log2: log) and at least units
+  uint32_t magic;        // division by width
+  int32_t shift;
   int32_t act;
   float eps;
 };
@@ -143,71 +146,58 @@ __device__ __forceinline__ Place place_of(const GnArgs& a) {
   const uint32_t rest = w - (uint32_t)p.b * per;
   p.chunk = (int32_t)(rest / (uint32_t)a.blocks);
   p.blk = (int32_t)(rest - (uint32_t)p.chunk * (uint32_t)a.blocks);
-  p.step = (int32_t)blockDim.x / a.units;
-  p.r = (int32_t)threadIdx.x / a.units;
-  p.unit = (int32_t)threadIdx.x - p.r * a.units;
+  p.step = (int32_t)blockDim.x >> a.log;
+  p.r = (int32_t)threadIdx.x >> a.log;
+  p.unit = (int32_t)threadIdx.x & (a.lanes - 1);
   p.c0 = p.blk * a.units * V;
   p.c1 = p.c0 + a.units * V < a.C ? p.c0 + a.units * V : a.C;
   p.c = p.c0 + p.unit * V;
-  p.active = p.r < p.step && p.c < a.C;
+  p.active = p.unit < a.units && p.c < a.C;
   p.r0 = p.chunk * a.rows;
   p.r1 = a.S - p.r0 < a.rows ? a.S : p.r0 + a.rows;
-  p.first = p.c0 / a.width;
-  p.here = (p.c1 - 1) / a.width - p.first + 1;
+  p.first = (int32_t)magic_divide((uint32_t)p.c0, a.magic, a.shift);
+  p.here = (int32_t)magic_divide((uint32_t)p.c1 - 1, a.magic, a.shift) - p.first + 1;
   return p;
 }
 
-// LDS of a tile's sums: one partial sum a thread and channel (each channel of
-// the vector padded by `units`, which keeps the reads below apart), then one a
-// helper and channel in the channels' own order.
-template <int V>
-__host__ __device__ constexpr int sums_floats(int threads, int units) {
-  return V * (threads + units) + (threads > units * V ? threads : units * V);
+// Rows that a tile's sums are left in: one a wave where a wave has several rows
+// of the block (those are added in registers), else one for each row of threads.
+__host__ __device__ __forceinline__ int slots_of(int threads, int log) {
+  return log < 6 ? threads >> 6 : threads >> log;
 }
 
-__device__ __forceinline__ int helpers_of(int channels) {
-  const int h = (int)blockDim.x / channels;
-  return h < 1 ? 1 : h;
-}
-
-// Sums each channel of the block over the threads that hold rows of it, to `h`
-// values [h][channels] in LDS; h is helpers_of(channels). Ends with a barrier.
+// A thread's V sums, added over the wave's rows, to lds[slot][channels].
 template <int V>
-__device__ __forceinline__ const float* sum_rows(const float (&v)[V], const Place& p, int units,
-                                                 float* lds) {
-  const int stride = (int)blockDim.x + units, channels = units * V, h = helpers_of(channels);
-  float* out = lds + V * stride;
-  if (p.r < p.step) {
+__device__ __forceinline__ void leave_sums(float (&v)[V], const Place& p, const GnArgs& a,
+                                           float* lds) {
+  for (int off = 32; off >= a.lanes; off >>= 1) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) lds[c * stride + threadIdx.x] = v[c];
+    for (int c = 0; c < V; ++c) v[c] += __shfl_xor(v[c], off, 64);
   }
-  __syncthreads();
-  for (int t = threadIdx.x; t < h * channels; t += blockDim.x) {
-    const int j = t / channels, k = t - j * channels, c = k / units, unit = k - c * units;
-    float s = 0.0f;
-#pragma unroll 4
-    for (int r = j; r < p.step; r += h) s += lds[c * stride + r * units + unit];
-    out[j * channels + unit * V + c] = s;
-  }
-  __syncthreads();
-  return out;
+  const int slot = a.log < 6 ? (int)threadIdx.x >> 6 : p.r;
+  if (p.unit < a.units && (a.log >= 6 || (int)(threadIdx.x & 63) < a.lanes))
+    store_vec<V>(lds + (slot * a.units + p.unit) * V, v);
 }
 
-// The sum over the block's part of each group, to seg[] in LDS, one wave a
-// group. Ends with a barrier.
-__device__ __forceinline__ void sum_groups(const float* from, int channels, int h, const Place& p,
-                                           int width, float* seg) {
+// The sum over the block's part of its j-th group, in every lane of a wave; lds
+// holds `slots` values a channel.
+__device__ __forceinline__ float group_sum(const float* lds, int slots, int channels, int j,
+                                           const Place& p, const GnArgs& a) {
   const int lane = threadIdx.x & 63;
-  for (int j = threadIdx.x >> 6; j < p.here; j += blockDim.x >> 6) {
-    const int g0 = (p.first + j) * width;
-    const int a = (g0 > p.c0 ? g0 : p.c0) - p.c0, b = (g0 + width < p.c1 ? g0 + width : p.c1) - p.c0;
-    float s = 0.0f;
-    for (int i = 0; i < h; ++i)
-      for (int k = a + lane; k < b; k += 64) s += from[i * channels + k];
-    s = wave_sum(s);
-    if (lane == 0) seg[j] = s;
+  const int g0 = (p.first + j) * a.width;
+  const int from = (g0 > p.c0 ? g0 : p.c0) - p.c0;
+  const int n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - p.c0 - from;
+  float s = 0.0f;
+  if (n == a.width) {
+    for (int k = lane; k < slots * n; k += 64) {
+      const int i = (int)magic_divide((uint32_t)k, a.magic, a.shift);
+      s += lds[i * channels + from + (k - i * n)];
+    }
+  } else {
+    for (int i = 0; i < slots; ++i)
+      for (int k = lane; k < n; k += 64) s += lds[i * channels + from + k];
   }
-  __syncthreads();
+  return wave_total(s);
 }
 
 // Statistics of a tile; with WHOLE (all rows, whole groups) the output too.
@@ -215,11 +205,12 @@ template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
   extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
-  const int channels = a.units * V, h = helpers_of(channels);
-  float* seg_mean = gn_lds;                // [segs]
-  float* seg_lo = seg_mean + a.segs;       // [segs]
-  float* seg_m2 = seg_lo + a.segs;         // [segs]
-  float* lds = seg_m2 + a.segs;
+  const int channels = a.units * V, slots = slots_of(blockDim.x, a.log);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  float* lds = gn_lds;                          // [2][slots][channels]
+  float* seg_mean = lds + 2 * slots * channels; // [segs]
+  float* seg_lo = seg_mean + a.segs;            // [segs]
+  float* seg_m2 = seg_lo + a.segs;              // [segs]
   const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
   const T* x = static_cast<const T*>(a.x) + at;
   const int32_t n_rows = p.r1 - p.r0;
@@ -239,7 +230,13 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
 #pragma unroll
     for (int c = 0; c < V; ++c) v[c] += f[c];
   }
-  sum_groups(sum_rows<V>(v, p, a.units, lds), channels, h, p, a.width, seg_mean);
+  leave_sums<V>(v, p, a, lds);
+  __syncthreads();
+  for (int j = wave; j < p.here; j += waves) {
+    const float s = group_sum(lds, slots, channels, j, p, a);
+    if ((threadIdx.x & 63) == 0) seg_mean[j] = s;
+  }
+  __syncthreads();
 
   // The mean of the tile's part of a group, and the deviations from it.
   float mu[V];
@@ -247,7 +244,7 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
 #pragma unroll
   for (int c = 0; c < V; ++c) {
     const int32_t ch = p.c + c < a.C ? p.c + c : a.C - 1;
-    j[c] = ch / a.width - p.first;
+    j[c] = (int32_t)magic_divide((uint32_t)ch, a.magic, a.shift) - p.first;
     const int32_t g0 = (p.first + j[c]) * a.width;
     const int32_t n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
     mu[c] = p.active ? seg_mean[j[c]] / ((float)n_rows * (float)n) : 0.0f;
@@ -272,8 +269,18 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
 #pragma unroll
     for (int c = 0; c < V; ++c) v[c] = q[c] = 0.0f;
   }
-  sum_groups(sum_rows<V>(v, p, a.units, lds), channels, h, p, a.width, seg_lo);
-  sum_groups(sum_rows<V>(q, p, a.units, lds), channels, h, p, a.width, seg_m2);
+  leave_sums<V>(v, p, a, lds);
+  leave_sums<V>(q, p, a, lds + slots * channels);
+  __syncthreads();
+  for (int j = wave; j < p.here; j += waves) {
+    const float s = group_sum(lds, slots, channels, j, p, a);
+    const float t = group_sum(lds + slots * channels, slots, channels, j, p, a);
+    if ((threadIdx.x & 63) == 0) {
+      seg_lo[j] = s;
+      seg_m2[j] = t;
+    }
+  }
+  __syncthreads();
 
   if constexpr (!WHOLE) {
     for (int s = threadIdx.x; s < p.here; s += blockDim.x) {
@@ -367,7 +374,7 @@ __global__ __launch_bounds__(kTile) void gn_apply_kernel(GnArgs a) {
   float mu[V], rs[V], ga[V], be[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
+    const int64_t g = (int64_t)p.b * a.groups + magic_divide((uint32_t)(p.c + c), a.magic, a.shift);
     mu[c] = a.mean[g];
     rs[c] = a.rstd[g];
     ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
@@ -390,11 +397,11 @@ template <class T, int V, bool WHOLE>
 __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
   extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
-  const int channels = a.units * V, h = helpers_of(channels);
-  float* seg1 = gn_lds;                       // [segs]
-  float* seg2 = seg1 + a.segs;                // [segs]
-  float* weighted = seg2 + a.segs;            // [channels] gamma times a channel's sum
-  float* lds = weighted + channels;
+  const int channels = a.units * V, slots = slots_of(blockDim.x, a.log);
+  const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  float* lds = gn_lds;                          // [2][slots][channels]
+  float* weighted = lds + 2 * slots * channels; // [2][channels]: gamma times a channel's sums
+  float* seg = weighted + 2 * channels;         // [segs][2]
   const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
   const T* x = static_cast<const T*>(a.x) + at;
   const T* dy = static_cast<const T*>(a.dy) + at;
@@ -417,7 +424,7 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
     rs[c] = mu[c] = be[c] = 0.0f;
     ga[c] = 1.0f;
     if (p.active) {
-      const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
+      const int64_t g = (int64_t)p.b * a.groups + magic_divide((uint32_t)(p.c + c), a.magic, a.shift);
       rs[c] = a.rstd[g];
       mu[c] = a.mean[g];
       if (a.gamma) ga[c] = a.gamma[p.c + c];
@@ -445,48 +452,47 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
       sg[c] += there ? dz[k][c] * xv[c] : 0.0f;
     }
   }
-  // One value a channel, to its place in the tile's or the example's sums.
-  const int64_t out_at = WHOLE ? (int64_t)p.b * a.C + p.c0
-                               : (((int64_t)p.b * a.chunks + p.chunk) * a.C + p.c0) * 2;
-  const float* from = sum_rows<V>(sb, p, a.units, lds);
+  leave_sums<V>(sb, p, a, lds);
+  leave_sums<V>(sg, p, a, lds + slots * channels);
+  __syncthreads();
+  // One pair a channel, to its place in the tile's or the example's sums.
   for (int k = threadIdx.x; k < p.c1 - p.c0; k += blockDim.x) {
-    float s = 0.0f;
-    for (int i = 0; i < h; ++i) s += from[i * channels + k];
+    float s = 0.0f, t = 0.0f;
+#pragma unroll 4
+    for (int i = 0; i < slots; ++i) {
+      s += lds[i * channels + k];
+      t += lds[(slots + i) * channels + k];
+    }
     if constexpr (WHOLE) {
-      a.dbeta[out_at + k] = s;
-      weighted[k] = a.gamma ? a.gamma[p.c0 + k] * s : s;
+      a.dbeta[(int64_t)p.b * a.C + p.c0 + k] = s;
+      a.dgamma[(int64_t)p.b * a.C + p.c0 + k] = t;
+      const float w = a.gamma ? a.gamma[p.c0 + k] : 1.0f;
+      weighted[k] = w * s;
+      weighted[channels + k] = w * t;
     } else {
-      a.partials[out_at + 2 * k] = s;
+      reinterpret_cast<float2*>(a.partials)[((int64_t)p.b * a.chunks + p.chunk) * a.C + p.c0 + k] =
+          make_float2(s, t);
     }
   }
   if constexpr (WHOLE) {
     __syncthreads();
-    sum_groups(weighted, channels, 1, p, a.width, seg1);
-  } else {
-    __syncthreads();
-  }
-  from = sum_rows<V>(sg, p, a.units, lds);
-  for (int k = threadIdx.x; k < p.c1 - p.c0; k += blockDim.x) {
-    float s = 0.0f;
-    for (int i = 0; i < h; ++i) s += from[i * channels + k];
-    if constexpr (WHOLE) {
-      a.dgamma[out_at + k] = s;
-      weighted[k] = a.gamma ? a.gamma[p.c0 + k] * s : s;
-    } else {
-      a.partials[out_at + 2 * k + 1] = s;
+    for (int j = wave; j < p.here; j += waves) {
+      const float s = group_sum(weighted, 1, channels, j, p, a);
+      const float t = group_sum(weighted + channels, 1, channels, j, p, a);
+      if ((threadIdx.x & 63) == 0) {
+        seg[2 * j] = s;
+        seg[2 * j + 1] = t;
+      }
     }
-  }
-  if constexpr (WHOLE) {
     __syncthreads();
-    sum_groups(weighted, channels, 1, p, a.width, seg2);
     if (!p.active) return;
     const float inv = 1.0f / ((float)a.S * (float)a.width);
     float m1[V], m2[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const int32_t g = (p.c + c) / a.width - p.first;
-      m1[c] = seg1[g] * inv;
-      m2[c] = seg2[g] * inv;
+      const int32_t j = (int32_t)magic_divide((uint32_t)(p.c + c), a.magic, a.shift) - p.first;
+      m1[c] = seg[2 * j] * inv;
+      m2[c] = seg[2 * j + 1] * inv;
     }
     T* dx = static_cast<T*>(a.out) + at;
 #pragma unroll
@@ -560,7 +566,7 @@ __global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
   float mu[V], rs[V], ga[V], be[V], m1[V], m2[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
-    const int64_t g = (int64_t)p.b * a.groups + (p.c + c) / a.width;
+    const int64_t g = (int64_t)p.b * a.groups + magic_divide((uint32_t)(p.c + c), a.magic, a.shift);
     mu[c] = a.mean[g];
     rs[c] = a.rstd[g];
     ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
@@ -588,7 +594,7 @@ __global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
 
 // Tiles of one direction: `per_thread` rows of a thread.
 struct GnPlan {
-  int vec, threads, units, blocks, segs;
+  int vec, threads, units, lanes, log, blocks, segs;
   int64_t chunks, rows;
   bool whole;
 };
@@ -603,6 +609,14 @@ int64_t block_channels(const dpsgd_group_norm& n, int vec, int64_t bytes) {
   return cb < n.C ? cb : n.C;
 }
 
+// Threads of a row: the power of two from `units` on, so that rows lie in whole
+// waves or waves in whole rows, and sums over a wave's rows are shuffles.
+void set_lanes(GnPlan* p) {
+  p->log = 0;
+  while ((1 << p->log) < p->units) ++p->log;
+  p->lanes = 1 << p->log;
+}
+
 GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
   GnPlan p;
   p.vec = vec_width(n.C, 4);
@@ -610,12 +624,14 @@ GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
   // All rows of a block of whole groups in one tile, where that fits.
   for (int64_t bytes : {128, 64}) {
     const int64_t cb = block_channels(n, p.vec, bytes), units = ceil_div(cb, p.vec);
-    if (units > kTile || ceil_div(n.S, kTile / units) > per_thread) continue;
-    p.whole = true;
+    if (units > kTile) continue;
     p.units = (int)units;
+    set_lanes(&p);
+    if (ceil_div(n.S, kTile / p.lanes) > per_thread) continue;
+    p.whole = true;
     p.blocks = (int)ceil_div(n.C, cb);
     // As many threads as one row each takes, within a workgroup.
-    const int64_t threads = round_up((size_t)(units * n.S), 64);
+    const int64_t threads = round_up((size_t)(p.lanes * n.S), 64);
     p.threads = (int)(threads < kTile ? threads : kTile);
     p.chunks = 1;
     p.rows = n.S;
@@ -627,7 +643,8 @@ GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
   const int64_t units = n.C / p.vec;
   p.blocks = (int)ceil_div(units, kTile);
   p.units = (int)ceil_div(units, p.blocks);
-  p.rows = (int64_t)per_thread * (kTile / p.units);
+  set_lanes(&p);
+  p.rows = (int64_t)per_thread * (kTile / p.lanes);
   if (p.rows > n.S) p.rows = n.S;
   p.chunks = ceil_div(n.S, p.rows);
   p.segs = (int)((int64_t)p.units * p.vec / width + 2);
@@ -662,6 +679,9 @@ GnArgs args_of(const dpsgd_group_norm& n, const GnPlan& p, const void* x, void* 
   a.blocks = p.blocks;
   a.units = p.units;
   a.segs = p.segs;
+  a.lanes = p.lanes;
+  a.log = p.log;
+  divide_magic(n.C / n.groups, &a.magic, &a.shift);
   a.act = n.act;
   a.eps = n.eps;
   return a;
@@ -672,7 +692,7 @@ int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hip
   const int64_t tiles = n.B * p.chunks * p.blocks, groups = n.B * n.groups;
   if (tiles > 0x7FFFFFFF || groups > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
   const dim3 grid((uint32_t)tiles), block((uint32_t)p.threads), by_group((uint32_t)groups);
-  const size_t sums = (size_t)sums_floats<V>(p.threads, p.units);
+  const size_t channels = (size_t)p.units * V, sums = 2 * (size_t)slots_of(p.threads, p.log) * channels;
   if (!backward) {
     const size_t lds = (sums + 3 * (size_t)p.segs) * sizeof(float);
     if (p.whole) {
@@ -686,7 +706,7 @@ int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hip
     hipLaunchKernelGGL((gn_apply_kernel<T, V>), grid, block, 0, stream, a);
     return check_launch();
   }
-  const size_t lds = (sums + 2 * (size_t)p.segs + (size_t)p.units * V) * sizeof(float);
+  const size_t lds = (sums + 2 * channels + 2 * (size_t)p.segs) * sizeof(float);
   if (p.whole) {
     hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, true>), grid, block, lds, stream, a);
     return check_launch();

@@ -128,6 +128,21 @@ inline int vec_width(int64_t n, int most) {
   return 1;
 }
 
+// Sum over the lanes of a wave in every lane, in a fixed order: shifts within rows
+// of 16 lanes, then the rows' last lanes to the rows after them (no LDS).
+__device__ __forceinline__ float wave_total(float v) {
+#define DPSGD_DPP(ctrl, rows) \
+  v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+  DPSGD_DPP(0x111, 0xf);   // row_shr 1, 2, 4, 8
+  DPSGD_DPP(0x112, 0xf);
+  DPSGD_DPP(0x114, 0xf);
+  DPSGD_DPP(0x118, 0xf);
+  DPSGD_DPP(0x142, 0xa);   // row_bcast 15, 31
+  DPSGD_DPP(0x143, 0xc);
+#undef DPSGD_DPP
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
 // n / d for n < 2^31, by the magic and shift of divide_magic.
 __device__ __forceinline__ uint32_t magic_divide(uint32_t n, uint32_t magic, int32_t shift) {
   return shift < 0 ? n : __umulhi(n, magic) >> shift;
