@@ -179,6 +179,12 @@ __device__ __forceinline__ void leave_sums(float (&v)[V], const Place& p, const 
     store_vec<V>(lds + (slot * a.units + p.unit) * V, v);
 }
 
+// Channels of the block's j-th group that are in the block.
+__device__ __forceinline__ int part_of(int j, const Place& p, const GnArgs& a) {
+  const int g0 = (p.first + j) * a.width;
+  return (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
+}
+
 // The sum over the block's part of its j-th group, in every lane of a wave; lds
 // holds `slots` values a channel.
 __device__ __forceinline__ float group_sum(const float* lds, int slots, int channels, int j,
@@ -186,7 +192,7 @@ __device__ __forceinline__ float group_sum(const float* lds, int slots, int chan
   const int lane = threadIdx.x & 63;
   const int g0 = (p.first + j) * a.width;
   const int from = (g0 > p.c0 ? g0 : p.c0) - p.c0;
-  const int n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - p.c0 - from;
+  const int n = part_of(j, p, a);
   float s = 0.0f;
   if (n == a.width) {
     for (int k = lane; k < slots * n; k += 64) {
@@ -202,16 +208,15 @@ __device__ __forceinline__ float group_sum(const float* lds, int slots, int chan
 
 // Statistics of a tile; with WHOLE (all rows, whole groups) the output too.
 template <class T, int V, bool WHOLE>
-__global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
+__global__ __launch_bounds__(kTile, 8) void gn_tile_kernel(GnArgs a) {
   extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
   const int channels = a.units * V, slots = slots_of(blockDim.x, a.log);
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   float* lds = gn_lds;                          // [2][slots][channels]
   float* seg_mean = lds + 2 * slots * channels; // [segs]
-  float* seg_lo = seg_mean + a.segs;            // [segs]
-  float* seg_m2 = seg_lo + a.segs;              // [segs]
-  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  float* seg_rstd = seg_mean + a.segs;          // [segs]
+  const int64_t at = ((int64_t)p.b * a.S + p.r0 + p.r) * a.C + p.c, stride = (int64_t)p.step * a.C;
   const T* x = static_cast<const T*>(a.x) + at;
   const int32_t n_rows = p.r1 - p.r0;
 
@@ -221,7 +226,7 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
   for (int k = 0; k < kTileRows<T>; ++k) {
     raw[k].zero();
     const int32_t r = p.r + k * p.step;
-    if (p.active && r < n_rows) raw[k].load(x + (int64_t)r * a.C);
+    if (p.active && r < n_rows) raw[k].load(x + k * stride);
   }
 #pragma unroll
   for (int k = 0; k < kTileRows<T>; ++k) {
@@ -234,21 +239,15 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
   __syncthreads();
   for (int j = wave; j < p.here; j += waves) {
     const float s = group_sum(lds, slots, channels, j, p, a);
-    if ((threadIdx.x & 63) == 0) seg_mean[j] = s;
+    if ((threadIdx.x & 63) == 0) seg_mean[j] = s / ((float)n_rows * (float)part_of(j, p, a));
   }
   __syncthreads();
 
-  // The mean of the tile's part of a group, and the deviations from it.
+  // The deviations from the mean of the tile's part of a group.
   float mu[V];
-  int32_t j[V];
 #pragma unroll
-  for (int c = 0; c < V; ++c) {
-    const int32_t ch = p.c + c < a.C ? p.c + c : a.C - 1;
-    j[c] = (int32_t)magic_divide((uint32_t)ch, a.magic, a.shift) - p.first;
-    const int32_t g0 = (p.first + j[c]) * a.width;
-    const int32_t n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
-    mu[c] = p.active ? seg_mean[j[c]] / ((float)n_rows * (float)n) : 0.0f;
-  }
+  for (int c = 0; c < V; ++c)
+    mu[c] = p.active ? seg_mean[magic_divide((uint32_t)(p.c + c), a.magic, a.shift) - (uint32_t)p.first] : 0.0f;
   float q[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) v[c] = q[c] = 0.0f;
@@ -256,6 +255,7 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
   for (int k = 0; k < kTileRows<T>; ++k) {
     if (p.r + k * p.step < n_rows) {
       float f[V];
+      raw[k].keep_raw();
       raw[k].widen(f);
 #pragma unroll
       for (int c = 0; c < V; ++c) {
@@ -276,51 +276,46 @@ __global__ __launch_bounds__(kTile) void gn_tile_kernel(GnArgs a) {
     const float s = group_sum(lds, slots, channels, j, p, a);
     const float t = group_sum(lds + slots * channels, slots, channels, j, p, a);
     if ((threadIdx.x & 63) == 0) {
-      seg_lo[j] = s;
-      seg_m2[j] = t;
+      if constexpr (WHOLE) {
+        // The group's mean and rstd, for everyone.
+        const float count = (float)a.S * (float)a.width, lo = s / count;
+        const float mean = seg_mean[j] + lo;
+        const float rstd = 1.0f / sqrtf(about_mean(t, count, lo) / count + a.eps);
+        const int64_t g = (int64_t)p.b * a.groups + p.first + j;
+        a.mean[g] = seg_mean[j] = mean;
+        a.rstd[g] = seg_rstd[j] = rstd;
+      } else {
+        const float count = (float)n_rows * (float)part_of(j, p, a), lo = s / count;
+        float* to = a.partials + ((int64_t)blockIdx.x * a.segs + j) * 3;
+        to[0] = seg_mean[j];
+        to[1] = lo;
+        to[2] = about_mean(t, count, lo);
+      }
     }
   }
-  __syncthreads();
 
-  if constexpr (!WHOLE) {
-    for (int s = threadIdx.x; s < p.here; s += blockDim.x) {
-      const int32_t g0 = (p.first + s) * a.width;
-      const int32_t n = (g0 + a.width < p.c1 ? g0 + a.width : p.c1) - (g0 > p.c0 ? g0 : p.c0);
-      const float count = (float)n_rows * (float)n, lo = seg_lo[s] / count;
-      float* to = a.partials + (((int64_t)blockIdx.x) * a.segs + s) * 3;
-      to[0] = seg_mean[s] / count;
-      to[1] = lo;
-      to[2] = about_mean(seg_m2[s], count, lo);
-    }
-  } else {
-    const float count = (float)a.S * (float)a.width;
-    for (int s = threadIdx.x; s < p.here; s += blockDim.x) {
-      const float lo = seg_lo[s] / count;
-      const int64_t g = (int64_t)p.b * a.groups + p.first + s;
-      a.mean[g] = seg_mean[s] / count + lo;
-      a.rstd[g] = 1.0f / sqrtf(about_mean(seg_m2[s], count, lo) / count + a.eps);
-    }
+  if constexpr (WHOLE) {
+    __syncthreads();
     if (!p.active) return;
-    float rs[V], ga[V], be[V];
+    float scale[V], be[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const float lo = seg_lo[j[c]] / count;
-      rs[c] = 1.0f / sqrtf(about_mean(seg_m2[j[c]], count, lo) / count + a.eps);
-      mu[c] += lo;
-      ga[c] = a.gamma ? a.gamma[p.c + c] : 1.0f;
+      const int32_t s = (int32_t)magic_divide((uint32_t)(p.c + c), a.magic, a.shift) - p.first;
+      mu[c] = seg_mean[s];
+      scale[c] = a.gamma ? seg_rstd[s] * a.gamma[p.c + c] : seg_rstd[s];
       be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
     }
     T* y = static_cast<T*>(a.out) + at;
 #pragma unroll
     for (int k = 0; k < kTileRows<T>; ++k) {
-      const int32_t r = p.r + k * p.step;
-      if (r < n_rows) {
+      if (p.r + k * p.step < n_rows) {
         float f[V];
+        raw[k].keep_raw();
         raw[k].widen(f);
 #pragma unroll
-        for (int c = 0; c < V; ++c) f[c] = fmaf((f[c] - mu[c]) * rs[c], ga[c], be[c]);
+        for (int c = 0; c < V; ++c) f[c] = fmaf(f[c] - mu[c], scale[c], be[c]);
         activate<V>(a.act, f);
-        store_vec<V>(y + (int64_t)r * a.C, f);
+        store_vec<V>(y + k * stride, f);
       }
     }
   }
@@ -694,7 +689,7 @@ int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hip
   const dim3 grid((uint32_t)tiles), block((uint32_t)p.threads), by_group((uint32_t)groups);
   const size_t channels = (size_t)p.units * V, sums = 2 * (size_t)slots_of(p.threads, p.log) * channels;
   if (!backward) {
-    const size_t lds = (sums + 3 * (size_t)p.segs) * sizeof(float);
+    const size_t lds = (sums + 2 * (size_t)p.segs) * sizeof(float);
     if (p.whole) {
       hipLaunchKernelGGL((gn_tile_kernel<T, V, true>), grid, block, lds, stream, a);
       return check_launch();

@@ -110,6 +110,15 @@ struct Raw {
     for (uint32_t& x : w) x = 0;
   }
 
+  // Keeps the compiler from holding on to values that were widened before: later
+  // uses widen again, from half the registers.
+  __device__ __forceinline__ void keep_raw() {
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+      for (uint32_t& x : w) asm volatile("" : "+v"(x));
+    }
+  }
+
   __device__ __forceinline__ void widen(float (&x)[V]) const {
 #pragma unroll
     for (int c = 0; c < V; ++c) {
