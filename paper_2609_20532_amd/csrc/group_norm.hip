@@ -25,6 +25,7 @@ namespace dpsgd {
 namespace {
 
 constexpr int kTile = 1024;    // most threads of a tile's workgroup
+constexpr uint32_t kXcds = 8;
 constexpr int kGradRows = 8;   // rows of a thread in a backward tile
 
 // Rows of a thread in a forward tile: 32 registers of 4 elements each.
@@ -40,45 +41,39 @@ __device__ __forceinline__ float sigmoid(float z) {
 constexpr float kGelu0 = 0.7978845608028654f;   // sqrt(2 / pi)
 constexpr float kGelu1 = 0.044715f;
 
-// x = act(x), or slope = act'(x), for V values. 0.5 (1 + tanh u) = sigmoid(2 u).
-template <int V>
-__device__ __forceinline__ void activate(int act, float (&x)[V]) {
-  if (act == DPSGD_ACT_RELU) {
+// x = act(x), or slope = act'(z), for V values. 0.5 (1 + tanh u) = sigmoid(2 u).
+template <int ACT, int V>
+__device__ __forceinline__ void activate(float (&x)[V]) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) x[c] = x[c] < 0.0f ? 0.0f : x[c];   // a NaN stays
-  } else if (act == DPSGD_ACT_SILU) {
-#pragma unroll
-    for (int c = 0; c < V; ++c) x[c] *= sigmoid(x[c]);
-  } else if (act == DPSGD_ACT_GELU) {
-#pragma unroll
-    for (int c = 0; c < V; ++c)
+  for (int c = 0; c < V; ++c) {
+    if constexpr (ACT == DPSGD_ACT_RELU) x[c] = x[c] < 0.0f ? 0.0f : x[c];   // a NaN stays
+    if constexpr (ACT == DPSGD_ACT_SILU) x[c] *= sigmoid(x[c]);
+    if constexpr (ACT == DPSGD_ACT_GELU)
       x[c] *= sigmoid(2.0f * kGelu0 * fmaf(kGelu1 * x[c] * x[c], x[c], x[c]));
   }
 }
 
-template <int V>
-__device__ __forceinline__ void slopes(int act, const float (&z)[V], float (&slope)[V]) {
-  if (act == DPSGD_ACT_RELU) {
+template <int ACT, int V>
+__device__ __forceinline__ void slopes(const float (&z)[V], float (&slope)[V]) {
 #pragma unroll
-    for (int c = 0; c < V; ++c) slope[c] = z[c] > 0.0f ? 1.0f : (z[c] == z[c] ? 0.0f : z[c]);
-  } else if (act == DPSGD_ACT_SILU) {
-#pragma unroll
-    for (int c = 0; c < V; ++c) {
+  for (int c = 0; c < V; ++c) {
+    slope[c] = 1.0f;
+    if constexpr (ACT == DPSGD_ACT_RELU) slope[c] = z[c] > 0.0f ? 1.0f : (z[c] == z[c] ? 0.0f : z[c]);
+    if constexpr (ACT == DPSGD_ACT_SILU) {
       const float p = sigmoid(z[c]);
       slope[c] = p * fmaf(z[c], 1.0f - p, 1.0f);
     }
-  } else if (act == DPSGD_ACT_GELU) {
-#pragma unroll
-    for (int c = 0; c < V; ++c) {
+    if constexpr (ACT == DPSGD_ACT_GELU) {
       const float p = sigmoid(2.0f * kGelu0 * fmaf(kGelu1 * z[c] * z[c], z[c], z[c]));
       const float du = kGelu0 * fmaf(3.0f * kGelu1 * z[c], z[c], 1.0f);
       slope[c] = fmaf(2.0f * z[c] * p * (1.0f - p), du, p);
     }
-  } else {
-#pragma unroll
-    for (int c = 0; c < V; ++c) slope[c] = 1.0f;
   }
 }
+
+// Rows of a thread's tile are worked on one after the other: interleaved, their
+// intermediate values do not fit the registers beside the tile.
+__device__ __forceinline__ void row_by_row() { __builtin_amdgcn_sched_barrier(0); }
 
 struct GnArgs {
   const void* x;
@@ -96,10 +91,10 @@ struct GnArgs {
   int32_t B, C, groups, width;
   int32_t chunks, blocks;   // tiles of an example: row chunks, channel blocks
   int32_t units, segs;   // channel vectors of a block; most groups that a block has a part of
+  int32_t by_xcd;        // order of the tiles (grid rounded up to whole rounds of examples)
   int32_t lanes, log;    // threads of a row, a power of two (log2: log) and at least units
   uint32_t magic;        // division by width
   int32_t shift;
-  int32_t act;
   float eps;
 };
 
@@ -142,8 +137,15 @@ template <int V>
 __device__ __forceinline__ Place place_of(const GnArgs& a) {
   Place p;
   const uint32_t w = blockIdx.x, per = (uint32_t)a.blocks * (uint32_t)a.chunks;
-  p.b = (int32_t)(w / per);
-  const uint32_t rest = w - (uint32_t)p.b * per;
+  uint32_t rest;
+  if (a.by_xcd) {   // workgroups go to the XCDs in turn: an example's tiles to one of them
+    const uint32_t i = w / kXcds;
+    p.b = (int32_t)(i / per * kXcds + w % kXcds);
+    rest = i % per;
+  } else {
+    p.b = (int32_t)(w / per);
+    rest = w - (uint32_t)p.b * per;
+  }
   p.chunk = (int32_t)(rest / (uint32_t)a.blocks);
   p.blk = (int32_t)(rest - (uint32_t)p.chunk * (uint32_t)a.blocks);
   p.step = (int32_t)blockDim.x >> a.log;
@@ -207,10 +209,11 @@ __device__ __forceinline__ float group_sum(const float* lds, int slots, int chan
 }
 
 // Statistics of a tile; with WHOLE (all rows, whole groups) the output too.
-template <class T, int V, bool WHOLE>
+template <class T, int V, int ACT, bool WHOLE>
 __global__ __launch_bounds__(kTile, 8) void gn_tile_kernel(GnArgs a) {
   extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
+  if (p.b >= a.B) return;   // the whole workgroup
   const int channels = a.units * V, slots = slots_of(blockDim.x, a.log);
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   float* lds = gn_lds;                          // [2][slots][channels]
@@ -297,12 +300,12 @@ __global__ __launch_bounds__(kTile, 8) void gn_tile_kernel(GnArgs a) {
   if constexpr (WHOLE) {
     __syncthreads();
     if (!p.active) return;
-    float scale[V], be[V];
+    float ga[V], be[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       const int32_t s = (int32_t)magic_divide((uint32_t)(p.c + c), a.magic, a.shift) - p.first;
       mu[c] = seg_mean[s];
-      scale[c] = a.gamma ? seg_rstd[s] * a.gamma[p.c + c] : seg_rstd[s];
+      ga[c] = a.gamma ? seg_rstd[s] * a.gamma[p.c + c] : seg_rstd[s];
       be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
     }
     T* y = static_cast<T*>(a.out) + at;
@@ -313,9 +316,10 @@ __global__ __launch_bounds__(kTile, 8) void gn_tile_kernel(GnArgs a) {
         raw[k].keep_raw();
         raw[k].widen(f);
 #pragma unroll
-        for (int c = 0; c < V; ++c) f[c] = fmaf(f[c] - mu[c], scale[c], be[c]);
-        activate<V>(a.act, f);
+        for (int c = 0; c < V; ++c) f[c] = fmaf(f[c] - mu[c], ga[c], be[c]);
+        activate<ACT, V>(f);
         store_vec<V>(y + k * stride, f);
+        row_by_row();
       }
     }
   }
@@ -359,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void gn_finish_kernel(GnArgs a) {
   }
 }
 
-template <class T, int V>
+template <class T, int V, int ACT>
 __global__ __launch_bounds__(kTile) void gn_apply_kernel(GnArgs a) {
   const Place p = place_of<V>(a);
   if (!p.active) return;
@@ -382,22 +386,23 @@ __global__ __launch_bounds__(kTile) void gn_apply_kernel(GnArgs a) {
     load_vec<V>(x + (int64_t)r * a.C, v);
 #pragma unroll
     for (int c = 0; c < V; ++c) v[c] = fmaf((v[c] - mu[c]) * rs[c], ga[c], be[c]);
-    activate<V>(a.act, v);
+    activate<ACT, V>(v);
     store_vec<V>(y + (int64_t)r * a.C, v);
   }
 }
 
 // Sums of a tile's dz and dz xh; with WHOLE dgamma_i, dbeta_i and dx too.
-template <class T, int V, bool WHOLE>
+template <class T, int V, int ACT, bool WHOLE>
 __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
   extern __shared__ __align__(16) float gn_lds[];
   const Place p = place_of<V>(a);
+  if (p.b >= a.B) return;   // the whole workgroup
   const int channels = a.units * V, slots = slots_of(blockDim.x, a.log);
   const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
   float* lds = gn_lds;                          // [2][slots][channels]
   float* weighted = lds + 2 * slots * channels; // [2][channels]: gamma times a channel's sums
   float* seg = weighted + 2 * channels;         // [segs][2]
-  const int64_t at = ((int64_t)p.b * a.S + p.r0) * a.C + p.c;
+  const int64_t at = ((int64_t)p.b * a.S + p.r0 + p.r) * a.C + p.c, stride = (int64_t)p.step * a.C;
   const T* x = static_cast<const T*>(a.x) + at;
   const T* dy = static_cast<const T*>(a.dy) + at;
   const int32_t n_rows = p.r1 - p.r0;
@@ -409,8 +414,8 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
     rd[k].zero();
     const int32_t r = p.r + k * p.step;
     if (p.active && r < n_rows) {
-      rx[k].load(x + (int64_t)r * a.C);
-      rd[k].load(dy + (int64_t)r * a.C);
+      rx[k].load(x + k * stride);
+      rd[k].load(dy + k * stride);
     }
   }
   float rs[V], mu[V], ga[V], be[V];
@@ -438,14 +443,16 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
       xv[c] = (xv[c] - mu[c]) * rs[c];
       z[c] = fmaf(xv[c], ga[c], be[c]);
     }
-    slopes<V>(a.act, z, slope);
+    slopes<ACT, V>(z, slope);
     const bool there = p.active && p.r + k * p.step < n_rows;
 #pragma unroll
     for (int c = 0; c < V; ++c) {
       dz[k][c] = there ? dz[k][c] * slope[c] : 0.0f;
       sb[c] += dz[k][c];
       sg[c] += there ? dz[k][c] * xv[c] : 0.0f;
+      if constexpr (sizeof(T) == 4 && WHOLE) rx[k].w[c] = __float_as_uint(xv[c]);   // xh in x's place
     }
+    row_by_row();
   }
   leave_sums<V>(sb, p, a, lds);
   leave_sums<V>(sg, p, a, lds + slots * channels);
@@ -492,16 +499,17 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
     T* dx = static_cast<T*>(a.out) + at;
 #pragma unroll
     for (int k = 0; k < kGradRows; ++k) {
-      const int32_t r = p.r + k * p.step;
-      if (r < n_rows) {
+      if (p.r + k * p.step < n_rows) {
         float xv[V];
+        rx[k].keep_raw();
         rx[k].widen(xv);
 #pragma unroll
         for (int c = 0; c < V; ++c) {
-          const float xh = (xv[c] - mu[c]) * rs[c];
+          const float xh = sizeof(T) == 4 ? xv[c] : (xv[c] - mu[c]) * rs[c];
           dz[k][c] = rs[c] * (fmaf(dz[k][c], ga[c], -m1[c]) - xh * m2[c]);
         }
-        store_vec<V>(dx + (int64_t)r * a.C, dz[k]);
+        store_vec<V>(dx + k * stride, dz[k]);
+        row_by_row();
       }
     }
   }
@@ -550,7 +558,7 @@ __global__ __launch_bounds__(kThreads) void gn_grad_finish_kernel(GnArgs a) {
   if (threadIdx.x == 0) a.sums[blockIdx.x] = make_float2(s1 * inv, s2 * inv);
 }
 
-template <class T, int V>
+template <class T, int V, int ACT>
 __global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
   const Place p = place_of<V>(a);
   if (!p.active) return;
@@ -580,7 +588,7 @@ __global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
       v[c] = (v[c] - mu[c]) * rs[c];
       z[c] = fmaf(v[c], ga[c], be[c]);
     }
-    slopes<V>(a.act, z, slope);
+    slopes<ACT, V>(z, slope);
 #pragma unroll
     for (int c = 0; c < V; ++c) d[c] = rs[c] * (fmaf(d[c] * slope[c], ga[c], -m1[c]) - v[c] * m2[c]);
     store_vec<V>(dx + (int64_t)r * a.C, d);
@@ -591,7 +599,7 @@ __global__ __launch_bounds__(kTile) void gn_grad_apply_kernel(GnArgs a) {
 struct GnPlan {
   int vec, threads, units, lanes, log, blocks, segs;
   int64_t chunks, rows;
-  bool whole;
+  bool whole, by_xcd;
 };
 
 // Channels of a block that are whole groups and whole vectors: the smallest
@@ -631,9 +639,10 @@ GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
     p.chunks = 1;
     p.rows = n.S;
     p.segs = (int)(cb / width);
+    p.by_xcd = bytes < 128 && p.blocks > 1 && n.B >= 64;
     return p;
   }
-  p.whole = false;
+  p.whole = p.by_xcd = false;
   p.threads = kTile;
   const int64_t units = n.C / p.vec;
   p.blocks = (int)ceil_div(units, kTile);
@@ -674,57 +683,69 @@ GnArgs args_of(const dpsgd_group_norm& n, const GnPlan& p, const void* x, void* 
   a.blocks = p.blocks;
   a.units = p.units;
   a.segs = p.segs;
+  a.by_xcd = p.by_xcd;
   a.lanes = p.lanes;
   a.log = p.log;
   divide_magic(n.C / n.groups, &a.magic, &a.shift);
-  a.act = n.act;
   a.eps = n.eps;
   return a;
 }
 
-template <class T, int V>
+template <class T, int V, int ACT>
 int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hipStream_t stream) {
-  const int64_t tiles = n.B * p.chunks * p.blocks, groups = n.B * n.groups;
+  const int64_t B = p.by_xcd ? (int64_t)round_up((size_t)n.B, kXcds) : n.B;
+  const int64_t tiles = B * p.chunks * p.blocks, groups = n.B * n.groups;
   if (tiles > 0x7FFFFFFF || groups > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
   const dim3 grid((uint32_t)tiles), block((uint32_t)p.threads), by_group((uint32_t)groups);
   const size_t channels = (size_t)p.units * V, sums = 2 * (size_t)slots_of(p.threads, p.log) * channels;
   if (!backward) {
     const size_t lds = (sums + 2 * (size_t)p.segs) * sizeof(float);
     if (p.whole) {
-      hipLaunchKernelGGL((gn_tile_kernel<T, V, true>), grid, block, lds, stream, a);
+      hipLaunchKernelGGL((gn_tile_kernel<T, V, ACT, true>), grid, block, lds, stream, a);
       return check_launch();
     }
-    hipLaunchKernelGGL((gn_tile_kernel<T, V, false>), grid, block, lds, stream, a);
+    hipLaunchKernelGGL((gn_tile_kernel<T, V, DPSGD_ACT_NONE, false>), grid, block, lds, stream, a);
     GnArgs f = a;
     f.units = p.units * V;   // channels of a block
     hipLaunchKernelGGL(gn_finish_kernel, by_group, dim3(kThreads), 0, stream, f);
-    hipLaunchKernelGGL((gn_apply_kernel<T, V>), grid, block, 0, stream, a);
+    hipLaunchKernelGGL((gn_apply_kernel<T, V, ACT>), grid, block, 0, stream, a);
     return check_launch();
   }
   const size_t lds = (sums + 2 * channels + 2 * (size_t)p.segs) * sizeof(float);
   if (p.whole) {
-    hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, true>), grid, block, lds, stream, a);
+    hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, ACT, true>), grid, block, lds, stream, a);
     return check_launch();
   }
-  hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, false>), grid, block, lds, stream, a);
+  hipLaunchKernelGGL((gn_grad_tile_kernel<T, V, ACT, false>), grid, block, lds, stream, a);
   hipLaunchKernelGGL(gn_grad_finish_kernel, by_group, dim3(kThreads), 0, stream, a);
-  hipLaunchKernelGGL((gn_grad_apply_kernel<T, V>), grid, block, 0, stream, a);
+  hipLaunchKernelGGL((gn_grad_apply_kernel<T, V, ACT>), grid, block, 0, stream, a);
   return check_launch();
+}
+
+template <class T, int V>
+int run_act(const dpsgd_group_norm& n, const GnPlan& p, bool backward, const GnArgs& a,
+            hipStream_t stream) {
+  switch (n.act) {
+    case DPSGD_ACT_RELU: return run<T, V, DPSGD_ACT_RELU>(n, p, backward, a, stream);
+    case DPSGD_ACT_SILU: return run<T, V, DPSGD_ACT_SILU>(n, p, backward, a, stream);
+    case DPSGD_ACT_GELU: return run<T, V, DPSGD_ACT_GELU>(n, p, backward, a, stream);
+    default: return run<T, V, DPSGD_ACT_NONE>(n, p, backward, a, stream);
+  }
 }
 
 int run_group_norm(const dpsgd_group_norm& n, const GnPlan& p, bool backward, const GnArgs& a,
                    hipStream_t stream) {
   if (n.dtype == DPSGD_BF16) {
     switch (p.vec) {
-      case 4: return run<uint16_t, 4>(n, p, backward, a, stream);
-      case 2: return run<uint16_t, 2>(n, p, backward, a, stream);
-      default: return run<uint16_t, 1>(n, p, backward, a, stream);
+      case 4: return run_act<uint16_t, 4>(n, p, backward, a, stream);
+      case 2: return run_act<uint16_t, 2>(n, p, backward, a, stream);
+      default: return run_act<uint16_t, 1>(n, p, backward, a, stream);
     }
   }
   switch (p.vec) {
-    case 4: return run<float, 4>(n, p, backward, a, stream);
-    case 2: return run<float, 2>(n, p, backward, a, stream);
-    default: return run<float, 1>(n, p, backward, a, stream);
+    case 4: return run_act<float, 4>(n, p, backward, a, stream);
+    case 2: return run_act<float, 2>(n, p, backward, a, stream);
+    default: return run_act<float, 1>(n, p, backward, a, stream);
   }
 }
 

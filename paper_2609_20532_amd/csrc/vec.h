@@ -110,8 +110,8 @@ struct Raw {
     for (uint32_t& x : w) x = 0;
   }
 
-  // Keeps the compiler from holding on to values that were widened before: later
-  // uses widen again, from half the registers.
+  // Keeps the compiler from holding on to what was formed from these elements
+  // before: later uses form it again, and only the elements stay in registers.
   __device__ __forceinline__ void keep_raw() {
     if constexpr (sizeof(T) == 2) {
 #pragma unroll
