@@ -14,8 +14,9 @@
 namespace dpsgd {
 namespace {
 
-constexpr int kBlock = 4096;        // entries that a workgroup takes at a time
-constexpr int kNormWgs = 1024;      // most workgroups (partial sums) of a launch
+constexpr int kBlock = 8192;        // entries that a workgroup takes at a time
+constexpr int kNormWgs = 2048;      // most workgroups (partial sums) of a launch
+constexpr int kPerThread = kBlock / (4 * kThreads);
 
 struct Tensor {
   const float* in;
@@ -27,8 +28,12 @@ struct Tensor {
 struct ClipArgs {
   Tensor t[kMaxLayersPerLaunch];
   int64_t blocks;
-  double* partials;     // of this launch
-  const float* factor;
+  double* partials;      // of this launch
+  const double* all;     // scale: the partial sums of every launch, and their number
+  int64_t n_all;
+  float* norm_out;
+  float* factor_out;
+  float max_norm;
   int32_t n;
 };
 
@@ -47,66 +52,96 @@ __device__ __forceinline__ double wave_sum_f64(double v) {
   return v;
 }
 
-__global__ __launch_bounds__(kThreads) void sum_squares_kernel(ClipArgs a) {
+// Sum over the workgroup, in every thread.
+__device__ __forceinline__ double block_sum_f64(double v) {
   __shared__ double red[kThreads / 64];
-  double s = 0.0;
-  for (int64_t b = blockIdx.x; b < a.blocks; b += gridDim.x) {
-    const Tensor& t = tensor_of(a, b);
-    const int64_t e0 = (b - t.begin) * kBlock;
-    for (int k = 0; k < kBlock / (4 * kThreads); ++k) {
-      const int64_t e = e0 + (k * kThreads + (int)threadIdx.x) * 4;
-      if (e + 4 <= t.numel) {
-        float x[4];
-        load_vec<4>(t.in + e, x);
-#pragma unroll
-        for (int c = 0; c < 4; ++c) s = fma((double)x[c], (double)x[c], s);
-      } else {
-        for (int64_t q = e; q < t.numel; ++q) s = fma((double)t.in[q], (double)t.in[q], s);
-      }
-    }
-  }
-  s = wave_sum_f64(s);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
+  v = wave_sum_f64(v);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
   __syncthreads();
-  if (threadIdx.x == 0) a.partials[blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+  return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// The norm and the factor from all partial sums.
-__global__ __launch_bounds__(kThreads) void norm_finish_kernel(const double* partials, int64_t n,
-                                                               float max_norm, float* norm_out,
-                                                               float* factor, float* factor_out) {
-  __shared__ double red[kThreads / 64];
+__global__ __launch_bounds__(kThreads) void sum_squares_kernel(ClipArgs a) {
   double s = 0.0;
-  for (int64_t k = threadIdx.x; k < n; k += kThreads) s += partials[k];
-  s = wave_sum_f64(s);
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  const double norm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
-  if (norm_out) *norm_out = (float)norm;
-  const float c = norm > (double)max_norm ? (float)((double)max_norm / norm)
-                                          : (norm == norm ? 1.0f : (float)norm);
-  if (factor) *factor = c;
-  if (factor_out) *factor_out = c;
+  int64_t b = blockIdx.x;
+  Tensor t = tensor_of(a, b);   // a workgroup's first block is there
+  while (true) {
+    const int64_t first = (b - t.begin) * kBlock, e0 = first + (int64_t)threadIdx.x * 4;
+    float x[kPerThread][4];
+    if (first + kBlock <= t.numel) {
+#pragma unroll
+      for (int k = 0; k < kPerThread; ++k) load_vec<4>(t.in + e0 + k * 4 * kThreads, x[k]);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kPerThread; ++k)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const int64_t e = e0 + k * 4 * kThreads + c;
+          x[k][c] = e < t.numel ? t.in[e] : 0.0f;
+        }
+    }
+    b += gridDim.x;
+    const bool more = b < a.blocks;
+    if (more) t = tensor_of(a, b);   // while the loads are in flight
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s = fma((double)x[k][c], (double)x[k][c], s);
+    if (!more) break;
+  }
+  s = block_sum_f64(s);
+  if (threadIdx.x == 0) a.partials[blockIdx.x] = s;
+}
+
+// The norm from the partial sums of every launch: each workgroup adds them for
+// itself, in the same order.
+__device__ __forceinline__ double norm_of(const ClipArgs& a) {
+  double s = 0.0;
+#pragma unroll 8
+  for (int64_t k = threadIdx.x; k < a.n_all; k += kThreads) s += a.all[k];
+  return sqrt(block_sum_f64(s));
+}
+
+__global__ __launch_bounds__(kThreads) void norm_kernel(ClipArgs a) {
+  const double norm = norm_of(a);
+  if (threadIdx.x == 0) *a.norm_out = (float)norm;
 }
 
 __global__ __launch_bounds__(kThreads) void scale_kernel(ClipArgs a) {
-  const float c = *a.factor;
-  const int64_t b = blockIdx.x;
+  // Last blocks first: they are the ones that the norm's pass has left in the
+  // last-level cache.
+  const int64_t b = a.blocks - 1 - blockIdx.x;
   const Tensor& t = tensor_of(a, b);
-  const int64_t e0 = (b - t.begin) * kBlock;
-  for (int k = 0; k < kBlock / (4 * kThreads); ++k) {
-    const int64_t e = e0 + (k * kThreads + (int)threadIdx.x) * 4;
-    if (e + 4 <= t.numel) {
-      float x[4];
-      load_vec<4>(t.in + e, x);
+  const int64_t e0 = (b - t.begin) * kBlock + (int64_t)threadIdx.x * 4;
+  const bool whole = e0 - (int64_t)threadIdx.x * 4 + kBlock <= t.numel;
+  float x[kPerThread][4];
+  if (whole) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] *= c;
-      store_vec<4>(t.out + e, x);
-    } else {
-      for (int64_t q = e; q < t.numel; ++q) t.out[q] = t.in[q] * c;
-    }
+    for (int k = 0; k < kPerThread; ++k) load_vec<4>(t.in + e0 + k * 4 * kThreads, x[k]);
   }
+  const double norm = norm_of(a);
+  const float c = norm > (double)a.max_norm ? (float)((double)a.max_norm / norm)
+                                            : (norm == norm ? 1.0f : (float)norm);
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (a.norm_out) *a.norm_out = (float)norm;
+    if (a.factor_out) *a.factor_out = c;
+  }
+  if (whole) {
+#pragma unroll
+    for (int k = 0; k < kPerThread; ++k) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[k][j] *= c;
+      // Not kept in the caches, which hold what is still to be read.
+      __builtin_nontemporal_store(f32x4_t{x[k][0], x[k][1], x[k][2], x[k][3]},
+                                  reinterpret_cast<f32x4_t*>(t.out + e0 + k * 4 * kThreads));
+    }
+    return;
+  }
+  for (int k = 0; k < kPerThread; ++k)
+    for (int j = 0; j < 4; ++j) {
+      const int64_t e = e0 + k * 4 * kThreads + j;
+      if (e < t.numel) t.out[e] = t.in[e] * c;
+    }
 }
 
 // The launch over the tensors [base, base + n).
@@ -121,25 +156,26 @@ ClipArgs args_of(const dpsgd_layer* layers, int32_t n, const float* const* in, f
   return a;
 }
 
-int64_t norm_wgs(const ClipArgs& a) { return a.blocks < kNormWgs ? a.blocks : kNormWgs; }
+// Workgroups of the norm's pass: as few blocks each as kNormWgs allow, and the
+// same number for nearly all.
+int64_t norm_wgs(const ClipArgs& a) { return ceil_div(a.blocks, ceil_div(a.blocks, kNormWgs)); }
 
 }  // namespace
 
-// Workspace: the factor, then one float64 partial sum per workgroup.
+// Workspace: one float64 partial sum per workgroup.
 size_t global_norm_workspace_bytes(const dpsgd_layer* layers, int32_t n) {
   int64_t partials = 0;
   for (int32_t base = 0; base < n; base += kMaxLayersPerLaunch) {
     const int32_t m = n - base < kMaxLayersPerLaunch ? n - base : kMaxLayersPerLaunch;
     partials += norm_wgs(args_of(layers + base, m, nullptr, nullptr));
   }
-  return 256 + (size_t)partials * sizeof(double);
+  return (size_t)partials * sizeof(double);
 }
 
 int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const* grads,
                        float* const* outs, float max_norm, float* norm_out, float* factor_out,
                        void* workspace, hipStream_t stream) {
-  float* factor = static_cast<float*>(workspace);
-  double* partials = reinterpret_cast<double*>(static_cast<char*>(workspace) + 256);
+  double* partials = static_cast<double*>(workspace);
   int64_t at = 0;
   for (int32_t base = 0; base < n; base += kMaxLayersPerLaunch) {
     const int32_t m = n - base < kMaxLayersPerLaunch ? n - base : kMaxLayersPerLaunch;
@@ -149,13 +185,26 @@ int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const*
     hipLaunchKernelGGL(sum_squares_kernel, dim3((uint32_t)norm_wgs(a)), dim3(kThreads), 0, stream, a);
     at += norm_wgs(a);
   }
-  hipLaunchKernelGGL(norm_finish_kernel, dim3(1), dim3(kThreads), 0, stream, partials, at, max_norm,
-                     norm_out, factor, factor_out);
-  if (!outs) return check_launch();
-  for (int32_t base = 0; base < n; base += kMaxLayersPerLaunch) {
+  if (!outs) {
+    ClipArgs a{};
+    a.all = partials;
+    a.n_all = at;
+    a.norm_out = norm_out;
+    hipLaunchKernelGGL(norm_kernel, dim3(1), dim3(kThreads), 0, stream, a);
+    return check_launch();
+  }
+  // Launches in reverse, for the same reason as the blocks of one.
+  const int32_t last = (n - 1) / kMaxLayersPerLaunch * kMaxLayersPerLaunch;
+  for (int32_t base = last; base >= 0; base -= kMaxLayersPerLaunch) {
     const int32_t m = n - base < kMaxLayersPerLaunch ? n - base : kMaxLayersPerLaunch;
     ClipArgs a = args_of(layers + base, m, grads + base, outs + base);
-    a.factor = factor;
+    a.all = partials;
+    a.n_all = at;
+    a.max_norm = max_norm;
+    if (base == last) {
+      a.norm_out = norm_out;
+      a.factor_out = factor_out;
+    }
     hipLaunchKernelGGL(scale_kernel, dim3((uint32_t)a.blocks), dim3(kThreads), 0, stream, a);
   }
   return check_launch();
