@@ -42,7 +42,6 @@ struct ClipArgs {
   float* factor_out;
   float max_norm;
   int32_t n;
-  int32_t past_caches;   // outputs are not kept in the caches
 };
 
 __device__ __forceinline__ const Tensor& tensor_of(const ClipArgs& a, int64_t block) {
@@ -115,6 +114,8 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(ClipArgs a) {
   if (threadIdx.x == 0) *a.norm_out = (float)norm;
 }
 
+// PAST_CACHES: the outputs are not kept in the caches.
+template <bool PAST_CACHES>
 __global__ __launch_bounds__(kThreads) void scale_kernel(ClipArgs a) {
   // Last blocks first: they are the ones that the norm's pass has left in the
   // last-level cache.
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(ClipArgs a) {
       for (int j = 0; j < 4; ++j) x[k][j] *= c;
       const f32x4_t y{x[k][0], x[k][1], x[k][2], x[k][3]};
       f32x4_t* to = reinterpret_cast<f32x4_t*>(t.out + e0 + k * 4 * kThreads);
-      if (a.past_caches) __builtin_nontemporal_store(y, to);
+      if constexpr (PAST_CACHES) __builtin_nontemporal_store(y, to);
       else *to = y;
     }
     return;
@@ -213,12 +214,15 @@ int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const*
     a.all = partials;
     a.n_all = at;
     a.max_norm = max_norm;
-    a.past_caches = apart >= kPastCaches;
     if (base == last) {
       a.norm_out = norm_out;
       a.factor_out = factor_out;
     }
-    hipLaunchKernelGGL(scale_kernel, dim3((uint32_t)a.blocks), dim3(kThreads), 0, stream, a);
+    const dim3 grid((uint32_t)a.blocks);
+    if (apart >= kPastCaches)
+      hipLaunchKernelGGL(scale_kernel<true>, grid, dim3(kThreads), 0, stream, a);
+    else
+      hipLaunchKernelGGL(scale_kernel<false>, grid, dim3(kThreads), 0, stream, a);
   }
   return check_launch();
 }

@@ -187,13 +187,19 @@ def _check(fn: str, status: int):
         raise DpsgdError(fn, status, _lib.dpsgd_status_string(status).decode())
 
 
+_raw_stream = None   # torch's (current device, raw handle of its current stream), once CUDA is initialised
+
+
 def _stream(stream):
-    import torch
+    global _raw_stream
     if stream is None:
         # The handle alone: building a torch.cuda.Stream object takes about 3 us
         # a call, a third of a small call's host time.
+        if _raw_stream is not None:
+            return _raw_stream[1](_raw_stream[0]())
+        import torch
         if torch.cuda.is_initialized():
-            return ctypes.c_void_p(torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()))
+            _raw_stream = (torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream)
         stream = torch.cuda.current_stream()
     return ctypes.c_void_p(stream.cuda_stream)
 
@@ -400,86 +406,97 @@ def dpsgd_gaussian(out, n, seed, tensor_id, step, stream=None):
 # ----------------------------------------- around the linear layers
 
 
+_codes = {}   # dpsgd_dtype of a torch dtype, names of the other types that arguments may have
+
+
+def _types():
+    if not _codes:
+        import torch
+        _codes.update({torch.float32: DPSGD_F32, torch.bfloat16: DPSGD_BF16, torch.int32: "i32",
+                       torch.int64: "i64", torch.uint8: "u8", "f32": torch.float32})
+    return _codes
+
+
 def _dtype_of(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return DPSGD_F32
-    if t.dtype == torch.bfloat16:
-        return DPSGD_BF16
+    code = _types().get(t.dtype)
+    if code is DPSGD_F32 or code is DPSGD_BF16:
+        return code
     raise ValueError(f"float32 or bfloat16 expected, not {t.dtype}")
 
 
-def _want(name, t, shape, dtype=None):
-    """Raises ValueError unless t is a contiguous device tensor of this shape (and dtype)."""
+def _want(name, t, shape, code=None):
+    """The address of t; raises ValueError unless it is a contiguous device tensor of
+    this shape (and of the type with this code)."""
     if not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous device tensor")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
-    if dtype is not None and t.dtype != dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if code is not None and _types().get(t.dtype) != code:
+        raise ValueError(f"{name} must not be {t.dtype}")
+    return t.data_ptr()
+
+
+def _may_want(name, t, shape, code):
+    return None if t is None else _want(name, t, shape, code)
 
 
 def _workspace(workspace):
-    return _ptr(workspace), 0 if workspace is None else workspace.numel() * workspace.element_size()
+    if workspace is None:
+        return None, 0
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
 def make_embedding(ids, table_shape, scale: float = 1.0) -> dpsgd_embedding:
     """Descriptor of a table [n_rows, d] and the ids [B, T] (int32 or int64, on the
     device) that look into it. An id outside the table is an empty position. The
     descriptor keeps ids alive."""
-    import torch
-    if ids.dim() != 2 or ids.dtype not in (torch.int32, torch.int64):
+    code = _types().get(ids.dtype)
+    if ids.dim() != 2 or (code != "i32" and code != "i64"):
         raise ValueError("ids must be [B, T], int32 or int64")
     if not ids.is_cuda or not ids.is_contiguous():
         raise ValueError("ids must be a contiguous device tensor")
+    B, T = ids.shape
     n_rows, d = table_shape
-    emb = dpsgd_embedding(ids.data_ptr(), ids.shape[0], ids.shape[1], n_rows, d,
-                          DPSGD_I64 if ids.dtype == torch.int64 else DPSGD_I32, scale)
+    emb = dpsgd_embedding(ids.data_ptr(), B, T, n_rows, d,
+                          DPSGD_I64 if code == "i64" else DPSGD_I32, scale)
     emb.keep = ids
     return emb
 
 
 def dpsgd_embedding_lookup(emb: dpsgd_embedding, table, out, stream=None):
-    load()
-    _want("table", table, (emb.n_rows, emb.d))
-    _want("out", out, (emb.B, emb.T, emb.d))
-    st = _lib.dpsgd_embedding_lookup(ctypes.byref(emb), _ptr(table), _dtype_of(table), _ptr(out),
-                                     _dtype_of(out), _stream(stream))
+    lib = _lib or load()
+    st = lib.dpsgd_embedding_lookup(
+        emb, _want("table", table, (emb.n_rows, emb.d)), _dtype_of(table),
+        _want("out", out, (emb.B, emb.T, emb.d)), _dtype_of(out), _stream(stream))
     _check("dpsgd_embedding_lookup", st)
 
 
 def dpsgd_embedding_workspace_bytes(emb: dpsgd_embedding) -> int:
-    load()
-    return int(_lib.dpsgd_embedding_workspace_bytes(ctypes.byref(emb)))
+    return int((_lib or load()).dpsgd_embedding_workspace_bytes(emb))
 
 
 def dpsgd_embedding_norms(emb: dpsgd_embedding, G, norms_sq, accumulate=False, workspace=None,
                           stream=None):
-    import torch
-    load()
-    _want("G", G, (emb.B, emb.T, emb.d))
-    _want("norms_sq", norms_sq, (emb.B,), torch.float32)
-    st = _lib.dpsgd_embedding_norms(ctypes.byref(emb), _ptr(G), _dtype_of(G), _ptr(norms_sq),
-                                    int(accumulate), *_workspace(workspace), _stream(stream))
+    lib = _lib or load()
+    B = emb.B
+    st = lib.dpsgd_embedding_norms(
+        emb, _want("G", G, (B, emb.T, emb.d)), _dtype_of(G),
+        _want("norms_sq", norms_sq, (B,), DPSGD_F32), int(accumulate), *_workspace(workspace),
+        _stream(stream))
     _check("dpsgd_embedding_norms", st)
 
 
 def dpsgd_embedding_clip_accumulate(emb: dpsgd_embedding, G, norms_sq, C, grad, accumulate=False,
                                     factors_out=None, mask_out=None, workspace=None, stream=None):
     """norms_sq None: the plain sum over the batch (C is not looked at)."""
-    import torch
-    load()
-    _want("G", G, (emb.B, emb.T, emb.d))
-    _want("grad", grad, (emb.n_rows, emb.d), torch.float32)
-    if norms_sq is not None:
-        _want("norms_sq", norms_sq, (emb.B,), torch.float32)
-    if factors_out is not None:
-        _want("factors_out", factors_out, (emb.B,), torch.float32)
-    if mask_out is not None:
-        _want("mask_out", mask_out, (emb.B,), torch.uint8)
-    st = _lib.dpsgd_embedding_clip_accumulate(
-        ctypes.byref(emb), _ptr(G), _dtype_of(G), _ptr(norms_sq), C, _ptr(grad), int(accumulate),
-        _ptr(factors_out), _ptr(mask_out), *_workspace(workspace), _stream(stream))
+    lib = _lib or load()
+    B, d = emb.B, emb.d
+    st = lib.dpsgd_embedding_clip_accumulate(
+        emb, _want("G", G, (B, emb.T, d)), _dtype_of(G),
+        _may_want("norms_sq", norms_sq, (B,), DPSGD_F32), C,
+        _want("grad", grad, (emb.n_rows, d), DPSGD_F32), int(accumulate),
+        _may_want("factors_out", factors_out, (B,), DPSGD_F32),
+        _may_want("mask_out", mask_out, (B,), "u8"), *_workspace(workspace), _stream(stream))
     _check("dpsgd_embedding_clip_accumulate", st)
 
 
@@ -489,64 +506,60 @@ def make_group_norm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
     between the first and the last is a position: [B, S, C], [B, H, W, C]; a
     channels_last tensor [B, C, H, W] is x.permute(0, 2, 3, 1)). act: a name of
     ACTIVATIONS. The descriptor keeps gamma and beta alive."""
-    import torch
-    if x.dim() < 2 or x.numel() == 0:
+    shape, n = x.shape, x.numel()
+    if len(shape) < 2 or n == 0:
         raise ValueError("x must be [B, ..., C] with no empty axis")
     if act not in ACTIVATIONS:
         raise ValueError(f"act must be one of {sorted(ACTIVATIONS)}")
-    B, C = x.shape[0], x.shape[-1]
-    for name, t in (("gamma", gamma), ("beta", beta)):
-        if t is not None:
-            _want(name, t, (C,), torch.float32)
-    gn = dpsgd_group_norm(B, x.numel() // (B * C), C, groups,
-                          None if gamma is None else gamma.data_ptr(),
-                          None if beta is None else beta.data_ptr(), _dtype_of(x),
+    B, C = shape[0], shape[-1]
+    gn = dpsgd_group_norm(B, n // (B * C), C, groups, _may_want("gamma", gamma, (C,), DPSGD_F32),
+                          _may_want("beta", beta, (C,), DPSGD_F32), _dtype_of(x),
                           ACTIVATIONS[act], eps)
     gn.keep = (gamma, beta)
     return gn
 
 
-def _want_rows(name, t, gn: dpsgd_group_norm):
-    _want(name, t, t.shape)
-    if t.shape[0] != gn.B or t.shape[-1] != gn.C or t.numel() != gn.B * gn.S * gn.C:
-        raise ValueError(f"{name} must be [{gn.B}, ({gn.S} positions), {gn.C}], not {list(t.shape)}")
-    if _dtype_of(t) != gn.dtype:
+def _want_rows(name, t, B, C, n, dtype):
+    """The address of t, a contiguous device tensor [B, ..., C] of n entries."""
+    if not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous device tensor")
+    shape = t.shape
+    if shape[0] != B or shape[-1] != C or t.numel() != n:
+        raise ValueError(f"{name} must be [{B}, ({n // (B * C)} positions), {C}], not {list(shape)}")
+    if _codes.get(t.dtype) != dtype:
         raise ValueError(f"{name} has another dtype than the descriptor")
+    return t.data_ptr()
 
 
 def dpsgd_group_norm_workspace_bytes(gn: dpsgd_group_norm) -> int:
-    load()
-    return int(_lib.dpsgd_group_norm_workspace_bytes(ctypes.byref(gn)))
+    return int((_lib or load()).dpsgd_group_norm_workspace_bytes(gn))
 
 
 def dpsgd_group_norm_forward(gn: dpsgd_group_norm, x, y, mean=None, rstd=None, workspace=None,
                              stream=None):
-    import torch
-    load()
-    _want_rows("x", x, gn)
-    _want_rows("y", y, gn)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        if t is not None:
-            _want(name, t, (gn.B, gn.groups), torch.float32)
-    st = _lib.dpsgd_group_norm_forward(ctypes.byref(gn), _ptr(x), _ptr(y), _ptr(mean), _ptr(rstd),
-                                       *_workspace(workspace), _stream(stream))
+    lib = _lib or load()
+    B, C, dt = gn.B, gn.C, gn.dtype
+    n, stat = B * gn.S * C, (B, gn.groups)
+    _types()
+    st = lib.dpsgd_group_norm_forward(
+        gn, _want_rows("x", x, B, C, n, dt), _want_rows("y", y, B, C, n, dt),
+        _may_want("mean", mean, stat, DPSGD_F32), _may_want("rstd", rstd, stat, DPSGD_F32),
+        *_workspace(workspace), _stream(stream))
     _check("dpsgd_group_norm_forward", st)
 
 
 def dpsgd_group_norm_backward(gn: dpsgd_group_norm, x, dy, mean, rstd, dx, dgamma, dbeta,
                               workspace=None, stream=None):
     """dgamma and dbeta are per example ([B, C]); affine_layer makes layers of them."""
-    import torch
-    load()
-    for name, t in (("x", x), ("dy", dy), ("dx", dx)):
-        _want_rows(name, t, gn)
-    for name, t in (("mean", mean), ("rstd", rstd)):
-        _want(name, t, (gn.B, gn.groups), torch.float32)
-    for name, t in (("dgamma", dgamma), ("dbeta", dbeta)):
-        _want(name, t, (gn.B, gn.C), torch.float32)
-    st = _lib.dpsgd_group_norm_backward(ctypes.byref(gn), _ptr(x), _ptr(dy), _ptr(mean),
-                                        _ptr(rstd), _ptr(dx), _ptr(dgamma), _ptr(dbeta),
-                                        *_workspace(workspace), _stream(stream))
+    lib = _lib or load()
+    B, C, dt = gn.B, gn.C, gn.dtype
+    n, stat, affine = B * gn.S * C, (B, gn.groups), (B, C)
+    _types()
+    st = lib.dpsgd_group_norm_backward(
+        gn, _want_rows("x", x, B, C, n, dt), _want_rows("dy", dy, B, C, n, dt),
+        _want("mean", mean, stat, DPSGD_F32), _want("rstd", rstd, stat, DPSGD_F32),
+        _want_rows("dx", dx, B, C, n, dt), _want("dgamma", dgamma, affine, DPSGD_F32),
+        _want("dbeta", dbeta, affine, DPSGD_F32), *_workspace(workspace), _stream(stream))
     _check("dpsgd_group_norm_backward", st)
 
 
@@ -559,50 +572,56 @@ def affine_layer(ones, grad, tensor_id: int) -> dpsgd_layer:
 
 
 def dpsgd_global_norm_workspace_bytes(layers) -> int:
-    load()
+    lib = _lib or load()
     arr, n = _array(layers)
-    return int(_lib.dpsgd_global_norm_workspace_bytes(arr, n))
+    return int(lib.dpsgd_global_norm_workspace_bytes(arr, n))
 
 
-def _want_gradients(name, tensors, layers):
-    import torch
-    if len(tensors) != len(layers):
-        raise ValueError(f"{name}: {len(layers)} tensors expected, not {len(tensors)}")
-    for t, L in zip(tensors, layers):
-        if (t.dtype != torch.float32 or not t.is_cuda or not t.is_contiguous()
-                or t.numel() != L.d_in * L.d_out):
+def _sizes(layers):
+    return [L.d_in * L.d_out for L in ([layers] if isinstance(layers, dpsgd_layer) else layers)]
+
+
+def _gradients(name, tensors, sizes):
+    """The addresses of contiguous float32 device tensors with these numbers of entries."""
+    if len(tensors) != len(sizes):
+        raise ValueError(f"{name}: {len(sizes)} tensors expected, not {len(tensors)}")
+    f32 = _types()["f32"]
+    arr = (ctypes.c_void_p * len(sizes))()
+    for k, (t, n) in enumerate(zip(tensors, sizes)):
+        if t.dtype is not f32 or not t.is_cuda or t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous float32 device tensors of d_out d_in entries")
+        arr[k] = t.data_ptr()
+    return arr
 
 
-def _want_scalar(name, t):
-    import torch
-    if t is not None and (t.dtype != torch.float32 or not t.is_cuda or t.numel() != 1):
+def _scalar(name, t):
+    if t is None:
+        return None
+    if _types().get(t.dtype) != DPSGD_F32 or not t.is_cuda or t.numel() != 1:
         raise ValueError(f"{name} must be one float32 value on the device")
+    return t.data_ptr()
 
 
 def dpsgd_global_norm_multi(layers, grads, norm_out, workspace=None, stream=None):
-    load()
-    _want_gradients("grads", grads, layers)
-    _want_scalar("norm_out", norm_out)
+    lib = _lib or load()
     arr, n = _array(layers)
-    st = _lib.dpsgd_global_norm_multi(arr, n, _ptr_array(grads), _ptr(norm_out),
-                                      *_workspace(workspace), _stream(stream))
+    st = lib.dpsgd_global_norm_multi(arr, n, _gradients("grads", grads, _sizes(layers)),
+                                     _scalar("norm_out", norm_out), *_workspace(workspace),
+                                     _stream(stream))
     _check("dpsgd_global_norm_multi", st)
 
 
 def dpsgd_global_clip_multi(layers, grads, outs, max_norm: float, norm_out=None, factor_out=None,
                             workspace=None, stream=None):
     """outs may be grads (in place)."""
-    load()
-    _want_gradients("grads", grads, layers)
-    if outs is not grads:
-        _want_gradients("outs", outs, layers)
-    _want_scalar("norm_out", norm_out)
-    _want_scalar("factor_out", factor_out)
+    lib = _lib or load()
     arr, n = _array(layers)
-    st = _lib.dpsgd_global_clip_multi(arr, n, _ptr_array(grads), _ptr_array(outs), max_norm,
-                                      _ptr(norm_out), _ptr(factor_out), *_workspace(workspace),
-                                      _stream(stream))
+    sizes = _sizes(layers)
+    g = _gradients("grads", grads, sizes)
+    o = g if outs is grads else _gradients("outs", outs, sizes)
+    st = lib.dpsgd_global_clip_multi(arr, n, g, o, max_norm, _scalar("norm_out", norm_out),
+                                     _scalar("factor_out", factor_out), *_workspace(workspace),
+                                     _stream(stream))
     _check("dpsgd_global_clip_multi", st)
 
 
