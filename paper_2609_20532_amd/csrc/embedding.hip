@@ -110,9 +110,21 @@ struct ExampleKey {   // key of entry k of a list of positions: its example
 // range again). Key by key counts of those and a prefix over keys and waves
 // give every wave its places. No entry's place depends on the order of an
 // atomic (the counts are integers).
+//
+// The sort is bound by its instructions and leaves the memory idle: workgroups
+// after the buckets' may fill `zeros` with zeros meanwhile.
 template <class Key>
 __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk, int32_t* order,
-                                                            int32_t* offsets) {
+                                                            int32_t* offsets, float* zeros,
+                                                            int64_t n_zeros) {
+  if (blockIdx.x >> bk.log) {
+    const int64_t step = (int64_t)(gridDim.x - (1u << bk.log)) * kSortThreads;
+    const int64_t first = (int64_t)(blockIdx.x - (1u << bk.log)) * kSortThreads + threadIdx.x;
+    for (int64_t k = first; k < n_zeros >> 2; k += step)
+      reinterpret_cast<f32x4_t*>(zeros)[k] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    if (first < (n_zeros & 3)) zeros[(n_zeros & ~INT64_C(3)) + first] = 0.0f;
+    return;
+  }
   extern __shared__ __align__(16) int32_t lds[];
   __shared__ uint2 kept_of[kSortWaves][kSortList];   // value, key within the bucket
   __shared__ int32_t less_of[kSortWaves];
@@ -234,10 +246,12 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk
 
 template <class Key>
 int launch_sort(const Key& keys, const Buckets& bk, int32_t* order, int32_t* offsets,
-                hipStream_t stream) {
+                hipStream_t stream, float* zeros = nullptr, int64_t n_zeros = 0) {
   const size_t lds = (size_t)(kSortWaves + 1) * bk.R * sizeof(int32_t);
-  hipLaunchKernelGGL(sort_kernel<Key>, dim3(1u << bk.log), dim3(kSortThreads), lds, stream, keys, bk,
-                     order, offsets);
+  const int64_t fill = ceil_div(n_zeros, 16 * kSortThreads);   // 64 bytes a thread, at most a round
+  const uint32_t wgs = (1u << bk.log) + (uint32_t)(fill < kSortBuckets ? fill : kSortBuckets);
+  hipLaunchKernelGGL(sort_kernel<Key>, dim3(wgs), dim3(kSortThreads), lds, stream, keys, bk, order,
+                     offsets, zeros, n_zeros);
   return check_launch();
 }
 
@@ -618,7 +632,7 @@ struct SumArgs {
   float* factors_out;
   uint8_t* mask_out;
   Buckets tokens;
-  int64_t V, B;
+  int64_t rows, B;   // rows that this launch fills where they have no token
   // Workgroups of the chunks, then of the empty rows, then of the factors.
   uint32_t chunk_wgs, row_wgs;
   int32_t chunks, blocks;   // chunks of the sorted list, column blocks of a row
@@ -725,7 +739,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(SumArgs a) {
   // Rows without a token.
   const int64_t v0 = ((int64_t)wg * (kThreads / 64) + wave) * kRowsPerWave;
   bool empty = false;
-  if (lane < kRowsPerWave && v0 + lane < a.V) {
+  if (lane < kRowsPerWave && v0 + lane < a.rows) {
     const uint32_t slot = a.tokens.slot((uint32_t)(v0 + lane));
     empty = a.offsets[slot] == a.offsets[slot + 1];
   }
@@ -812,12 +826,12 @@ size_t list_bytes(int64_t N, const Buckets& b) {
 }
 
 int sort_tokens(const dpsgd_embedding& e, const Buckets& b, int32_t* order, int32_t* offsets,
-                hipStream_t stream) {
+                hipStream_t stream, float* zeros = nullptr, int64_t n_zeros = 0) {
   if (e.index_dtype == DPSGD_I64)
     return launch_sort(TokenKey<int64_t>{static_cast<const int64_t*>(e.ids), (int32_t)(e.B * e.T)}, b, order, offsets,
-                       stream);
+                       stream, zeros, n_zeros);
   return launch_sort(TokenKey<int32_t>{static_cast<const int32_t*>(e.ids), (int32_t)(e.B * e.T)}, b, order, offsets,
-                     stream);
+                     stream, zeros, n_zeros);
 }
 
 template <class T, int V>
@@ -930,7 +944,16 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
   a.tokens = buckets_of(e.n_rows);
   int32_t* order = reinterpret_cast<int32_t*>(ws);
   int32_t* offsets = reinterpret_cast<int32_t*>(ws + order_bytes(N));
-  const int st = sort_tokens(e, a.tokens, order, offsets, stream);
+  // Rows from `filled` on are zeroed beside the sort, about as many as the memory
+  // takes meanwhile (at 6 TB/s; the sort takes 5 us and 0.3 ns an entry), and
+  // those with a token are written again. They are the last ones, as frequent
+  // words have small ids. (50257 x 768, 32768 tokens: norms and sum 68.7 us, 73.7
+  // with every empty row filled by the sum.)
+  const int64_t fill_rows = accumulate ? 0 : ((INT64_C(30) << 20) + 1800 * N) / (e.d * (int64_t)sizeof(float));
+  const int64_t filled = fill_rows < e.n_rows ? round_up((size_t)(e.n_rows - fill_rows), 4) : 0;
+  const bool fill = !accumulate && filled < e.n_rows;
+  const int st = sort_tokens(e, a.tokens, order, offsets, stream, fill ? grad + filled * e.d : nullptr,
+                             fill ? (e.n_rows - filled) * e.d : 0);
   if (st != DPSGD_OK) return st;
   a.ids = e.ids;
   a.G = G;
@@ -941,7 +964,7 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
   a.partials = reinterpret_cast<float*>(ws + list_bytes(N, a.tokens));
   a.factors_out = factors_out;
   a.mask_out = mask_out;
-  a.V = e.n_rows;
+  a.rows = accumulate ? 0 : fill ? filled : e.n_rows;
   a.B = e.B;
   a.d = (int32_t)e.d;
   a.accumulate = accumulate;
@@ -953,7 +976,7 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
   a.chunks = (int32_t)chunk_count(N);
   a.blocks = (int32_t)ceil_div(e.d, 64 * vec);
   const int64_t chunk_wgs = ceil_div((int64_t)a.chunks * a.blocks, kThreads / 64);
-  const int64_t row_wgs = accumulate ? 0 : ceil_div(a.V, kThreads / 64 * kRowsPerWave);
+  const int64_t row_wgs = ceil_div(a.rows, kThreads / 64 * kRowsPerWave);
   const int64_t wgs = chunk_wgs + row_wgs + (factors_out || mask_out ? ceil_div(e.B, kThreads) : 0);
   if (wgs > 0x1FFFFFFF) return DPSGD_ERR_INVALID_ARG;   // jobs stay below 2^31
   a.chunk_wgs = (uint32_t)chunk_wgs;
