@@ -299,19 +299,23 @@ __global__ __launch_bounds__(kTile, 8) void gn_tile_kernel(GnArgs a) {
 
   if constexpr (WHOLE) {
     __syncthreads();
-    if (!p.active) return;
+    // The thread's place once more, so that no register holds it until here.
+    int32_t tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int32_t r = tid >> a.log, unit = tid & (a.lanes - 1), ch = p.c0 + unit * V;
+    if (unit >= a.units || ch >= a.C) return;
     float ga[V], be[V];
 #pragma unroll
     for (int c = 0; c < V; ++c) {
-      const int32_t s = (int32_t)magic_divide((uint32_t)(p.c + c), a.magic, a.shift) - p.first;
+      const int32_t s = (int32_t)magic_divide((uint32_t)(ch + c), a.magic, a.shift) - p.first;
       mu[c] = seg_mean[s];
-      ga[c] = a.gamma ? seg_rstd[s] * a.gamma[p.c + c] : seg_rstd[s];
-      be[c] = a.beta ? a.beta[p.c + c] : 0.0f;
+      ga[c] = a.gamma ? seg_rstd[s] * a.gamma[ch + c] : seg_rstd[s];
+      be[c] = a.beta ? a.beta[ch + c] : 0.0f;
     }
-    T* y = static_cast<T*>(a.out) + at;
+    T* y = static_cast<T*>(a.out) + ((int64_t)p.b * a.S + r) * a.C + ch;
 #pragma unroll
     for (int k = 0; k < kTileRows<T>; ++k) {
-      if (p.r + k * p.step < n_rows) {
+      if (r + k * p.step < n_rows) {
         float f[V];
         raw[k].keep_raw();
         raw[k].widen(f);
