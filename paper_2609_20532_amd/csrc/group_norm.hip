@@ -411,17 +411,6 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
   const T* dy = static_cast<const T*>(a.dy) + at;
   const int32_t n_rows = p.r1 - p.r0;
 
-  Raw<T, V> rx[kGradRows], rd[kGradRows];
-#pragma unroll
-  for (int k = 0; k < kGradRows; ++k) {
-    rx[k].zero();
-    rd[k].zero();
-    const int32_t r = p.r + k * p.step;
-    if (p.active && r < n_rows) {
-      rx[k].load(x + k * stride);
-      rd[k].load(dy + k * stride);
-    }
-  }
   float rs[V], mu[V], ga[V], be[V];
 #pragma unroll
   for (int c = 0; c < V; ++c) {
@@ -433,6 +422,17 @@ __global__ __launch_bounds__(kTile) void gn_grad_tile_kernel(GnArgs a) {
       mu[c] = a.mean[g];
       if (a.gamma) ga[c] = a.gamma[p.c + c];
       if (a.beta) be[c] = a.beta[p.c + c];
+    }
+  }
+  Raw<T, V> rx[kGradRows], rd[kGradRows];
+#pragma unroll
+  for (int k = 0; k < kGradRows; ++k) {
+    rx[k].zero();
+    rd[k].zero();
+    const int32_t r = p.r + k * p.step;
+    if (p.active && r < n_rows) {
+      rx[k].load(x + k * stride);
+      rd[k].load(dy + k * stride);
     }
   }
   float sb[V] = {}, sg[V] = {};

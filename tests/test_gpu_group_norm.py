@@ -147,6 +147,13 @@ def test_forward_and_backward(dp, B, S, C, groups, act, dtype):
     _check(x, dy, gamma, beta, groups, 1e-5, act, dtype, got)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,S,C,groups", [(520, 8200, 1, 1), (260, 4200, 12, 3)])
+def test_tiles_of_several_batches_of_rows(dp, B, S, C, groups, dtype):
+    x, dy, gamma, beta = _values(B, S, C, dtype, seed=3)
+    _check(x, dy, gamma, beta, groups, 1e-5, "silu", dtype, _run(dp, x, dy, gamma, beta, groups, 1e-5, "silu"))
+
+
 @pytest.mark.parametrize("affine", ["none", "gamma", "beta"])
 def test_without_affine_parameters(dp, affine):
     x, dy, gamma, beta = _values(3, 50, 24, "f32", seed=1)
