@@ -16,6 +16,12 @@
 // order; rows without a token are filled by waves of their own in the same
 // launch. For the norms every example's tokens are sorted in LDS, and equal
 // tokens, then neighbours, are added before they are squared.
+//
+// All of it is bound by memory traffic where it is large, by launches and the
+// sorts' latency where it is small. 128 x 256 tokens, a 50257 x 768 table, bf16 G
+// (50 MB): lookup (float32 to bf16) 17 us, 104 MB, 6.0 TB/s; norms 23 us;
+// sort and part of the zeros 19 us; sum 22 us; join 5 us: the two calls 69 us, where
+// reading G twice and writing the table once takes 42.
 #include <math.h>
 
 #include "vec.h"

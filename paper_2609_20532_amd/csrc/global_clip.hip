@@ -6,7 +6,10 @@
 // Bound by memory traffic: the tensors are read once for the norm and, since
 // the factor needs all of it, once more to be scaled. Squares are summed in
 // float64: the conversion and the fused multiply-add are far below the memory
-// time, no square overflows or vanishes, and the norm is rounded once.
+// time, no square overflows or vanishes, and the norm is rounded once. Every
+// workgroup of the second pass adds up the first one's partial sums itself: two
+// launches. 48 tensors of 340 MB: 57 us (6.0 TB/s) and 110 us (680 MB, 6.2 TB/s);
+// 24 tensors of 0.3 MB: 4.6 and 6.7 us.
 #include <math.h>
 
 #include "vec.h"
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(ClipArgs a) {
 template <bool PAST_CACHES>
 __global__ __launch_bounds__(kThreads) void scale_kernel(ClipArgs a) {
   // Last blocks first: they are the ones that the norm's pass has left in the
-  // last-level cache.
+  // last-level cache (340 MB: 110 us, 118 in plain order).
   const int64_t b = a.blocks - 1 - blockIdx.x;
   const Tensor& t = tensor_of(a, b);
   const int64_t e0 = (b - t.begin) * kBlock + (int64_t)threadIdx.x * 4;
