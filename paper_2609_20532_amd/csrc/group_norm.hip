@@ -16,9 +16,8 @@
 //
 // [256, 1024, 64]: float32 forward 33-37 us (134 MB, 3.9 TB/s: all tiles load, then
 // all store), backward 37 us (201 MB, 5.4 TB/s); bf16 forward 20 us (67 MB).
-// [2, 16384, 320] in bf16, which has no tile of all rows: forward 12 + 4 + 14 us,
-// backward 18 + 5 + 15; each tile's sums and the launches are what it takes, with
-// half or a quarter of the rows a tile the first passes take 14 and 22 us, 31.
+// [2, 16384, 320] in bf16, which has no tile of all rows: forward 11 + 4 + 12 us,
+// backward 15 + 4 + 14, mostly each tile's sums and the launches.
 //
 // Statistics are taken in two passes over the registers, the mean and then the
 // deviations from it, and tiles are merged by their counts: no difference of
@@ -31,6 +30,7 @@ namespace dpsgd {
 namespace {
 
 constexpr int kTile = 1024;    // most threads of a tile's workgroup
+constexpr int kPartTile = 256; // threads of a tile that has a part of the rows or of a group
 constexpr uint32_t kXcds = 8;
 constexpr int kGradRows = 8;   // rows of a thread in a backward tile
 
@@ -656,12 +656,20 @@ GnPlan plan_of(const dpsgd_group_norm& n, int per_thread) {
     return p;
   }
   p.whole = p.by_xcd = false;
-  p.threads = kTile;
-  const int64_t units = n.C / p.vec;
-  p.blocks = (int)ceil_div(units, kTile);
-  p.units = (int)ceil_div(units, p.blocks);
+  // Blocks of 128 bytes where rows are whole lines, so that no lane is idle at
+  // C = 320, of 256 where neighbouring blocks share lines; wider for few rows.
+  // [2, 16384, 320] bf16, forward and backward: 27 and 33 us, 29 and 40 with all
+  // channels in tiles of 1024 threads ([4, 9000, 1030]: 82 and 101, 113 and 124;
+  // [2, 16384, 324]: 29 and 40, 28 and 38, and 33 and 47 with blocks of 128 bytes).
+  // Tiles of 512 threads take 29 and 35 us, of 128 threads 29 and 34.
+  p.threads = kPartTile;
+  const int64_t units = n.C / p.vec, elem = n.dtype == DPSGD_BF16 ? 2 : 4;
+  int64_t most = (n.C * elem % 128 == 0 ? 128 : 256) / (p.vec * elem);
+  while (most * n.S < kPartTile) most *= 2;
+  p.units = (int)(units < most ? units : most);
+  p.blocks = (int)ceil_div(units, p.units);
   set_lanes(&p);
-  p.rows = (int64_t)per_thread * (kTile / p.lanes);
+  p.rows = (int64_t)per_thread * (kPartTile / p.lanes);
   if (p.rows > n.S) p.rows = n.S;
   p.chunks = ceil_div(n.S, p.rows);
   p.segs = (int)((int64_t)p.units * p.vec / width + 2);

@@ -154,6 +154,19 @@ def test_tiles_of_several_batches_of_rows(dp, B, S, C, groups, dtype):
     _check(x, dy, gamma, beta, groups, 1e-5, "silu", dtype, _run(dp, x, dy, gamma, beta, groups, 1e-5, "silu"))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,S,C,groups", [
+    (2, 2100, 320, 32),     # rows of whole lines, groups that straddle the blocks
+    (1, 2500, 324, 27),     # rows that share lines, the last block smaller
+    (2, 2049, 77, 7),
+    (3, 1, 4160, 1),        # one row, a group over many blocks
+    (2, 2, 5001, 3),
+])
+def test_tiles_of_a_part_of_the_channels(dp, B, S, C, groups, dtype):
+    x, dy, gamma, beta = _values(B, S, C, dtype, seed=S + C)
+    _check(x, dy, gamma, beta, groups, 1e-5, "silu", dtype, _run(dp, x, dy, gamma, beta, groups, 1e-5, "silu"))
+
+
 @pytest.mark.parametrize("affine", ["none", "gamma", "beta"])
 def test_without_affine_parameters(dp, affine):
     x, dy, gamma, beta = _values(3, 50, 24, "f32", seed=1)

@@ -188,11 +188,15 @@ def tile_plan(B, S, C, groups, elem, rows):
         threads = min(1024, ceil_div(lanes * S, 64) * 64)
         return True, V, units, lanes, ceil_div(C, cb), threads, 1, S, cb // width
     total = C // V
-    blocks = ceil_div(total, 1024)
-    units = ceil_div(total, blocks)
+    most = (128 if C * elem % 128 == 0 else 256) // (V * elem)
+    while most * S < 256:
+        most *= 2
+    units = min(total, most)
+    blocks = ceil_div(total, units)
     lanes = 1 << (units - 1).bit_length()
-    of_tile = min(S, rows * (1024 // lanes))
-    return False, V, units, lanes, blocks, 1024, ceil_div(S, of_tile), of_tile, units * V // width + 2
+    assert lanes <= 256
+    of_tile = min(S, rows * (256 // lanes))
+    return False, V, units, lanes, blocks, 256, ceil_div(S, of_tile), of_tile, units * V // width + 2
 
 
 @pytest.mark.parametrize("elem,rows", [(4, 8), (2, 16), (2, 8)])
@@ -200,7 +204,7 @@ def test_group_norm_tiles_cover_every_value_once(elem, rows):
     rng = random.Random(5)
     cases = [(1, 1, 64, 1), (2, 1024, 64, 16), (1, 3000, 16, 16), (5, 7, 33, 11), (1, 17, 1032, 8),
              (1, 2048, 320, 32), (2, 3, 4100, 1), (1, 9, 2051, 1), (1, 40, 6200, 2), (1, 100, 8197, 7),
-             (2, 16384, 320, 32), (1, 70000, 4, 2)]
+             (2, 16384, 320, 32), (1, 70000, 4, 2), (1, 1, 8200, 1), (3, 2, 5001, 1), (2, 2100, 324, 27)]
     for _ in range(300):
         width, groups = rng.choice([1, 2, 3, 4, 9, 10, 32, 77]), rng.choice([1, 2, 5, 16])
         cases.append((1, rng.randint(1, 3000), width * groups, groups))
