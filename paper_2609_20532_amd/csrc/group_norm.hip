@@ -104,8 +104,8 @@ struct GnArgs {
   float eps;
 };
 
-// n values: their mean as an unevaluated sum hi + lo (lo at most a rounding of
-// hi), and the sum of squared deviations from it. The second word keeps the
+// n values: their mean as an unevaluated sum hi + lo (lo at most a few roundings
+// of hi), and the sum of squared deviations from it. The second word keeps the
 // difference of two means, whose square enters the sum when they are merged, as
 // exact as the values themselves when the mean is far larger than the spread.
 struct Stat {
@@ -119,9 +119,15 @@ __device__ __forceinline__ float about_mean(float m2, float n, float lo) {
   return m < 0.0f ? 0.0f : m;
 }
 
+// An empty side is left alone: its mean of 0 says nothing, and the square of the
+// other's distance from it may not be finite.
 __device__ __forceinline__ void merge(Stat& a, const Stat& b) {
+  if (b.n == 0.0f) return;
+  if (a.n == 0.0f) {
+    a = b;
+    return;
+  }
   const float t = a.n + b.n;
-  if (t == 0.0f) return;
   const float w = b.n / t, d = (b.hi - a.hi) + (b.lo - a.lo);
   a.m2 = a.m2 + b.m2 + d * d * a.n * w;
   const float lo = fmaf(d, w, a.lo), hi = a.hi + lo;
@@ -368,7 +374,7 @@ __global__ __launch_bounds__(kThreads) void gn_finish_kernel(GnArgs a) {
     __syncthreads();
   }
   if (threadIdx.x == 0) {
-    a.mean[blockIdx.x] = st.hi;
+    a.mean[blockIdx.x] = st.hi + st.lo;   // a statistic that was merged with nothing still has both
     a.rstd[blockIdx.x] = 1.0f / sqrtf(st.m2 / ((float)a.S * (float)a.width) + a.eps);
   }
 }
