@@ -72,7 +72,9 @@ __device__ __forceinline__ void slopes(const float (&z)[V], float (&slope)[V]) {
     if constexpr (ACT == DPSGD_ACT_GELU) {
       const float p = sigmoid(2.0f * kGelu0 * fmaf(kGelu1 * z[c] * z[c], z[c], z[c]));
       const float du = kGelu0 * fmaf(3.0f * kGelu1 * z[c], z[c], 1.0f);
-      slope[c] = fmaf(2.0f * z[c] * p * (1.0f - p), du, p);
+      // Where p is 0 or 1 the first term is 0, also where du has left float32.
+      const float w = 2.0f * z[c] * p * (1.0f - p);
+      slope[c] = w == 0.0f ? p : fmaf(w, du, p);
     }
   }
 }

@@ -1,12 +1,14 @@
 """Group norm at the ends of its ranges, on the GPU against float64: means whose square
-leaves float32.
+leaves float32, pre-activations far from 0.
 
 Bounds as in test_gpu_group_norm.py.
 """
 
+import numpy as np
 import pytest
 
 import test_gpu_group_norm as base
+from oracle import model_oracle as mo
 
 pytestmark = pytest.mark.gpu
 U = base.U
@@ -32,3 +34,16 @@ def test_mean_whose_square_leaves_float32(dp, B, S, C, groups):
     x = x * 3e16 + 3e19
     base._check(x, dy, gamma, beta, groups, 1e-5, "none", "f32",
                 base._run(dp, x, dy, gamma, beta, groups, 1e-5, "none"))
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("B,S,C,groups", [(2, 49, 30, 10), (1, 5000, 12, 4)])
+def test_slope_far_from_zero(dp, B, S, C, groups, act):
+    # gamma 1e20: |z| is 1e13 and more, where y is max(z, 0) and its slope 0 or 1 in float64
+    # too, and z^2 leaves float32. ReLU's bounds hold then.
+    x, dy, gamma, beta = base._values(B, S, C, "f32", seed=S)
+    gamma = gamma * 1e20
+    z = mo.group_norm(x.double().numpy(), groups, gamma.double().numpy(), beta.double().numpy(), 1e-5, "none")[0]
+    assert np.abs(z).min() > 1e13 and np.abs(z).max() > 5e19
+    base._check(x, dy, gamma, beta, groups, 1e-5, "relu", "f32",
+                base._run(dp, x, dy, gamma, beta, groups, 1e-5, act))
