@@ -345,7 +345,7 @@ size_t dpsgd_embedding_workspace_bytes(const dpsgd_embedding* emb);
 /* norms_sq[i] = (accumulate ? norms_sq[i] : 0) + ||g_i||_F^2 (float32 [B]):
  * with accumulate, the table joins the norm over the linear layers. dtype is
  * G's. Every group of equal tokens of an example is summed in float32 before
- * its squared norm is taken. */
+ * its squared norm is taken, and scale^2 multiplies the sum of squares. */
 int dpsgd_embedding_norms(const dpsgd_embedding* emb, const void* G, int32_t dtype,
                           float* norms_sq, int32_t accumulate, void* workspace,
                           size_t workspace_bytes, void* stream);

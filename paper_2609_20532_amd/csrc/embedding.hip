@@ -616,7 +616,8 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormArgs a) {
   if (threadIdx.x == 0) {
     float t = 0.0f;
     for (int k = 0; k < kNormWaves; ++k) t += red[k];
-    t *= a.scale * a.scale;
+    // The square of the scale may be outside float32 where the norm is not.
+    t = (float)((double)t * ((double)a.scale * (double)a.scale));
     a.partials[blockIdx.x] = a.accumulate ? a.partials[blockIdx.x] + t : t;
   }
 }
