@@ -316,6 +316,10 @@ int dpsgd_noise_adamw_multi(const dpsgd_layer* layers, int32_t n_layers,
  * table [n_rows][d], ids [B][T], out and G [B][T][d], all row-major and
  * contiguous. An id outside [0, n_rows) is an empty position (padding): a row
  * of zeros in out, no part of the gradient; its row of G is not read.
+ * A launch has fewer than 2^32 threads; calls that would need more are refused
+ * (DPSGD_ERR_INVALID_ARG) with nothing enqueued. Never refused for it: lookups;
+ * norms with B ceil(d / 1024) < 2^22 and n_rows <= 2^30; sums with
+ * B T <= 2^28 - 32, n_rows <= 2^28 and B T ceil(d / 64) <= 2^30.
  * ids is aligned to its element, table, out and G to 16 bytes.
  * ------------------------------------------------------------------------- */
 typedef enum dpsgd_index_dtype {

@@ -101,6 +101,9 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
+// HIP launches fewer than 2^32 threads in a dimension.
+inline bool launchable(int64_t wgs, int64_t threads) { return wgs < (INT64_C(1) << 32) / threads; }
+
 // ------------------------------------------------------------ launchers
 // Each launcher validates nothing (the C ABI layer does) and returns a
 // dpsgd_status. Tables are built on the host and passed as kernel arguments.

@@ -250,14 +250,18 @@ __global__ __launch_bounds__(kSortThreads) void sort_kernel(Key keys, Buckets bk
   }
 }
 
+// Workgroups: the buckets', and those of the zeros (64 bytes a thread, at most a round).
+int64_t sort_wgs(const Buckets& bk, int64_t n_zeros = 0) {
+  const int64_t fill = ceil_div(n_zeros, 16 * kSortThreads);
+  return (INT64_C(1) << bk.log) + (fill < kSortBuckets ? fill : kSortBuckets);
+}
+
 template <class Key>
 int launch_sort(const Key& keys, const Buckets& bk, int32_t* order, int32_t* offsets,
                 hipStream_t stream, float* zeros = nullptr, int64_t n_zeros = 0) {
   const size_t lds = (size_t)(kSortWaves + 1) * bk.R * sizeof(int32_t);
-  const int64_t fill = ceil_div(n_zeros, 16 * kSortThreads);   // 64 bytes a thread, at most a round
-  const uint32_t wgs = (1u << bk.log) + (uint32_t)(fill < kSortBuckets ? fill : kSortBuckets);
-  hipLaunchKernelGGL(sort_kernel<Key>, dim3(wgs), dim3(kSortThreads), lds, stream, keys, bk, order,
-                     offsets, zeros, n_zeros);
+  hipLaunchKernelGGL(sort_kernel<Key>, dim3((uint32_t)sort_wgs(bk, n_zeros)), dim3(kSortThreads), lds,
+                     stream, keys, bk, order, offsets, zeros, n_zeros);
   return check_launch();
 }
 
@@ -883,7 +887,11 @@ int launch_embedding_norms(const dpsgd_embedding& e, const void* G, int32_t dtyp
   const int64_t N = e.B * e.T;
   const NormPlan p = norm_plan(e, dtype);
   const int64_t wgs = e.B * p.wgs * p.blocks;
-  if (wgs > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
+  // Launches that cannot be made are refused before the first.
+  if (!launchable(wgs, kNormThreads)) return DPSGD_ERR_INVALID_ARG;
+  if (!p.in_lds && !(launchable(sort_wgs(buckets_of(e.n_rows)), kSortThreads) &&
+                     launchable(sort_wgs(buckets_of(e.B)), kSortThreads)))
+    return DPSGD_ERR_INVALID_ARG;
   NormArgs a{};
   a.ids = e.ids;
   a.G = G;
@@ -959,9 +967,6 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
   const int64_t fill_rows = accumulate ? 0 : ((INT64_C(30) << 20) + 1800 * N) / (e.d * (int64_t)sizeof(float));
   const int64_t filled = fill_rows < e.n_rows ? round_up((size_t)(e.n_rows - fill_rows), 4) : 0;
   const bool fill = !accumulate && filled < e.n_rows;
-  const int st = sort_tokens(e, a.tokens, order, offsets, stream, fill ? grad + filled * e.d : nullptr,
-                             fill ? (e.n_rows - filled) * e.d : 0);
-  if (st != DPSGD_OK) return st;
   a.ids = e.ids;
   a.G = G;
   a.order = order;
@@ -985,9 +990,15 @@ int launch_embedding_sum(const dpsgd_embedding& e, const void* G, int32_t dtype,
   const int64_t chunk_wgs = ceil_div((int64_t)a.chunks * a.blocks, kThreads / 64);
   const int64_t row_wgs = ceil_div(a.rows, kThreads / 64 * kRowsPerWave);
   const int64_t wgs = chunk_wgs + row_wgs + (factors_out || mask_out ? ceil_div(e.B, kThreads) : 0);
-  if (wgs > 0x1FFFFFFF) return DPSGD_ERR_INVALID_ARG;   // jobs stay below 2^31
   a.chunk_wgs = (uint32_t)chunk_wgs;
   a.row_wgs = (uint32_t)row_wgs;
+  const int64_t n_zeros = fill ? (e.n_rows - filled) * e.d : 0;
+  // Launches that cannot be made are refused before the first.
+  if (!launchable(sort_wgs(a.tokens, n_zeros), kSortThreads) || !launchable(wgs, kThreads) ||
+      !launchable(a.chunks, kJoinThreads))
+    return DPSGD_ERR_INVALID_ARG;
+  const int st = sort_tokens(e, a.tokens, order, offsets, stream, fill ? grad + filled * e.d : nullptr, n_zeros);
+  if (st != DPSGD_OK) return st;
   const dim3 grid((uint32_t)wgs), block(kThreads), jgrid((uint32_t)a.chunks, (uint32_t)a.blocks);
 #define DPSGD_SUM(V)                                                                                \
   if (dtype == DPSGD_BF16) {                                                                        \
