@@ -379,6 +379,10 @@ int dpsgd_embedding_clip_accumulate(const dpsgd_embedding* emb, const void* G, i
  * gamma and beta are float32 [C] (NULL: 1 and 0). Statistics and arithmetic
  * are float32; y is rounded once to dtype. x, y, dy, dx are contiguous and
  * 16-byte aligned.
+ * A launch has fewer than 2^32 threads: 64 or more an example, up to four a
+ * vector of channels of a row (4, 2 or 1 channels, the most that divides C), and
+ * 256 a group where all rows of a group are no single tile. Calls that would
+ * need more are refused (DPSGD_ERR_INVALID_ARG) with nothing enqueued.
  * ------------------------------------------------------------------------- */
 typedef enum dpsgd_activation {
   DPSGD_ACT_NONE = 0,

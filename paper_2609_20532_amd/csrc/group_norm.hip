@@ -724,7 +724,9 @@ template <class T, int V, int ACT>
 int run(const dpsgd_group_norm& n, const GnPlan& p, bool backward, GnArgs a, hipStream_t stream) {
   const int64_t B = p.by_xcd ? (int64_t)round_up((size_t)n.B, kXcds) : n.B;
   const int64_t tiles = B * p.chunks * p.blocks, groups = n.B * n.groups;
-  if (tiles > 0x7FFFFFFF || groups > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
+  // Launches that cannot be made are refused before the first.
+  if (!launchable(tiles, p.threads) || (!p.whole && !launchable(groups, kThreads)))
+    return DPSGD_ERR_INVALID_ARG;
   const dim3 grid((uint32_t)tiles), block((uint32_t)p.threads), by_group((uint32_t)groups);
   const size_t channels = (size_t)p.units * V, sums = 2 * (size_t)slots_of(p.threads, p.log) * channels;
   if (!backward) {

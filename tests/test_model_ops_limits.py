@@ -46,3 +46,20 @@ def test_embedding_sum(lib, B, T, n_rows, d, accumulate):
         assert lib.dpsgd_embedding_clip_accumulate(
             ctypes.byref(e), P(16), dpsgd.DPSGD_F32, nsq, 1.0, P(1 << 44), accumulate, fac, None,
             P(64), 1 << 60, None) == INVALID
+
+
+@pytest.mark.parametrize("B,S,C,groups", [
+    (1 << 26, 1, 4, 1),             # 64 threads an example
+    ((1 << 31) - 1, 1, 1, 1),
+    (1 << 22, 511, 8, 1),           # 1024 threads an example
+    (1 << 13, 1 << 17, 512, 512),   # tiles of a part of the rows
+    (1 << 12, 3000, 4096, 4096),    # a workgroup a group, where the tiles are joined
+    (1 << 17, 9000, 128, 128),
+])
+@pytest.mark.parametrize("dtype", [dpsgd.DPSGD_F32, dpsgd.DPSGD_BF16])
+def test_group_norm(lib, B, S, C, groups, dtype):
+    n = dpsgd.dpsgd_group_norm(B, S, C, groups, None, None, dtype, 0, 1e-5)
+    a = [P(k << 44) for k in range(1, 10)]
+    assert lib.dpsgd_group_norm_forward(ctypes.byref(n), a[0], a[1], None, None, a[2], 1 << 60,
+                                        None) == INVALID
+    assert lib.dpsgd_group_norm_backward(ctypes.byref(n), *a[:7], a[7], 1 << 60, None) == INVALID
