@@ -440,6 +440,9 @@ int dpsgd_group_norm_backward(const dpsgd_group_norm* gn, const void* x, const v
  * infinite norm gives c = 0 (an infinite entry then becomes NaN, the others
  * 0), a NaN norm c = NaN. norm_out and factor_out: float32 [1], device, either
  * may be NULL in dpsgd_global_clip_multi.
+ * A launch has fewer than 2^32 threads: clipping takes up to 2^37 - 2^19 entries in
+ * any 48 tensors in a row, and calls that would need more threads are refused
+ * (DPSGD_ERR_INVALID_ARG) with nothing enqueued.
  * ------------------------------------------------------------------------- */
 size_t dpsgd_global_norm_workspace_bytes(const dpsgd_layer* layers, int32_t n_layers);
 

@@ -188,12 +188,18 @@ size_t global_norm_workspace_bytes(const dpsgd_layer* layers, int32_t n) {
 int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const* grads,
                        float* const* outs, float max_norm, float* norm_out, float* factor_out,
                        void* workspace, hipStream_t stream) {
+  // The scaling has a workgroup a block; launches that cannot be made are refused
+  // before the first.
+  for (int32_t base = 0; outs && base < n; base += kMaxLayersPerLaunch) {
+    const int32_t m = n - base < kMaxLayersPerLaunch ? n - base : kMaxLayersPerLaunch;
+    if (!launchable(args_of(layers + base, m, nullptr, nullptr).blocks, kThreads))
+      return DPSGD_ERR_INVALID_ARG;
+  }
   double* partials = static_cast<double*>(workspace);
   int64_t at = 0;
   for (int32_t base = 0; base < n; base += kMaxLayersPerLaunch) {
     const int32_t m = n - base < kMaxLayersPerLaunch ? n - base : kMaxLayersPerLaunch;
     ClipArgs a = args_of(layers + base, m, grads + base, nullptr);
-    if (a.blocks > 0x7FFFFFFF) return DPSGD_ERR_INVALID_ARG;
     a.partials = partials + at;
     hipLaunchKernelGGL(sum_squares_kernel, dim3((uint32_t)norm_wgs(a)), dim3(kThreads), 0, stream, a);
     at += norm_wgs(a);

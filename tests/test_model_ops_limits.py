@@ -63,3 +63,16 @@ def test_group_norm(lib, B, S, C, groups, dtype):
     assert lib.dpsgd_group_norm_forward(ctypes.byref(n), a[0], a[1], None, None, a[2], 1 << 60,
                                         None) == INVALID
     assert lib.dpsgd_group_norm_backward(ctypes.byref(n), *a[:7], a[7], 1 << 60, None) == INVALID
+
+
+@pytest.mark.parametrize("shapes", [
+    [(1 << 18, 1 << 19)],                        # 2^24 blocks of 8192 entries
+    [(1, 1)] * 49 + [(1 << 19, 1 << 20)],        # in the second launch
+    [(1 << 17, 1 << 18)] * 4,
+])
+def test_global_clip(lib, shapes):
+    layers = (dpsgd.dpsgd_layer * len(shapes))(*[dpsgd.shape_layer(1, 1, b, a) for a, b in shapes])
+    g = (P * len(shapes))(*[(k + 1) << 44 for k in range(len(shapes))])
+    for outs in (g, (P * len(shapes))(*[(k + 100) << 44 for k in range(len(shapes))])):
+        assert lib.dpsgd_global_clip_multi(layers, len(shapes), g, outs, 1.0, None, None, P(64),
+                                           1 << 60, None) == INVALID
