@@ -441,8 +441,12 @@ def _may_want(name, t, shape, code):
 
 
 def _workspace(workspace):
+    """Address and bytes of a workspace; raises ValueError unless the device holds all of
+    its bytes in a row."""
     if workspace is None:
         return None, 0
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous device tensor")
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
