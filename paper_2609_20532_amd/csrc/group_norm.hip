@@ -38,8 +38,11 @@ constexpr int kGradRows = 8;   // rows of a thread in a backward tile
 template <class T>
 constexpr int kTileRows = 32 / (int)sizeof(T);
 
-// 1 / (1 + exp(-z)) to a few units in the last place, by the hardware's
-// exponential and reciprocal.
+// 1 / (1 + exp(-z)) by the hardware's exponential and reciprocal. The exponent's
+// rounding enters the exponential times |z|: the relative error is at most
+// (1.25 |z| + 7) 2^-24 for z < 0 (z sigmoid(z) measured, in 2^-23: 1.4 from -1 on
+// up, 4.7 at -10 .. -8, 15 at -30 .. -20, 32 at -80 .. -60), and the value is 0
+// from about -87 on, where it would be below 2e-38.
 __device__ __forceinline__ float sigmoid(float z) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504f * z));
 }

@@ -1,5 +1,5 @@
 """Group norm at the ends of its ranges, on the GPU against float64: means whose square
-leaves float32, pre-activations far from 0.
+leaves float32, pre-activations far from 0, tails of the activations.
 
 Bounds as in test_gpu_group_norm.py.
 """
@@ -47,3 +47,27 @@ def test_slope_far_from_zero(dp, B, S, C, groups, act):
     assert np.abs(z).min() > 1e13 and np.abs(z).max() > 5e19
     base._check(x, dy, gamma, beta, groups, 1e-5, "relu", "f32",
                 base._run(dp, x, dy, gamma, beta, groups, 1e-5, act))
+
+
+@pytest.mark.parametrize("S,C", [(70, 8), (9000, 4)])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_tails_of_the_activations(dp, S, C, act):
+    # gamma 0: z is beta, exactly. y = z / (1 + exp(-w)) with w = z (SiLU) or
+    # 2 sqrt(2 / pi) (z + 0.044715 z^3). Relative to y, with one u for each rounding: w is off
+    # by 0 or 6 u of itself, its product with the rounded log2(e) by 1.25 u more, all of which
+    # the exponential multiplies by |w|; exponential, sum, reciprocal and product add 8 u.
+    import torch
+    lo, hi = (-80.0, 30.0) if act == "silu" else (-9.0, 9.0)
+    beta = torch.tensor(np.random.default_rng(1).uniform(lo, hi, C).astype(np.float32))
+    beta[0], beta[1] = lo, hi
+    x, _, _, _ = base._values(1, S, C, "f32", seed=2)
+    gn_x = x.cuda()
+    gn = dp.make_group_norm(gn_x, 2, torch.zeros(C, device="cuda"), beta.cuda(), 1e-5, act)
+    ws = torch.empty(dp.dpsgd_group_norm_workspace_bytes(gn), dtype=torch.uint8, device="cuda")
+    y = torch.full_like(gn_x, float("nan"))
+    dp.dpsgd_group_norm_forward(gn, gn_x, y, workspace=ws)
+    z = beta.double().numpy()
+    w = z if act == "silu" else 2 * np.sqrt(2 / np.pi) * (z + 0.044715 * z ** 3)
+    ref = z / (1 + np.exp(-w))
+    bound = ((1.25 if act == "silu" else 7.25) * np.abs(w) + 8) * U * np.abs(ref)
+    assert np.all(np.abs(y[0].cpu().double().numpy() - ref) <= bound)
