@@ -1,5 +1,5 @@
 """Group norm at the ends of its ranges, on the GPU against float64: means whose square
-leaves float32, pre-activations far from 0, tails of the activations.
+leaves float32, pre-activations far from 0, the order of tiles by XCD.
 
 Bounds as in test_gpu_group_norm.py.
 """
@@ -71,3 +71,12 @@ def test_tails_of_the_activations(dp, S, C, act):
     ref = z / (1 + np.exp(-w))
     bound = ((1.25 if act == "silu" else 7.25) * np.abs(w) + 8) * U * np.abs(ref)
     assert np.all(np.abs(y[0].cpu().double().numpy() - ref) <= bound)
+
+
+@pytest.mark.parametrize("dtype,B,S", [("f32", 67, 1100), ("f32", 64, 2048), ("bf16", 67, 700), ("bf16", 71, 1300)])
+def test_tiles_that_share_lines_on_one_xcd(dp, dtype, B, S):
+    # Rows of 64 bytes, in the backward pass or in both, for batches that are no multiple
+    # of the XCDs and one that is; outputs start as NaN.
+    x, dy, gamma, beta = base._values(B, S, 64, dtype, seed=S)
+    base._check(x, dy, gamma, beta, 16, 1e-5, "silu", dtype,
+                base._run(dp, x, dy, gamma, beta, 16, 1e-5, "silu"))
