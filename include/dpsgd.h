@@ -436,10 +436,12 @@ int dpsgd_group_norm_backward(const dpsgd_group_norm* gn, const void* x, const v
  * grads and outs: one float32 buffer of d_out d_in entries a layer, 16-byte
  * aligned; outs[l] may be grads[l] (in place), and overlaps nothing else. Only
  * d_in and d_out of a descriptor are read. Squares are summed in float64 and
- * the norm is rounded once to float32. max_norm > 0 (+inf: no clipping). An
- * infinite norm gives c = 0 (an infinite entry then becomes NaN, the others
- * 0), a NaN norm c = NaN. norm_out and factor_out: float32 [1], device, either
- * may be NULL in dpsgd_global_clip_multi.
+ * the norm is rounded once to float32, infinite above its range; c is formed
+ * from the norm before it is rounded. max_norm > 0 (+inf: c = 1, also for an
+ * infinite norm). An infinite entry gives c = 0 under a finite max_norm (the
+ * entry becomes NaN, finite ones 0), a NaN norm c = NaN. norm_out and
+ * factor_out: float32 [1], device, either may be NULL in
+ * dpsgd_global_clip_multi.
  * A launch has fewer than 2^32 threads: clipping takes up to 2^37 - 2^19 entries in
  * any 48 tensors in a row, and calls that would need more threads are refused
  * (DPSGD_ERR_INVALID_ARG) with nothing enqueued.

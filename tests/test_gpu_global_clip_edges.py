@@ -60,3 +60,22 @@ def test_outputs_where_squares_leave_float32(dp, size):
     assert factor < 1.0
     for got, r in zip(outs, ref):
         assert np.all(np.abs(got.cpu().double().numpy() - r) <= 2.0 ** -22 * np.abs(r) + 1e-44)
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_norm_above_float32_and_infinite_bound(dp, in_place):
+    import torch
+    grads = [torch.full((100, 90), 3e38, device="cuda"), torch.full((1, 3), -1e38, device="cuda")]
+    host = [g.cpu().numpy() for g in grads]
+    limit = float(np.float32(1e38))
+    ref_n, ref_c, ref = mo.global_clip(host, limit)      # 2.8e40
+    norm, factor, outs = base._clip(dp, grads, limit, in_place)
+    assert norm == math.inf and abs(factor - ref_c) <= 2.0 ** -23 * ref_c
+    for got, r in zip(outs, ref):
+        assert np.all(np.abs(got.cpu().double().numpy() - r) <= 2.0 ** -23 * np.abs(r))
+    # No bound: nothing changes, an infinite entry neither.
+    grads = [torch.tensor([[1.5, -math.inf, 3.0]], device="cuda"), torch.ones(4, 5, device="cuda")]
+    keep = [g.clone() for g in grads]
+    norm, factor, outs = base._clip(dp, grads, math.inf, in_place)
+    assert norm == math.inf and factor == 1.0
+    assert all(torch.equal(a, b) for a, b in zip(outs, keep))
