@@ -8,8 +8,8 @@
 // float64: the conversion and the fused multiply-add are far below the memory
 // time, no square overflows or vanishes, and the norm is rounded once. Every
 // workgroup of the second pass adds up the first one's partial sums itself: two
-// launches. 48 tensors of 340 MB: 57 us (6.0 TB/s) and 110 us (680 MB, 6.2 TB/s);
-// 24 tensors of 0.3 MB: 4.6 and 6.7 us.
+// launches. 48 tensors of 340 MB: 58 us (5.9 TB/s) and 110 us (680 MB, 6.2 TB/s);
+// 24 tensors of 0.59 MB: 4.6 and 6.7 us.
 #include <math.h>
 
 #include "vec.h"
