@@ -458,6 +458,217 @@ int dpsgd_global_clip_multi(const dpsgd_layer* layers, int32_t n_layers,
                             size_t workspace_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Log probabilities of tokens, and the loss.
+ * Paper: Section 2.2 (the per-example loss whose gradient is clipped), for a
+ * language model or a classifier.
+ *
+ * logits: B T rows of V entries, float32 or bf16; row r begins at entry
+ * r * stride, stride >= V (entries between V and stride are not read, nor
+ * written in a gradient). Per row, in float32:
+ *
+ *   z = scale * logits;  m = max z;  S = sum_v exp(z_v - m)
+ *   lse = m + ln S;  p_v = exp(z_v - m) / S;  logprob = (z_target - m) - ln S
+ *   entropy = ln S - sum_v p_v (z_v - m)
+ *
+ *  - targets [B][T]; one outside [0, V) is an empty position (padding): its row
+ *    is not read; logprob, lse and entropy are 0, it has no alternatives, and
+ *    its gradient is a row of zeros. targets NULL: no position is empty, and
+ *    there are no log probabilities of targets.
+ *  - z_v = -inf (a masked token) has p_v = 0. A row whose every z is -inf has no
+ *    distribution: lse and logprob are -inf, entropy 0, no alternatives, and the
+ *    gradient is 0. A z of +inf or NaN makes the row's outputs and gradient NaN,
+ *    without alternatives.
+ * ------------------------------------------------------------------------- */
+#define DPSGD_MOST_ALTERNATIVES 64
+
+typedef struct dpsgd_logits {
+  const void* targets;  /* [B][T] token ids, index_dtype; may be NULL        */
+  int64_t B;            /* examples, >= 1                                    */
+  int64_t T;            /* positions per example, >= 1; B T <= 2^30          */
+  int64_t V;            /* tokens (classes), 1 .. 2^24                       */
+  int64_t stride;       /* entries from a row to the next, V .. 2^31;
+                           B T stride <= 2^40                                */
+  int32_t index_dtype;  /* dpsgd_index_dtype                                 */
+  int32_t dtype;        /* dpsgd_dtype of logits and their gradient          */
+  float scale;          /* > 0, finite (1 / temperature)                     */
+} dpsgd_logits;
+
+/* Scratch of dpsgd_token_logprobs with k alternatives and of dpsgd_token_loss
+ * (k = 0) (device, 16-byte aligned); 0 for an invalid descriptor or k. Does not
+ * read targets. */
+size_t dpsgd_token_workspace_bytes(const dpsgd_logits* desc, int32_t k);
+
+/* logprobs, lse, entropy: float32 [B][T]. top_ids (int64) and top_logprobs
+ * (float32) [B][T][k]: the k largest logits of a row and their log
+ * probabilities, largest first, of equal logits the lower token first; where a
+ * row has fewer than k logits above -inf, id -1 and -inf follow (NaN instead of
+ * -inf where the row is NaN). 0 <= k <= DPSGD_MOST_ALTERNATIVES; with k = 0
+ * top_ids and top_logprobs must be NULL. Any output may be NULL, not all; with
+ * targets NULL logprobs must be. logits is aligned to its element. */
+int dpsgd_token_logprobs(const dpsgd_logits* desc, const void* logits, float* logprobs, float* lse,
+                         float* entropy, int32_t k, int64_t* top_ids, float* top_logprobs,
+                         void* workspace, size_t workspace_bytes, void* stream);
+
+/* The gradient of sum grad_logprobs logprob + grad_lse lse + grad_entropy entropy
+ * (each float32 [B][T]; NULL: 0, not all of them) by the logits, rounded once to
+ * dtype:
+ *   dlogits_v = scale (p_v (grad_lse - grad_logprobs - grad_entropy (ln p_v + entropy))
+ *                      + grad_logprobs [v = target])
+ * lse and entropy are dpsgd_token_logprobs' (entropy is read only with
+ * grad_entropy). A row whose three factors are 0 gets zeros, whatever its
+ * logits. Row r of dlogits begins at entry r * dlogits_stride (V .. 2^31).
+ * dlogits may be logits (with the same stride), and overlaps nothing else. */
+int dpsgd_token_logprobs_backward(const dpsgd_logits* desc, const void* logits, const float* lse,
+                                  const float* entropy, const float* grad_logprobs,
+                                  const float* grad_lse, const float* grad_entropy, void* dlogits,
+                                  int64_t dlogits_stride, void* stream);
+
+/* Per-example losses and the gradient of their sum, the logits read once where a
+ * row fits a workgroup's registers (V up to 131072 in bf16, 65536 in float32):
+ *   losses[i] = -sum_t w_it logprob_it                     (float32 [B], or NULL)
+ *   dlogits   = scale w_it (p_v - [v = target])            as above
+ * weights float32 [B][T]; NULL: all 1. A position of weight 0 adds nothing and
+ * gets zeros, whatever its logits. logprobs (float32 [B][T]) may be NULL.
+ * targets must not be NULL. */
+int dpsgd_token_loss(const dpsgd_logits* desc, const void* logits, const float* weights,
+                     float* losses, float* logprobs, void* dlogits, int64_t dlogits_stride,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * The residual sum between two blocks, with the norms on both sides of it.
+ * Paper: Section 2.2, per-example gradients of the trainable parameters.
+ *
+ *   u = post ? norm(block) post_gamma + post_beta : block
+ *   r = residual_scale x + gate u            (rounded to dtype)
+ *   y = norm(r) gamma + beta                 (of r as it is stored)
+ *   norm(v) = (v - mean) rstd, rstd = 1 / sqrt(var + eps)      (LAYER)
+ *           = v rstd, rstd = 1 / sqrt(mean(v^2) + eps)         (RMS)
+ *
+ * over rows of C channels; x, block, r, y [B][S][C], contiguous. block NULL: r =
+ * residual_scale x, with no gate and no post. Arithmetic and statistics are
+ * float32; r and y are rounded once each. Every tensor, the affine parameters and
+ * their gradients among them, is 16-byte aligned.
+ * ------------------------------------------------------------------------- */
+typedef enum dpsgd_row_norm {
+  DPSGD_ROW_NORM_LAYER = 0,
+  DPSGD_ROW_NORM_RMS = 1
+} dpsgd_row_norm;
+
+typedef struct dpsgd_residual_norm {
+  int64_t B;                 /* examples, >= 1                                    */
+  int64_t S;                 /* positions per example, >= 1; B S < 2^31           */
+  int64_t C;                 /* channels, 1 .. 16384                              */
+  const float* gamma;        /* [C], device; NULL: 1                              */
+  const float* beta;         /* [C], device; NULL: 0                              */
+  const float* post_gamma;   /* the same for the block's norm; NULL without post  */
+  const float* post_beta;
+  const float* gate;         /* NULL: 1; [C], or [B][C] with gate_per_example     */
+  int32_t gate_per_example;
+  int32_t post;              /* the block's output is normed before it is added   */
+  int32_t kind;              /* dpsgd_row_norm of both norms                      */
+  int32_t dtype;             /* dpsgd_dtype of x, block, r, y and their gradients */
+  float residual_scale;      /* finite                                            */
+  float eps;                 /* > 0, finite                                       */
+} dpsgd_residual_norm;
+
+/* stats (float32 [B][S][4]: mean, rstd of r, mean, rstd of the block's output; 0
+ * where there is none) is kept for the backward call; NULL
+ * where there is none. r may be x and y may be block; r may be NULL (not
+ * written; y is formed from the same rounded values). Outputs overlap nothing
+ * else. */
+int dpsgd_residual_norm_forward(const dpsgd_residual_norm* desc, const void* x, const void* block,
+                                void* r, void* y, float* stats, void* stream);
+
+/* Scratch of the call below (device, 16-byte aligned); 0 for an invalid
+ * descriptor. Does not read the pointers of the descriptor. */
+size_t dpsgd_residual_norm_workspace_bytes(const dpsgd_residual_norm* desc);
+
+/* From dy and dr (the gradient that reaches r past the norm; NULL: 0), with
+ * D(g, vh) the norm's backward, rstd (g - mean(g) - vh mean(g vh)) (RMS: without
+ * mean(g)):
+ *   dR = dr + D(dy gamma, rh);  dx = residual_scale dR;  dU = gate dR
+ *   dblock = post ? D(dU post_gamma, bh) : dU
+ * and the per-example gradients (float32 [B][C], each may be NULL: not formed)
+ *   dgamma_i = sum_s dy rh;  dbeta_i = sum_s dy;  dgate_i = sum_s dR u
+ *   dpost_gamma_i = sum_s dU bh;  dpost_beta_i = sum_s dU
+ * which the norm, clip, noise and step calls take as layers with T = 1, d_in = 1,
+ * A = 1. block and dblock are NULL together; block is not read without post and
+ * dgate. r is the forward call's (x for a block NULL with residual_scale 1).
+ * dx may be dr or NULL, dblock may be dy; they overlap nothing else. A launch has
+ * fewer than 2^32 threads, 64 to 1024 for each example at least; calls that would
+ * need more are refused (DPSGD_ERR_INVALID_ARG; never with B < 2^22) with nothing
+ * enqueued. */
+int dpsgd_residual_norm_backward(const dpsgd_residual_norm* desc, const void* block, const void* r,
+                                 const void* dy, const void* dr, const float* stats, void* dx,
+                                 void* dblock, float* dgamma, float* dbeta, float* dgate,
+                                 float* dpost_gamma, float* dpost_beta, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Noise + AdamW step with moments in 8 bits.
+ * Paper: GPU-side algorithm, its last two steps, as dpsgd_noise_adamw.
+ *
+ * The moments of a tensor of n entries are n codes each, and a pair of exponents
+ * (k_m, k_v, uint8, biased by 127) for every 256 entries in a row:
+ *   m: bit 7 the sign, bits 6..3 an exponent E, bits 2..0 a fraction F
+ *      |m| = (1 + F/8) 2^(E - 15 + k_m - 127),  E = 0: F/8 2^(-14 + k_m - 127)
+ *   v: bits 7..3 E, bits 2..0 F
+ *      v = (1 + F/8) 2^(E - 31 + k_v - 127),    E = 0: F/8 2^(-30 + k_v - 127)
+ * All zeros stand for moments of 0. A block's exponent is that of its largest
+ * magnitude rounded up to 3 bits of fraction, at least 32 (m) or 48 (v); the
+ * exponent 255 stands for a block with a magnitude that is not finite (or is
+ * above 1.875 2^127), which reads back as NaN.
+ *
+ * One step, every operation rounded to float32 by itself (no fused multiply-add;
+ * the constants are formed in double on the host and rounded):
+ *   g = scale * (grad + sigma C z)                (z, and its sum, as dpsgd_noise_adamw)
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) (g g)
+ *   param = param (1 - lr weight_decay)
+ *           - (m / (sqrt(v) (1 / sqrt(1 - beta2^t)) + eps)) (lr / (1 - beta1^t))
+ * with m and v in float32, which are then rounded to codes:
+ *  - DPSGD_ROUND_NEAREST: to nearest, ties to even.
+ *  - DPSGD_ROUND_STOCHASTIC: up with the probability of the distance from the
+ *    value below, in steps of 2^-16 (the mean of many steps is kept, which nearest
+ *    rounding loses for changes of less than half a code, as most of v's are).
+ *    Entry e takes word e mod 4 of the Philox4x32-10 block j = e / 4 with counter
+ *    (j mod 2^32, j >> 32, tensor_id, t) and the complement of round_seed as its
+ *    key: bits 0..15 for m, 16..31 for v.
+ * A v above 0 is never rounded to 0.
+ * ------------------------------------------------------------------------- */
+#define DPSGD_STATE_BLOCK 256
+
+typedef enum dpsgd_rounding {
+  DPSGD_ROUND_NEAREST = 0,
+  DPSGD_ROUND_STOCHASTIC = 1
+} dpsgd_rounding;
+
+/* Arrays and arguments as in dpsgd_noise_adamw_multi; exp_avgs and exp_avg_sqs
+ * hold codes (uint8 [d_out d_in]), exponents uint8 [ceil(d_out d_in / 256)][2],
+ * all 16-byte aligned and pairwise non-overlapping. round_seed is read only with
+ * DPSGD_ROUND_STOCHASTIC. A launch has fewer than 2^32 threads: any 48 tensors in a
+ * row have up to 2^35 entries together (less 2^18 for their ends), and calls that
+ * would need more are refused. */
+int dpsgd_noise_adamw8_multi(const dpsgd_layer* layers, int32_t n_layers,
+                             const float* const* grads, float* const* params,
+                             uint8_t* const* exp_avgs, uint8_t* const* exp_avg_sqs,
+                             uint8_t* const* exponents, float* const* noisy_outs, float sigma,
+                             float C, uint64_t seed, uint32_t step, float scale,
+                             const dpsgd_adamw* opt, int32_t rounding, uint64_t round_seed,
+                             void* stream);
+
+/* float32 moments (v >= 0) to codes and exponents, to nearest, and codes to
+ * moments, float32 or bf16 (both exact). A NaN, infinite or (v) negative
+ * moment makes its block NaN. */
+int dpsgd_adamw8_pack_multi(const dpsgd_layer* layers, int32_t n_layers,
+                            const float* const* exp_avgs_in, const float* const* exp_avg_sqs_in,
+                            uint8_t* const* exp_avgs, uint8_t* const* exp_avg_sqs,
+                            uint8_t* const* exponents, void* stream);
+int dpsgd_adamw8_unpack_multi(const dpsgd_layer* layers, int32_t n_layers,
+                              const uint8_t* const* exp_avgs, const uint8_t* const* exp_avg_sqs,
+                              const uint8_t* const* exponents, void* const* exp_avgs_out,
+                              void* const* exp_avg_sqs_out, int32_t out_dtype, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Inspection hooks for tests (same stream as dpsgd_add_noise).
  *   dpsgd_philox_u32: out[4*b + w] = word w of block (first_block + b), b < n_blocks.
  *   dpsgd_gaussian:   out[e] = z_e of the stream above for e < n.

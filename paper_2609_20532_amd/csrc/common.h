@@ -342,6 +342,39 @@ int launch_global_clip(const dpsgd_layer* layers, int32_t n, const float* const*
                        float* const* outs, float max_norm, float* norm_out, float* factor_out,
                        void* workspace, hipStream_t stream);
 
+// Log probabilities and loss (token_loss.hip), residual norms (residual_norm.hip),
+// AdamW with 8-bit moments (adamw8.hip).
+size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k);
+int launch_token_logprobs(const dpsgd_logits& d, const void* logits, float* logprobs, float* lse,
+                          float* entropy, int32_t k, int64_t* top_ids, float* top_logprobs,
+                          void* workspace, hipStream_t stream);
+int launch_token_backward(const dpsgd_logits& d, const void* logits, const float* lse,
+                          const float* entropy, const float* g_logp, const float* g_lse,
+                          const float* g_entropy, void* dlogits, int64_t dlogits_stride,
+                          hipStream_t stream);
+int launch_token_loss(const dpsgd_logits& d, const void* logits, const float* weights,
+                      float* losses, float* logprobs, void* dlogits, int64_t dlogits_stride,
+                      void* workspace, hipStream_t stream);
+size_t residual_norm_workspace_bytes(const dpsgd_residual_norm& n);
+int launch_residual_norm_forward(const dpsgd_residual_norm& n, const void* x, const void* block,
+                                 void* r, void* y, float* stats, hipStream_t stream);
+// grads: dgamma, dbeta, dgate, dpost_gamma, dpost_beta (null: not formed).
+int launch_residual_norm_backward(const dpsgd_residual_norm& n, const void* block, const void* r,
+                                  const void* dy, const void* dr, const float* stats, void* dx,
+                                  void* dblock, float* const* grads, void* workspace,
+                                  hipStream_t stream);
+int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* const* grads,
+                        float* const* params, uint8_t* const* ms, uint8_t* const* vs,
+                        uint8_t* const* exps, float* const* noisy, float sigma, float C,
+                        uint64_t seed, uint32_t step, float scale, const dpsgd_adamw& opt,
+                        int32_t rounding, uint64_t round_seed, hipStream_t stream);
+int launch_adamw8_pack(const dpsgd_layer* layers, int n_layers, const float* const* ms_in,
+                       const float* const* vs_in, uint8_t* const* ms, uint8_t* const* vs,
+                       uint8_t* const* exps, hipStream_t stream);
+int launch_adamw8_unpack(const dpsgd_layer* layers, int n_layers, const uint8_t* const* ms,
+                         const uint8_t* const* vs, const uint8_t* const* exps, void* const* ms_out,
+                         void* const* vs_out, int32_t out_dtype, hipStream_t stream);
+
 inline int check_launch() {
   return hipGetLastError() == hipSuccess ? DPSGD_OK : DPSGD_ERR_HIP;
 }

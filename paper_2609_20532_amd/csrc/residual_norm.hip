@@ -1,0 +1,513 @@
+// The residual sum between two blocks with the norms on both sides of it, and its
+// gradients. Per row of C channels:
+//
+//   u = norm(block) post_gamma + post_beta;  r = alpha x + gate u;  y = norm(r) gamma + beta
+//
+//   D(g, vh) = rstd (g - mean(g) - vh mean(g vh))     (RMS: without mean(g))
+//   dR = dr + D(dy gamma, rh);  dx = alpha dR;  dU = gate dR;  dblock = D(dU post_gamma, bh)
+//   per example: dgamma = sum_s dy rh, dbeta = sum_s dy, dgate = sum_s dR u,
+//                dpost_gamma = sum_s dU bh, dpost_beta = sum_s dU
+//
+// Bound by memory traffic: forward 4 rows of C elements (x, block, r, y), backward
+// 6 (r, block, dy, dr, dx, dblock), each touched once. A group of threads has a row
+// in registers, a fixed set of channels a thread, and takes several rows: the affine
+// parameters stay in registers, and so do the per-example sums of a backward group,
+// which are joined over a workgroup's groups in LDS and over an example's workgroups
+// by a second launch.
+#include <math.h>
+
+#include "vec.h"
+
+namespace dpsgd {
+namespace {
+
+constexpr int kMostThreads = 1024;
+constexpr int kWaves = kMostThreads / 64;
+constexpr int kGrads = 5;   // dgamma, dbeta, dgate, dpost_gamma, dpost_beta
+
+struct RnArgs {
+  const void* x;         // backward: r
+  const void* block;     // may be null
+  const void* dy;
+  const void* dr;        // may be null
+  void* r;               // backward: dx (may be null)
+  void* y;               // backward: dblock (null without a block)
+  float* stats;          // [B S][4]
+  const float* gamma;    // null: 1
+  const float* beta;     // null: 0
+  const float* post_gamma;
+  const float* post_beta;
+  const float* gate;
+  float* grads[kGrads];  // [B][C], or null
+  float* partials;       // [B][chunks][kGrads][C]
+  int64_t rows;          // B S
+  int64_t S;
+  int32_t C, log;        // log2 of the threads of a row
+  int32_t iters;         // rows of a group
+  int32_t chunks;        // backward: workgroups of an example
+  int32_t gate_per_example, post, layer;
+  float alpha, eps, inv_C;
+};
+
+// Sums of K values over the threads of each row, in all of them. For rows of more
+// than a wave every thread of the workgroup has to call it; `slot` goes between 0
+// and 1 from call to call, so that one barrier a call is enough.
+template <int K>
+__device__ __forceinline__ void row_sum(float (&v)[K], int log, float (*lds)[kWaves][2], int& slot) {
+  if (log < 6) {
+    for (int off = 1; off < (1 << log); off <<= 1) {
+#pragma unroll
+      for (int k = 0; k < K; ++k) v[k] += __shfl_xor(v[k], off, 64);
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = wave_total(v[k]);
+  if (log == 6) return;
+  const int wave = threadIdx.x >> 6, per = 1 << (log - 6), from = wave & ~(per - 1);
+  if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) lds[slot][wave][k] = v[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < K; ++k) v[k] = 0.0f;
+  for (int w = 0; w < per; ++w) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) v[k] += lds[slot][from + w][k];
+  }
+  slot ^= 1;
+}
+
+// A row's (or a parameter's) vectors of V elements that a thread has.
+template <int V, int NV>
+struct Channels {
+  int32_t first, step, C;
+  __device__ __forceinline__ int32_t at(int j) const { return first + j * step; }
+  __device__ __forceinline__ bool has(int j) const { return at(j) < C; }
+};
+
+template <class T, int V, int NV>
+__device__ __forceinline__ void load_row(const T* p, const Channels<V, NV>& ch, bool active,
+                                         Raw<T, V> (&raw)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    raw[j].zero();
+    if (active && ch.has(j)) raw[j].load(p + ch.at(j));
+  }
+}
+
+template <class T, int V, int NV>
+__device__ __forceinline__ void widen_row(const Raw<T, V> (&raw)[NV], float (&x)[NV][V]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) raw[j].widen(x[j]);
+}
+
+template <class T, int V, int NV>
+__device__ __forceinline__ void store_row(T* p, const Channels<V, NV>& ch, const float (&x)[NV][V]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j)
+    if (ch.has(j)) store_vec<V>(p + ch.at(j), x[j]);
+}
+
+template <int V, int NV>
+__device__ __forceinline__ void load_affine(const float* p, float none, const Channels<V, NV>& ch,
+                                            float (&x)[NV][V]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) x[j][c] = none;
+    if (p && ch.has(j)) load_vec<V>(p + ch.at(j), x[j]);
+  }
+}
+
+// x rounded to the row's type and widened again.
+template <class T, int V>
+__device__ __forceinline__ void round_to(float (&x)[V]) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int c = 0; c < V; ++c) x[c] = bf16_lo(pack_bf16x2(x[c], 0.0f));
+  }
+}
+
+// Mean (0 without `layer`) and rstd of a row in registers, channels past the end 0.
+template <int V, int NV>
+__device__ __forceinline__ float2 row_stats(const float (&x)[NV][V], const Channels<V, NV>& ch,
+                                            const RnArgs& a, float (*lds)[kWaves][2], int& slot) {
+  float s[1] = {0.0f}, mean = 0.0f;
+  if (a.layer) {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) s[0] += x[j][c];
+    row_sum<1>(s, a.log, lds, slot);
+    mean = s[0] / (float)a.C;
+    s[0] = 0.0f;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    if (ch.has(j)) {
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        const float d = x[j][c] - mean;
+        s[0] = fmaf(d, d, s[0]);
+      }
+    }
+  }
+  row_sum<1>(s, a.log, lds, slot);
+  return make_float2(mean, 1.0f / sqrtf(s[0] / (float)a.C + a.eps));
+}
+
+template <class T, int V, int NV, int MOST>
+__global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
+  __shared__ float lds[2][kWaves][2];
+  const int group = (int)threadIdx.x >> a.log, groups = (int)blockDim.x >> a.log;
+  const int lane = (int)threadIdx.x & ((1 << a.log) - 1);
+  const Channels<V, NV> ch{lane * V, V << a.log, a.C};
+  int slot = 0;
+  float ga[NV][V], be[NV][V], gt[NV][V], pg[NV][V], pb[NV][V];
+  load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
+  load_affine<V, NV>(a.beta, 0.0f, ch, be);
+  load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
+  load_affine<V, NV>(a.post_beta, 0.0f, ch, pb);
+  load_affine<V, NV>(a.gate_per_example ? nullptr : a.gate, 1.0f, ch, gt);
+  for (int i = 0; i < a.iters; ++i) {
+    const int64_t row = ((int64_t)blockIdx.x * a.iters + i) * groups + group;
+    const bool active = row < a.rows;
+    const int64_t at = row * a.C;
+    Raw<T, V> rx[NV], rb[NV];
+    load_row<T, V, NV>(static_cast<const T*>(a.x) + at, ch, active, rx);
+    load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active && a.block, rb);
+    if (a.gate_per_example && active) load_affine<V, NV>(a.gate + row / a.S * a.C, 1.0f, ch, gt);
+    float x[NV][V], u[NV][V];
+    widen_row<T, V, NV>(rx, x);
+    widen_row<T, V, NV>(rb, u);
+    float2 post = make_float2(0.0f, 0.0f);
+    if (a.post) {
+      post = row_stats<V, NV>(u, ch, a, lds, slot);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) u[j][c] = fmaf((u[j][c] - post.x) * post.y, pg[j][c], pb[j][c]);
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int c = 0; c < V; ++c) x[j][c] = ch.has(j) ? fmaf(gt[j][c], u[j][c], a.alpha * x[j][c]) : 0.0f;
+      round_to<T, V>(x[j]);
+    }
+    const float2 st = row_stats<V, NV>(x, ch, a, lds, slot);
+    if (!active) continue;
+    if (a.r) store_row<T, V, NV>(static_cast<T*>(a.r) + at, ch, x);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) x[j][c] = fmaf((x[j][c] - st.x) * st.y, ga[j][c], be[j][c]);
+    store_row<T, V, NV>(static_cast<T*>(a.y) + at, ch, x);
+    if (a.stats && lane == 0)
+      reinterpret_cast<float4*>(a.stats)[row] = make_float4(st.x, st.y, post.x, post.y);
+  }
+}
+
+// One workgroup: some rows of one example, which its groups take in turn.
+template <class T, int V, int NV, int MOST>
+__global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
+  extern __shared__ __align__(16) float rn_lds[];   // [groups][C], where there are several groups
+  __shared__ float lds[2][kWaves][2];
+  const int group = (int)threadIdx.x >> a.log, groups = (int)blockDim.x >> a.log;
+  const int lane = (int)threadIdx.x & ((1 << a.log) - 1);
+  const Channels<V, NV> ch{lane * V, V << a.log, a.C};
+  const int64_t example = blockIdx.x / (uint32_t)a.chunks;
+  const int32_t chunk = (int32_t)(blockIdx.x - (uint32_t)example * (uint32_t)a.chunks);
+  const bool want_u = a.grads[2] != nullptr, read_block = a.block && (a.post || want_u);
+  int slot = 0;
+  float ga[NV][V], gt[NV][V], pg[NV][V], pb[NV][V];
+  load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
+  load_affine<V, NV>(a.gate ? a.gate + (a.gate_per_example ? example * a.C : 0) : nullptr, 1.0f, ch, gt);
+  load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
+  load_affine<V, NV>(a.post_beta, 0.0f, ch, pb);
+  float acc[kGrads][NV][V] = {};
+  for (int i = 0; i < a.iters; ++i) {
+    const int64_t s = ((int64_t)chunk * a.iters + i) * groups + group;
+    const bool active = s < a.S;
+    const int64_t row = example * a.S + s, at = row * a.C;
+    Raw<T, V> rr[NV], rb[NV], rdy[NV], rdr[NV];
+    load_row<T, V, NV>(static_cast<const T*>(a.x) + at, ch, active, rr);
+    load_row<T, V, NV>(static_cast<const T*>(a.dy) + at, ch, active, rdy);
+    load_row<T, V, NV>(static_cast<const T*>(a.dr) + at, ch, active && a.dr, rdr);
+    load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active && read_block, rb);
+    float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (active) st = reinterpret_cast<const float4*>(a.stats)[row];
+    float d[NV][V], vh[NV][V];
+    widen_row<T, V, NV>(rdy, d);
+    widen_row<T, V, NV>(rr, vh);
+    float m[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        vh[j][c] = ch.has(j) ? (vh[j][c] - st.x) * st.y : 0.0f;
+        acc[0][j][c] = fmaf(d[j][c], vh[j][c], acc[0][j][c]);
+        acc[1][j][c] += d[j][c];
+        d[j][c] *= ga[j][c];
+        m[0] += d[j][c];
+        m[1] = fmaf(d[j][c], vh[j][c], m[1]);
+      }
+    row_sum<2>(m, a.log, lds, slot);
+    m[0] = a.layer ? m[0] * a.inv_C : 0.0f;
+    m[1] *= a.inv_C;
+    float dr[NV][V];
+    widen_row<T, V, NV>(rdr, dr);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        dr[j][c] = fmaf(st.y, d[j][c] - fmaf(vh[j][c], m[1], m[0]), dr[j][c]);
+        d[j][c] = a.alpha * dr[j][c];
+      }
+    }
+    if (active && a.r) store_row<T, V, NV>(static_cast<T*>(a.r) + at, ch, d);
+    if (!a.y) continue;
+    widen_row<T, V, NV>(rb, vh);
+    m[0] = m[1] = 0.0f;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        if (!ch.has(j)) dr[j][c] = 0.0f;
+        if (a.post) vh[j][c] = ch.has(j) ? (vh[j][c] - st.z) * st.w : 0.0f;
+        const float u = a.post ? fmaf(vh[j][c], pg[j][c], pb[j][c]) : vh[j][c];
+        acc[2][j][c] = fmaf(dr[j][c], u, acc[2][j][c]);
+        const float du = gt[j][c] * dr[j][c];
+        d[j][c] = du;
+        if (a.post) {
+          acc[3][j][c] = fmaf(du, vh[j][c], acc[3][j][c]);
+          acc[4][j][c] += du;
+          d[j][c] = du * pg[j][c];
+          m[0] += d[j][c];
+          m[1] = fmaf(d[j][c], vh[j][c], m[1]);
+        }
+      }
+    if (a.post) {
+      row_sum<2>(m, a.log, lds, slot);
+      m[0] = a.layer ? m[0] * a.inv_C : 0.0f;
+      m[1] *= a.inv_C;
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) d[j][c] = st.w * (d[j][c] - fmaf(vh[j][c], m[1], m[0]));
+    }
+    if (active) store_row<T, V, NV>(static_cast<T*>(a.y) + at, ch, d);
+  }
+
+  // The groups' sums, added in their order, to the example's row or to a partial one.
+#pragma unroll
+  for (int k = 0; k < kGrads; ++k) {
+    if (!a.grads[k]) continue;
+    float* to = a.chunks == 1 ? a.grads[k] + example * a.C
+                              : a.partials + ((int64_t)blockIdx.x * kGrads + k) * a.C;
+    if (groups == 1) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (ch.has(j)) store_vec<V>(to + ch.at(j), acc[k][j]);
+      continue;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+      if (ch.has(j)) store_vec<V>(rn_lds + group * a.C + ch.at(j), acc[k][j]);
+    __syncthreads();
+    for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
+      float t = 0.0f;
+      for (int g = 0; g < groups; ++g) t += rn_lds[g * a.C + c];
+      to[c] = t;
+    }
+  }
+}
+
+// One thread a channel of an example's gradient: its workgroups' sums in order.
+__global__ __launch_bounds__(kThreads) void rn_join_kernel(RnArgs a, int64_t total) {
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total;
+       i += (int64_t)gridDim.x * kThreads) {
+    const int64_t example = i / (kGrads * a.C);
+    const int32_t rest = (int32_t)(i - example * (kGrads * a.C)), k = rest / a.C;
+    float* to = a.grads[k];
+    if (!to) continue;
+    const float* from = a.partials + example * a.chunks * kGrads * a.C + rest;
+    float t = 0.0f;
+    for (int32_t c = 0; c < a.chunks; ++c) t += from[(int64_t)c * kGrads * a.C];
+    to[example * a.C + rest - k * a.C] = t;
+  }
+}
+
+// How a call is laid out: V elements a vector, nv vectors a thread, 2^log threads a
+// row, `threads` a workgroup.
+struct RnPlan {
+  int V, nv, log, threads, groups;
+  int iters;
+  int64_t wgs, chunks;
+};
+
+RnPlan plan_rows(const dpsgd_residual_norm& n) {
+  RnPlan p{};
+  p.V = vec_width(n.C, n.dtype == DPSGD_BF16 ? 8 : 4);
+  const int64_t units = n.C / p.V;
+  // As many vectors a thread as 16 elements hold, if that leaves a wave or more; wide
+  // rows of them to keep a row within 1024 threads.
+  p.nv = p.V >= 8 ? 2 : 4;
+  while (p.nv > 1 && units <= 64 * (p.nv / 2)) p.nv /= 2;
+  while (units > (int64_t)p.nv * kMostThreads) p.nv *= 2;
+  while (((int64_t)p.nv << p.log) < units) ++p.log;
+  p.threads = p.log <= 8 ? kThreads : 1 << p.log;
+  p.groups = p.threads >> p.log;
+  return p;
+}
+
+constexpr int64_t kForwardWgs = 4096, kBackwardWgs = 2048;
+
+RnPlan plan_forward(const dpsgd_residual_norm& n) {
+  RnPlan p = plan_rows(n);
+  const int64_t batches = ceil_div(n.B * n.S, p.groups);
+  p.iters = (int)ceil_div(batches, kForwardWgs);
+  p.wgs = ceil_div(batches, p.iters);
+  return p;
+}
+
+RnPlan plan_backward(const dpsgd_residual_norm& n) {
+  RnPlan p = plan_rows(n);
+  while (p.threads > 64 && p.groups > 1 && p.groups / 2 >= n.S) {   // few rows: smaller workgroups
+    p.threads /= 2;
+    p.groups /= 2;
+  }
+  const int64_t batches = ceil_div(n.S, p.groups);
+  const int64_t most = n.B >= kBackwardWgs ? 1 : ceil_div(kBackwardWgs, n.B);
+  p.iters = (int)ceil_div(batches, most < batches ? most : batches);
+  p.chunks = ceil_div(batches, p.iters);
+  p.wgs = n.B * p.chunks;
+  return p;
+}
+
+RnArgs common_args(const dpsgd_residual_norm& n, const RnPlan& p) {
+  RnArgs a{};
+  a.gamma = n.gamma;
+  a.beta = n.beta;
+  a.post_gamma = n.post_gamma;
+  a.post_beta = n.post_beta;
+  a.gate = n.gate;
+  a.rows = n.B * n.S;
+  a.S = n.S;
+  a.C = (int32_t)n.C;
+  a.log = p.log;
+  a.iters = p.iters;
+  a.chunks = (int32_t)p.chunks;
+  a.gate_per_example = n.gate && n.gate_per_example;
+  a.post = n.post ? 1 : 0;
+  a.layer = n.kind == DPSGD_ROW_NORM_LAYER;
+  a.alpha = n.residual_scale;
+  a.eps = n.eps;
+  a.inv_C = 1.0f / (float)n.C;
+  return a;
+}
+
+template <class T, int V, int NV, bool BACK>
+void run(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+  if (p.threads <= kThreads) {
+    if constexpr (BACK)
+      hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, kThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), lds, stream, a);
+    else
+      hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, kThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), 0, stream, a);
+  } else {
+    if constexpr (BACK)
+      hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, kMostThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), lds, stream, a);
+    else
+      hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, kMostThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), 0, stream, a);
+  }
+}
+
+template <class T, int V, bool BACK>
+void pick_vectors(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+  switch (p.nv) {
+    case 1: return run<T, V, 1, BACK>(p, a, lds, stream);
+    case 2: return run<T, V, 2, BACK>(p, a, lds, stream);
+    case 4:
+      if constexpr (V <= 4) return run<T, V, 4, BACK>(p, a, lds, stream);
+      return;
+    case 8:
+      if constexpr (V <= 2) return run<T, V, 8, BACK>(p, a, lds, stream);
+      return;
+    case 16:
+      if constexpr (V <= 1) return run<T, V, 16, BACK>(p, a, lds, stream);
+      return;
+  }
+}
+
+template <bool BACK>
+int launch(const dpsgd_residual_norm& n, const RnPlan& p, const RnArgs& a, size_t lds,
+           hipStream_t stream) {
+  if (!launchable(p.wgs, p.threads)) return DPSGD_ERR_INVALID_ARG;
+  if (n.dtype == DPSGD_BF16) {
+    switch (p.V) {
+      case 8: pick_vectors<uint16_t, 8, BACK>(p, a, lds, stream); break;
+      case 4: pick_vectors<uint16_t, 4, BACK>(p, a, lds, stream); break;
+      case 2: pick_vectors<uint16_t, 2, BACK>(p, a, lds, stream); break;
+      default: pick_vectors<uint16_t, 1, BACK>(p, a, lds, stream); break;
+    }
+  } else {
+    switch (p.V) {
+      case 4: pick_vectors<float, 4, BACK>(p, a, lds, stream); break;
+      case 2: pick_vectors<float, 2, BACK>(p, a, lds, stream); break;
+      default: pick_vectors<float, 1, BACK>(p, a, lds, stream); break;
+    }
+  }
+  return check_launch();
+}
+
+}  // namespace
+
+size_t residual_norm_workspace_bytes(const dpsgd_residual_norm& n) {
+  const RnPlan p = plan_backward(n);
+  const size_t bytes = p.chunks == 1 ? 0 : (size_t)p.wgs * kGrads * (size_t)n.C * sizeof(float);
+  return bytes + 16;
+}
+
+int launch_residual_norm_forward(const dpsgd_residual_norm& n, const void* x, const void* block,
+                                 void* r, void* y, float* stats, hipStream_t stream) {
+  const RnPlan p = plan_forward(n);
+  RnArgs a = common_args(n, p);
+  a.x = x;
+  a.block = block;
+  a.r = r;
+  a.y = y;
+  a.stats = stats;
+  return launch<false>(n, p, a, 0, stream);
+}
+
+int launch_residual_norm_backward(const dpsgd_residual_norm& n, const void* block, const void* r,
+                                  const void* dy, const void* dr, const float* stats, void* dx,
+                                  void* dblock, float* const* grads, void* workspace,
+                                  hipStream_t stream) {
+  const RnPlan p = plan_backward(n);
+  RnArgs a = common_args(n, p);
+  a.x = r;
+  a.block = block;
+  a.dy = dy;
+  a.dr = dr;
+  a.stats = const_cast<float*>(stats);
+  a.r = dx;
+  a.y = dblock;
+  a.partials = static_cast<float*>(workspace);
+  bool any = false;
+  for (int k = 0; k < kGrads; ++k) {
+    a.grads[k] = grads[k];
+    any = any || grads[k];
+  }
+  const size_t lds = any && p.groups > 1 ? (size_t)p.groups * (size_t)n.C * sizeof(float) : 0;
+  const int st = launch<true>(n, p, a, lds, stream);
+  if (st != DPSGD_OK || !any || p.chunks == 1) return st;
+  const int64_t total = n.B * kGrads * n.C, wgs = ceil_div(total, kThreads);
+  hipLaunchKernelGGL(rn_join_kernel, dim3((uint32_t)(wgs < 65536 ? wgs : 65536)), dim3(kThreads), 0,
+                     stream, a, total);
+  return check_launch();
+}
+
+}  // namespace dpsgd

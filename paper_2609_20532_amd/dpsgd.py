@@ -34,6 +34,15 @@ DPSGD_ACT_GELU = 3
 ACTIVATIONS = {"none": DPSGD_ACT_NONE, "relu": DPSGD_ACT_RELU, "silu": DPSGD_ACT_SILU,
                "gelu": DPSGD_ACT_GELU}
 
+DPSGD_MOST_ALTERNATIVES = 64   # of dpsgd_token_logprobs
+DPSGD_ROW_NORM_LAYER = 0
+DPSGD_ROW_NORM_RMS = 1
+#: Norms over rows by name.
+ROW_NORMS = {"layer": DPSGD_ROW_NORM_LAYER, "rms": DPSGD_ROW_NORM_RMS}
+DPSGD_STATE_BLOCK = 256        # entries that share the exponents of 8-bit moments
+DPSGD_ROUND_NEAREST = 0
+DPSGD_ROUND_STOCHASTIC = 1
+
 DPSGD_OK = 0
 DPSGD_ERR_INVALID_ARG = -1
 DPSGD_ERR_UNSUPPORTED = -2
@@ -53,6 +62,10 @@ EXPORTED = (
     "dpsgd_embedding_clip_accumulate", "dpsgd_group_norm_workspace_bytes",
     "dpsgd_group_norm_forward", "dpsgd_group_norm_backward", "dpsgd_global_norm_workspace_bytes",
     "dpsgd_global_norm_multi", "dpsgd_global_clip_multi",
+    "dpsgd_token_workspace_bytes", "dpsgd_token_logprobs", "dpsgd_token_logprobs_backward",
+    "dpsgd_token_loss", "dpsgd_residual_norm_forward", "dpsgd_residual_norm_workspace_bytes",
+    "dpsgd_residual_norm_backward", "dpsgd_noise_adamw8_multi", "dpsgd_adamw8_pack_multi",
+    "dpsgd_adamw8_unpack_multi",
 )
 
 
@@ -112,6 +125,38 @@ class dpsgd_group_norm(ctypes.Structure):  # noqa: N801 - mirrors the C struct n
     ]
 
 
+class dpsgd_logits(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
+    _fields_ = [
+        ("targets", ctypes.c_void_p),
+        ("B", ctypes.c_int64),
+        ("T", ctypes.c_int64),
+        ("V", ctypes.c_int64),
+        ("stride", ctypes.c_int64),
+        ("index_dtype", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+    ]
+
+
+class dpsgd_residual_norm(ctypes.Structure):  # noqa: N801 - mirrors the C struct name
+    _fields_ = [
+        ("B", ctypes.c_int64),
+        ("S", ctypes.c_int64),
+        ("C", ctypes.c_int64),
+        ("gamma", ctypes.c_void_p),
+        ("beta", ctypes.c_void_p),
+        ("post_gamma", ctypes.c_void_p),
+        ("post_beta", ctypes.c_void_p),
+        ("gate", ctypes.c_void_p),
+        ("gate_per_example", ctypes.c_int32),
+        ("post", ctypes.c_int32),
+        ("kind", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("residual_scale", ctypes.c_float),
+        ("eps", ctypes.c_float),
+    ]
+
+
 _lib = None
 
 
@@ -119,6 +164,7 @@ def _declare(lib):
     P = ctypes.POINTER
     L = P(dpsgd_layer)
     E, N = P(dpsgd_embedding), P(dpsgd_group_norm)
+    K, R = P(dpsgd_logits), P(dpsgd_residual_norm)
     vp, i32, i64, u32, u64, f32, sz = (ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64,
                                        ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float,
                                        ctypes.c_size_t)
@@ -155,6 +201,18 @@ def _declare(lib):
         "dpsgd_global_norm_workspace_bytes": (sz, [L, i32]),
         "dpsgd_global_norm_multi": (ctypes.c_int, [L, i32, P(vp), vp, vp, sz, vp]),
         "dpsgd_global_clip_multi": (ctypes.c_int, [L, i32, P(vp), P(vp), f32, vp, vp, vp, sz, vp]),
+        "dpsgd_token_workspace_bytes": (sz, [K, i32]),
+        "dpsgd_token_logprobs": (ctypes.c_int, [K, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]),
+        "dpsgd_token_logprobs_backward": (ctypes.c_int, [K, vp, vp, vp, vp, vp, vp, vp, i64, vp]),
+        "dpsgd_token_loss": (ctypes.c_int, [K, vp, vp, vp, vp, vp, i64, vp, sz, vp]),
+        "dpsgd_residual_norm_forward": (ctypes.c_int, [R, vp, vp, vp, vp, vp, vp]),
+        "dpsgd_residual_norm_workspace_bytes": (sz, [R]),
+        "dpsgd_residual_norm_backward": (ctypes.c_int, [R] + [vp] * 13 + [sz, vp]),
+        "dpsgd_noise_adamw8_multi": (ctypes.c_int, [L, i32, P(vp), P(vp), P(vp), P(vp), P(vp),
+                                                    P(vp), f32, f32, u64, u32, f32,
+                                                    P(dpsgd_adamw), i32, u64, vp]),
+        "dpsgd_adamw8_pack_multi": (ctypes.c_int, [L, i32] + [P(vp)] * 5 + [vp]),
+        "dpsgd_adamw8_unpack_multi": (ctypes.c_int, [L, i32] + [P(vp)] * 5 + [i32, vp]),
         "dpsgd_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "dpsgd_version": (ctypes.c_int, []),
     }
@@ -627,6 +685,278 @@ def dpsgd_global_clip_multi(layers, grads, outs, max_norm: float, norm_out=None,
                                      _scalar("factor_out", factor_out), *_workspace(workspace),
                                      _stream(stream))
     _check("dpsgd_global_clip_multi", st)
+
+
+# -------------------------------------- between and behind the blocks
+
+
+def _here(name, t):
+    """Raises ValueError unless t is on the current device, whose stream the calls use."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    import torch
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} is on {t.device}, which is not the current device")
+
+
+def _logit_rows(name, t):
+    """B, T, V and the entries from a row to the next of logits [B, T, V]."""
+    if t.dim() != 3 or t.numel() == 0:
+        raise ValueError(f"{name} must be [B, T, V] with no empty axis")
+    B, T, V = t.shape
+    sB, sT, sV = t.stride()
+    stride = sT if T > 1 else (sB if B > 1 else V)
+    if (V > 1 and sV != 1) or stride < V or (B > 1 and T > 1 and sB != T * sT):
+        raise ValueError(f"{name}: entries of a row must be neighbours, and rows evenly spaced")
+    return B, T, V, stride
+
+
+def make_logits(logits, targets=None, scale: float = 1.0) -> dpsgd_logits:
+    """Descriptor of logits [B, T, V] (float32 or bfloat16; a view such as x[..., :V] or
+    x[:, -1:] is taken as it lies) and the token of each position, targets [B, T] (int32
+    or int64, contiguous; one outside [0, V) is an empty position), or None. scale is 1 /
+    temperature. The descriptor keeps targets alive, and is for logits of this layout."""
+    _here("logits", logits)
+    B, T, V, stride = _logit_rows("logits", logits)
+    at, code = None, "i64"
+    if targets is not None:
+        code = _types().get(targets.dtype)
+        if code != "i32" and code != "i64":
+            raise ValueError("targets must be [B, T], int32 or int64")
+        _here("targets", targets)
+        at = _want("targets", targets, (B, T))
+    desc = dpsgd_logits(at, B, T, V, stride, DPSGD_I64 if code == "i64" else DPSGD_I32,
+                        _dtype_of(logits), scale)
+    desc.keep = targets
+    return desc
+
+
+def _want_logits(name, t, desc, stride=None):
+    """The address of t, rows like the descriptor's, and the entries from row to row."""
+    _here(name, t)
+    B, T, V, s = _logit_rows(name, t)
+    if (B, T, V) != (desc.B, desc.T, desc.V) or (stride is not None and s != stride):
+        raise ValueError(f"{name} must be [{desc.B}, {desc.T}, {desc.V}] as the descriptor has it")
+    if _dtype_of(t) != desc.dtype:
+        raise ValueError(f"{name} has another dtype than the descriptor")
+    return t.data_ptr(), s
+
+
+def dpsgd_token_workspace_bytes(desc: dpsgd_logits, k: int = 0) -> int:
+    return int((_lib or load()).dpsgd_token_workspace_bytes(desc, k))
+
+
+def dpsgd_token_logprobs(desc: dpsgd_logits, logits, logprobs=None, lse=None, entropy=None,
+                         top_ids=None, top_logprobs=None, workspace=None, stream=None):
+    """Any of the outputs; top_ids (int64) and top_logprobs are [B, T, k]."""
+    lib = _lib or load()
+    rows, k = (desc.B, desc.T), 0
+    for t in (top_ids, top_logprobs):
+        if t is not None:
+            k = t.shape[-1]
+            if k == 0:
+                raise ValueError("no alternatives: leave top_ids and top_logprobs out")
+    p, _ = _want_logits("logits", logits, desc, desc.stride)
+    st = lib.dpsgd_token_logprobs(
+        desc, p, _may_want("logprobs", logprobs, rows, DPSGD_F32),
+        _may_want("lse", lse, rows, DPSGD_F32), _may_want("entropy", entropy, rows, DPSGD_F32), k,
+        _may_want("top_ids", top_ids, (*rows, k), "i64"),
+        _may_want("top_logprobs", top_logprobs, (*rows, k), DPSGD_F32), *_workspace(workspace),
+        _stream(stream))
+    _check("dpsgd_token_logprobs", st)
+
+
+def dpsgd_token_logprobs_backward(desc: dpsgd_logits, logits, lse, dlogits, entropy=None,
+                                  grad_logprobs=None, grad_lse=None, grad_entropy=None,
+                                  stream=None):
+    """dlogits may be logits."""
+    lib = _lib or load()
+    rows = (desc.B, desc.T)
+    p, _ = _want_logits("logits", logits, desc, desc.stride)
+    g, g_stride = _want_logits("dlogits", dlogits, desc)
+    st = lib.dpsgd_token_logprobs_backward(
+        desc, p, _want("lse", lse, rows, DPSGD_F32),
+        _may_want("entropy", entropy, rows, DPSGD_F32),
+        _may_want("grad_logprobs", grad_logprobs, rows, DPSGD_F32),
+        _may_want("grad_lse", grad_lse, rows, DPSGD_F32),
+        _may_want("grad_entropy", grad_entropy, rows, DPSGD_F32), g, g_stride, _stream(stream))
+    _check("dpsgd_token_logprobs_backward", st)
+
+
+def dpsgd_token_loss(desc: dpsgd_logits, logits, dlogits, losses=None, weights=None, logprobs=None,
+                     workspace=None, stream=None):
+    """Per-example losses [B] and the gradient of their sum; dlogits may be logits."""
+    lib = _lib or load()
+    rows = (desc.B, desc.T)
+    p, _ = _want_logits("logits", logits, desc, desc.stride)
+    g, g_stride = _want_logits("dlogits", dlogits, desc)
+    st = lib.dpsgd_token_loss(
+        desc, p, _may_want("weights", weights, rows, DPSGD_F32),
+        _may_want("losses", losses, (desc.B,), DPSGD_F32),
+        _may_want("logprobs", logprobs, rows, DPSGD_F32), g, g_stride, *_workspace(workspace),
+        _stream(stream))
+    _check("dpsgd_token_loss", st)
+
+
+def make_residual_norm(x, kind: str = "layer", gamma=None, beta=None, gate=None, post: bool = False,
+                       post_gamma=None, post_beta=None, residual_scale: float = 1.0,
+                       eps: float = 1e-5) -> dpsgd_residual_norm:
+    """Descriptor of the residual sum and norms over rows like x's, [B, ..., C] (every
+    axis between the first and the last is a position). kind: a name of ROW_NORMS. gate
+    is [C] or, one for each example, [B, C]. The descriptor keeps the parameters alive."""
+    shape, n = x.shape, x.numel()
+    if len(shape) < 2 or n == 0:
+        raise ValueError("x must be [B, ..., C] with no empty axis")
+    if kind not in ROW_NORMS:
+        raise ValueError(f"kind must be one of {sorted(ROW_NORMS)}")
+    B, C = shape[0], shape[-1]
+    each = gate is not None and gate.dim() == 2
+    affine = (gamma, beta, post_gamma, post_beta)
+    for name, t in zip(("gamma", "beta", "post_gamma", "post_beta", "gate"), (*affine, gate)):
+        if t is not None:
+            _here(name, t)
+    desc = dpsgd_residual_norm(
+        B, n // (B * C), C, *(_may_want(name, t, (C,), DPSGD_F32) for name, t in
+                              zip(("gamma", "beta", "post_gamma", "post_beta"), affine)),
+        _may_want("gate", gate, (B, C) if each else (C,), DPSGD_F32), int(each), int(bool(post)),
+        ROW_NORMS[kind], _dtype_of(x), residual_scale, eps)
+    desc.keep = (*affine, gate)
+    return desc
+
+
+def _may_want_rows(name, t, desc):
+    if t is None:
+        return None
+    _here(name, t)
+    return _want_rows(name, t, desc.B, desc.C, desc.B * desc.S * desc.C, desc.dtype)
+
+
+def _want_stats(stats, desc):
+    return _may_want("stats", stats, (desc.B, desc.S, 4), DPSGD_F32)
+
+
+def dpsgd_residual_norm_forward(desc: dpsgd_residual_norm, x, block, r, y, stats=None, stream=None):
+    """block None: r = residual_scale x; r None: not written. stats: [B, S, 4]."""
+    lib = _lib or load()
+    _types()
+    st = lib.dpsgd_residual_norm_forward(
+        desc, _may_want_rows("x", x, desc), _may_want_rows("block", block, desc),
+        _may_want_rows("r", r, desc), _may_want_rows("y", y, desc), _want_stats(stats, desc),
+        _stream(stream))
+    _check("dpsgd_residual_norm_forward", st)
+
+
+def dpsgd_residual_norm_workspace_bytes(desc: dpsgd_residual_norm) -> int:
+    return int((_lib or load()).dpsgd_residual_norm_workspace_bytes(desc))
+
+
+def dpsgd_residual_norm_backward(desc: dpsgd_residual_norm, block, r, dy, dr, stats, dx=None,
+                                 dblock=None, dgamma=None, dbeta=None, dgate=None,
+                                 dpost_gamma=None, dpost_beta=None, workspace=None, stream=None):
+    """The gradients of the affine parameters are per example ([B, C]); affine_layer
+    makes layers of them. Any of the results may be left out (dblock with block)."""
+    lib = _lib or load()
+    _types()
+    affine = (desc.B, desc.C)
+    st = lib.dpsgd_residual_norm_backward(
+        desc, *(_may_want_rows(name, t, desc) for name, t in
+                (("block", block), ("r", r), ("dy", dy), ("dr", dr))), _want_stats(stats, desc),
+        _may_want_rows("dx", dx, desc), _may_want_rows("dblock", dblock, desc),
+        *(_may_want(name, t, affine, DPSGD_F32) for name, t in
+          (("dgamma", dgamma), ("dbeta", dbeta), ("dgate", dgate), ("dpost_gamma", dpost_gamma),
+           ("dpost_beta", dpost_beta))), *_workspace(workspace), _stream(stream))
+    _check("dpsgd_residual_norm_backward", st)
+
+
+def make_states8(layers, device="cuda"):
+    """8-bit moments of 0 for the layers' tensors: exp_avgs, exp_avg_sqs (uint8 [d_out,
+    d_in]) and exponents (uint8 [ceil(d_out d_in / 256), 2])."""
+    import torch
+    ms, vs, exps = [], [], []
+    for L in [layers] if isinstance(layers, dpsgd_layer) else layers:
+        for to in (ms, vs):
+            to.append(torch.zeros(L.d_out, L.d_in, dtype=torch.uint8, device=device))
+        exps.append(torch.zeros(-(-L.d_out * L.d_in // DPSGD_STATE_BLOCK), 2, dtype=torch.uint8,
+                                device=device))
+    return ms, vs, exps
+
+
+def _tensors(name, tensors, sizes, dtype):
+    """The addresses of contiguous tensors on the current device with this torch dtype and
+    these numbers of entries."""
+    if len(tensors) != len(sizes):
+        raise ValueError(f"{name}: {len(sizes)} tensors expected, not {len(tensors)}")
+    import torch
+    arr, here = (ctypes.c_void_p * len(sizes))(), -1
+    for k, (t, n) in enumerate(zip(tensors, sizes)):
+        if t.dtype is not dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name}[{k}] must be a contiguous {dtype} device tensor of {n} entries")
+        here = torch.cuda.current_device() if here < 0 else here
+        if t.device.index != here:
+            raise ValueError(f"{name}[{k}] is on {t.device}, which is not the current device")
+        arr[k] = t.data_ptr()
+    return arr
+
+
+def _states8(exp_avgs, exp_avg_sqs, exponents, sizes):
+    import torch
+    blocks = [2 * -(-n // DPSGD_STATE_BLOCK) for n in sizes]
+    return (_tensors("exp_avgs", exp_avgs, sizes, torch.uint8),
+            _tensors("exp_avg_sqs", exp_avg_sqs, sizes, torch.uint8),
+            _tensors("exponents", exponents, blocks, torch.uint8))
+
+
+def dpsgd_noise_adamw8_multi(layers, grads, params, exp_avgs, exp_avg_sqs, exponents, sigma, C,
+                             seed, step, scale, opt, round_seed=None, noisy_outs=None,
+                             stream=None):
+    """round_seed: of stochastic rounding of the moments; None rounds to nearest."""
+    lib = _lib or load()
+    import torch
+    arr, n = _array(layers)
+    sizes = _sizes(layers)
+    noisy = None
+    if noisy_outs is not None:
+        there = [k for k, t in enumerate(noisy_outs) if t is not None]
+        _tensors("noisy_outs", [noisy_outs[k] for k in there], [sizes[k] for k in there], torch.float32)
+        if len(noisy_outs) != n:
+            raise ValueError(f"noisy_outs: {n} entries expected, not {len(noisy_outs)}")
+        noisy = _ptr_array(noisy_outs)
+    st = lib.dpsgd_noise_adamw8_multi(
+        arr, n, _tensors("grads", grads, sizes, torch.float32),
+        _tensors("params", params, sizes, torch.float32),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes), noisy, sigma, C, seed, step, scale,
+        ctypes.byref(opt), DPSGD_ROUND_NEAREST if round_seed is None else DPSGD_ROUND_STOCHASTIC,
+        0 if round_seed is None else round_seed, _stream(stream))
+    _check("dpsgd_noise_adamw8_multi", st)
+
+
+def dpsgd_adamw8_pack_multi(layers, exp_avgs_in, exp_avg_sqs_in, exp_avgs, exp_avg_sqs, exponents,
+                            stream=None):
+    """float32 moments to 8 bits."""
+    lib = _lib or load()
+    import torch
+    arr, n = _array(layers)
+    sizes = _sizes(layers)
+    st = lib.dpsgd_adamw8_pack_multi(
+        arr, n, _tensors("exp_avgs_in", exp_avgs_in, sizes, torch.float32),
+        _tensors("exp_avg_sqs_in", exp_avg_sqs_in, sizes, torch.float32),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes), _stream(stream))
+    _check("dpsgd_adamw8_pack_multi", st)
+
+
+def dpsgd_adamw8_unpack_multi(layers, exp_avgs, exp_avg_sqs, exponents, exp_avgs_out,
+                              exp_avg_sqs_out, stream=None):
+    """The moments that 8-bit states stand for, all float32 or all bfloat16 (both exact)."""
+    lib = _lib or load()
+    arr, n = _array(layers)
+    sizes = _sizes(layers)
+    dtype = exp_avgs_out[0].dtype
+    code = _dtype_of(exp_avgs_out[0])
+    st = lib.dpsgd_adamw8_unpack_multi(
+        arr, n, *_states8(exp_avgs, exp_avg_sqs, exponents, sizes),
+        _tensors("exp_avgs_out", exp_avgs_out, sizes, dtype),
+        _tensors("exp_avg_sqs_out", exp_avg_sqs_out, sizes, dtype), code, _stream(stream))
+    _check("dpsgd_adamw8_unpack_multi", st)
 
 
 # ------------------------------------------------------------ whole step
