@@ -17,7 +17,7 @@
 namespace dpsgd {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int64_t kMostWgs = 1 << 20;
 
 struct TokenArgs {
@@ -74,137 +74,640 @@ __device__ __forceinline__ uint64_t order_of(float x, int32_t v) {
   return (uint64_t)o << 32 | (uint32_t)~v;
 }
 
-__device__ __forceinline__ float block_max(float v, float* red) {
-#pragma unroll
-  for (int off = 32; off >= 1; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  const float r = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  __syncthreads();
-  return r;
+// Largest value of the wave in every lane (a NaN is passed over).
+__device__ __forceinline__ float wave_max(float v) {
+#define DPSGD_DPP_MAX(ctrl, rows)                                                                 \
+  v = fmaxf(v, __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v),   \
+                                                          ctrl, rows, 0xf, false)))
+  DPSGD_DPP_MAX(0x111, 0xf);   // row_shr 1, 2, 4, 8
+  DPSGD_DPP_MAX(0x112, 0xf);
+  DPSGD_DPP_MAX(0x114, 0xf);
+  DPSGD_DPP_MAX(0x118, 0xf);
+  DPSGD_DPP_MAX(0x142, 0xa);   // row_bcast 15, 31
+  DPSGD_DPP_MAX(0x143, 0xc);
+#undef DPSGD_DPP_MAX
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-__device__ __forceinline__ uint64_t block_max_u64(uint64_t v, uint64_t* red) {
+__device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) {
     const uint64_t o = (uint64_t)__shfl_xor((unsigned long long)v, off, 64);
     v = o > v ? o : v;
   }
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-  __syncthreads();
-  uint64_t r = red[0];
-  for (int w = 1; w < 4; ++w) r = red[w] > r ? red[w] : r;
-  __syncthreads();
-  return r;
+  return v;
 }
 
-// A row's statistics.
-struct RowStats {
-  float m, sum, log_sum, entropy;
-  bool nan, none;   // NaN or +inf; all -inf
+// n entries in a row from an address of any alignment, in the registers of NT
+// threads: vectors of 16 bytes between the first and the last 16-byte boundary, and
+// the entries before and after them, one a thread. Places without an entry hold -inf.
+template <class T, int NT, int NVEC>
+struct Held {
+  static constexpr int VE = 16 / (int)sizeof(T);
+  static constexpr int kMost = NT * NVEC * VE;   // entries that always fit
+  Raw<T, VE> raw[NVEC];
+  float edge;
+  int32_t edge_at;   // -1: none
+  int32_t head, vecs;
+
+  __device__ __forceinline__ void load(const T* x, int32_t n, int32_t tid) {
+    head = (int32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int32_t)sizeof(T);
+    head = head < n ? head : n;
+    vecs = (n - head) / VE;
+    const int32_t tail = n - head - vecs * VE;
+    edge_at = tid < head ? tid : (tid - head < tail ? n - tail + tid - head : -1);
+#pragma unroll
+    for (int j = 0; j < NVEC; ++j) {
+#pragma unroll
+      for (uint32_t& w : raw[j].w) w = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+      if (j * NT + tid < vecs) raw[j].load(x + head + (j * NT + tid) * VE);
+    }
+    edge = edge_at >= 0 ? entry(x, edge_at) : -INFINITY;
+  }
+
+  // f(x) for every entry of the thread, and for places without one.
+  template <class F>
+  __device__ __forceinline__ void each(F f) const {
+#pragma unroll
+    for (int j = 0; j < NVEC; ++j) {
+      if (j * NT < vecs) {
+        float x[VE];
+        raw[j].widen(x);
+#pragma unroll
+        for (int c = 0; c < VE; ++c) f(x[c]);
+      }
+    }
+    f(edge);
+  }
+
+  // f(x, place in the row) for the entries x >= least.
+  template <class F>
+  __device__ __forceinline__ void each_from(float least, int32_t tid, F f) const {
+#pragma unroll
+    for (int j = 0; j < NVEC; ++j) {
+      if (j * NT + tid < vecs) {
+        float x[VE];
+        raw[j].widen(x);
+#pragma unroll
+        for (int c = 0; c < VE; ++c)
+          if (x[c] >= least) f(x[c], head + (j * NT + tid) * VE + c);
+      }
+    }
+    if (edge >= least && edge_at >= 0) f(edge, edge_at);
+  }
+
+  __device__ __forceinline__ void keep_raw() {
+#pragma unroll
+    for (int j = 0; j < NVEC; ++j) raw[j].keep_raw();
+  }
 };
 
-template <class T>
-__device__ __forceinline__ RowStats stats_of(const TokenArgs& a, const T* x, float* red) {
-  float m = -INFINITY;
-  for (int32_t v = threadIdx.x; v < a.V; v += kThreads) m = fmaxf(m, a.scale * entry(x, v));
-  m = block_max(m, red);
-  const float m0 = m == -INFINITY ? 0.0f : m;
-  float s = 0.0f, e = 0.0f;
-  for (int32_t v = threadIdx.x; v < a.V; v += kThreads) {
-    const float d = a.scale * entry(x, v) - m0, p = exp_of(d);
-    s += p;
-    e += p == 0.0f ? 0.0f : p * d;
+// Reductions over the NT threads of a row (a wave of its own, or a workgroup). With a
+// workgroup every thread has to call them, and `slot` goes from call to call between
+// two places, so that one barrier a call is enough.
+template <int NT>
+struct Team {
+  float (*red)[NT / 64][2];   // [2]
+  int slot;
+
+  __device__ __forceinline__ float max(float v) {
+    v = wave_max(v);
+    if constexpr (NT == 64) return v;
+    if ((threadIdx.x & 63) == 0) red[slot][threadIdx.x >> 6][0] = v;
+    __syncthreads();
+    float r = red[slot][0][0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) r = fmaxf(r, red[slot][w][0]);
+    slot ^= 1;
+    return r;
   }
-  s = block_sum(s, red);
-  e = block_sum(e, red);
-  RowStats st;
-  st.nan = !(s == s) || m == INFINITY;
-  st.none = !st.nan && m == -INFINITY;
-  st.m = m;
-  st.sum = s;
-  st.log_sum = logf(s);
-  st.entropy = st.nan ? NAN : (st.none ? 0.0f : st.log_sum - e / s);
-  return st;
+
+  __device__ __forceinline__ void sum(float& a, float& b) {
+    a = wave_total(a);
+    b = wave_total(b);
+    if constexpr (NT == 64) return;
+    if ((threadIdx.x & 63) == 0) {
+      red[slot][threadIdx.x >> 6][0] = a;
+      red[slot][threadIdx.x >> 6][1] = b;
+    }
+    __syncthreads();
+    a = b = 0.0f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+      a += red[slot][w][0];
+      b += red[slot][w][1];
+    }
+    slot ^= 1;
+  }
+
+  __device__ __forceinline__ void barrier() {
+    if constexpr (NT == 64) {   // LDS accesses of one wave stay in order; so has the compiler to
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    } else {
+      __syncthreads();
+    }
+  }
+};
+
+// The exponents (base 2) of a row's entries relative to its largest one, top. Near 0
+// they are one multiply-add, x c - top c: the product's rounding, `off`, is the same
+// for all entries, at most 2^-4, and is taken back where it matters. For |top c| above
+// 2^20 that would not do, and z - m is formed from the rounded products.
+struct Exponents {
+  float scale, m, c, top_c, off;
+  bool near;
+
+  __device__ __forceinline__ Exponents(float scale_, float top) {
+    scale = scale_;
+    m = top == -INFINITY ? 0.0f : scale * top;
+    c = scale * kLog2e;
+    top_c = top * c;
+    near = fabsf(top_c) <= 1048576.0f;
+    off = near ? fmaf(top, c, -top_c) : 0.0f;
+  }
+  template <bool NEAR>
+  __device__ __forceinline__ float at(float x) const {
+    return NEAR ? fmaf(x, c, -top_c) : (scale * x - m) * kLog2e;
+  }
+};
+
+// S and E of the entries, both relative to the exact largest one: S = sum 2^t, E =
+// sum 2^t t.
+template <bool NEAR, bool ENTROPY, class H>
+__device__ __forceinline__ void sums_of(const H& held, const Exponents& ex, float& S, float& E) {
+  S = E = 0.0f;
+  held.each([&](float x) {
+    const float t = ex.at<NEAR>(x), p = __builtin_amdgcn_exp2f(t);
+    S += p;
+    if constexpr (ENTROPY) E = fmaf(p, fmaxf(t, -256.0f), E);   // 0 for -inf; a NaN is in p
+  });
 }
 
-__device__ __forceinline__ float logp_of(const RowStats& st, float z) {
-  return st.nan ? NAN : (st.none ? -INFINITY : (z - st.m) - st.log_sum);
+// What a row's (or a part's) sums say.
+struct RowStats {
+  float top, m, S, E, log_S;   // largest logit and scale times it
+  bool nan, none;
+
+  __device__ __forceinline__ RowStats(float scale, float top_, float S_, float E_) {
+    top = top_;
+    m = scale * top;
+    S = S_;
+    E = E_;
+    nan = !(S == S) || top == INFINITY;
+    none = !nan && top == -INFINITY;
+    log_S = logf(S);
+  }
+  __device__ __forceinline__ float lse() const { return nan ? NAN : (none ? -INFINITY : m + log_S); }
+  __device__ __forceinline__ float entropy() const {
+    return nan ? NAN : (none ? 0.0f : log_S - kLn2 * (E / S));
+  }
+  __device__ __forceinline__ float logp(float z) const {
+    return nan ? NAN : (none ? -INFINITY : (z - m) - log_S);
+  }
+};
+
+template <class Tm, class H>
+__device__ __forceinline__ void reduce_row(Tm& team, const H& held, float scale, bool entropy,
+                                           float& top, float& S, float& E, float& mine) {
+  mine = -INFINITY;
+  held.each([&](float x) { mine = fmaxf(mine, x); });
+  top = team.max(mine);
+  const Exponents ex(scale, top);
+  if (ex.near) {
+    if (entropy) sums_of<true, true>(held, ex, S, E); else sums_of<true, false>(held, ex, S, E);
+  } else {
+    if (entropy) sums_of<false, true>(held, ex, S, E); else sums_of<false, false>(held, ex, S, E);
+  }
+  team.sum(S, E);
+  E = fmaf(-ex.off, S, E);
+  const float back = __builtin_amdgcn_exp2f(-ex.off);
+  S *= back;
+  E *= back;
+}
+
+constexpr int kListed = 1024;       // candidates that a workgroup's list holds
+constexpr int kListedWave = 256;    // that a wave's list holds
+
+// Where the most likely entries of a row are collected.
+template <int NT>
+struct TopLds {
+  static constexpr int kMost = NT == 64 ? kListedWave : kListed;
+  uint64_t key[kMost];
+  uint32_t group[64];
+  uint32_t least;
+  int32_t count;
+};
+
+__device__ __forceinline__ uint32_t order_bits(float x) { return (uint32_t)(order_of(x, 0) >> 32); }
+__device__ __forceinline__ float logit_of(uint64_t order) {
+  const uint32_t o = (uint32_t)(order >> 32);
+  return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
+}
+
+// The k largest entries in order: put(i, order) for i < the number that there are.
+// The threads' largest ones, joined to 64 groups, give a bound: the k-th largest of
+// the groups' is not above the k-th largest entry, and few entries are above it. Those
+// are listed, and each finds its place by counting the larger ones. `first` is added to
+// the entries' places. Where the list is too short (many equal or sorted logits) the
+// entries are taken one by one.
+template <int NT, class H, class P>
+__device__ __forceinline__ int32_t top_entries(Team<NT>& team, const H& held, float mine, int32_t k,
+                                               int32_t first, TopLds<NT>& lds, uint64_t* red64, P put) {
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  constexpr int kLanes = NT / 64;   // threads of a group
+  uint32_t g = order_bits(mine);
+#pragma unroll
+  for (int off = 1; off < kLanes; off <<= 1) {
+    const uint32_t o = (uint32_t)__shfl_xor((int)g, off, 64);
+    g = o > g ? o : g;
+  }
+  if (tid % kLanes == 0) lds.group[tid / kLanes] = g;
+  if (tid == 0) lds.count = 0;
+  team.barrier();
+  if (tid < 64) {
+    const uint32_t own = lds.group[tid];
+    int rank = 0;
+#pragma unroll
+    for (int j = 0; j < 64; ++j) {
+      const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)own, j);
+      rank += o > own || (o == own && j < tid) ? 1 : 0;
+    }
+    if (rank == k - 1) lds.least = own;
+  }
+  team.barrier();
+  // Entries of -inf are none.
+  const uint32_t none = order_bits(-INFINITY);
+  const uint32_t least = lds.least > none ? lds.least : none + 1;
+  if (order_bits(mine) >= least) {
+    held.each_from(logit_of((uint64_t)least << 32), tid, [&](float x, int32_t v) {
+      const int32_t at = atomicAdd(&lds.count, 1);
+      if (at < TopLds<NT>::kMost) lds.key[at] = order_of(x, first + v);
+    });
+  }
+  team.barrier();
+  const int32_t n = lds.count;
+  int32_t found;
+  if (n <= TopLds<NT>::kMost) {
+    for (int32_t i = tid; i < n; i += NT) {
+      const uint64_t own = lds.key[i];
+      int32_t rank = 0;
+#pragma unroll 4
+      for (int32_t j = 0; j < n; ++j) rank += lds.key[j] > own ? 1 : 0;
+      if (rank < k) put(rank, own);
+    }
+    found = n < k ? n : k;
+  } else {
+    uint64_t last = ~(uint64_t)0;
+    for (found = 0; found < k; ++found) {
+      uint64_t best = 0;
+      held.each_from(-3.402823466e38f, tid, [&](float x, int32_t v) {
+        const uint64_t o = order_of(x, first + v);
+        if (o < last && o > best) best = o;
+      });
+      best = wave_max_u64(best);
+      if constexpr (NT > 64) {
+        if ((threadIdx.x & 63) == 0) red64[threadIdx.x >> 6] = best;
+        __syncthreads();
+        for (int w = 0; w < NT / 64; ++w) best = red64[w] > best ? red64[w] : best;
+        __syncthreads();
+      }
+      if (best == 0) break;
+      if (tid == 0) put(found, best);
+      last = best;
+    }
+  }
+  team.barrier();   // the lists may be written again
+  return found;
+}
+
+// Alternatives from place `from` on that there are none of.
+__device__ __forceinline__ void fill_top(const TokenArgs& a, int64_t row, int32_t from, int32_t step,
+                                         bool nan) {
+  for (int32_t i = from; i < a.k; i += step) {
+    if (a.top_ids) a.top_ids[row * a.k + i] = -1;
+    if (a.top_logprobs) a.top_logprobs[row * a.k + i] = nan ? NAN : -INFINITY;
+  }
 }
 
 template <class T>
-__global__ __launch_bounds__(kThreads) void token_row_kernel(TokenArgs a) {
-  __shared__ float red[4];
-  __shared__ uint64_t red64[4];
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+__device__ __forceinline__ void write_zeros(T* g, int32_t n, int32_t tid, int32_t threads) {
+  constexpr int VE = 16 / (int)sizeof(T);
+  int32_t head = (int32_t)((16 - (reinterpret_cast<uintptr_t>(g) & 15)) & 15) / (int32_t)sizeof(T);
+  head = head < n ? head : n;
+  const int32_t vecs = (n - head) / VE, tail = n - head - vecs * VE;
+  const float zero[VE] = {};
+  for (int32_t j = tid; j < vecs; j += threads) store_vec<VE>(g + head + j * VE, zero);
+  if (tid < head) put(g, tid, 0.0f);
+  if (tid >= head && tid - head < tail) put(g, n - tail + tid - head, 0.0f);
+}
+
+// value(x) of entries in registers to g, `add` added at the target (a place among them,
+// or any other number: it is not there).
+template <class T, int NT, int NVEC, class F>
+__device__ __forceinline__ void write_entries(const Held<T, NT, NVEC>& held, const T* x, T* g, int32_t tid,
+                                              int32_t target, float add, F value) {
+  constexpr int VE = Held<T, NT, NVEC>::VE;
+  const int32_t rel = target - held.head, vec = rel >= 0 && rel < held.vecs * VE ? rel / VE : -1;
+  const int32_t at_j = vec >= 0 && vec % NT == tid ? vec / NT : -1;   // where this thread has the target
+  const bool same = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(g)) & 15) == 0;
+#pragma unroll
+  for (int j = 0; j < NVEC; ++j) {
+    if (j * NT + tid < held.vecs) {
+      float v[VE];
+      held.raw[j].widen(v);
+#pragma unroll
+      for (int c = 0; c < VE; ++c) v[c] = value(v[c]);
+      if (j == at_j) {
+#pragma unroll
+        for (int c = 0; c < VE; ++c) v[c] += c == rel % VE ? add : 0.0f;
+      }
+      T* to = g + held.head + (j * NT + tid) * VE;
+      if (same) {
+        store_vec<VE>(to, v);
+      } else {
+#pragma unroll
+        for (int c = 0; c < VE; ++c) put(to, c, v[c]);
+      }
+    }
+  }
+  if (held.edge_at >= 0) put(g, held.edge_at, value(held.edge) + (held.edge_at == target ? add : 0.0f));
+}
+
+// scale w (p_v - [v = target]) of n entries in registers, of a row with these sums.
+template <class T, int NT, int NVEC>
+__device__ __forceinline__ void write_gradient(const Held<T, NT, NVEC>& held, const T* x, T* g, int32_t n,
+                                               int32_t tid, int32_t target, float w, float scale,
+                                               const RowStats& st) {
+  if (w == 0.0f || st.none) return write_zeros(g, n, tid, NT);
+  const Exponents ex(scale, st.top);
+  const float f = scale * w, fp = f * (__builtin_amdgcn_exp2f(-ex.off) / st.S);
+  if (ex.near)
+    write_entries(held, x, g, tid, target, -f,
+                  [&](float v) { return fp * __builtin_amdgcn_exp2f(ex.template at<true>(v)); });
+  else
+    write_entries(held, x, g, tid, target, -f,
+                  [&](float v) { return fp * __builtin_amdgcn_exp2f(ex.template at<false>(v)); });
+}
+
+// One row a team: a wave of its own (NT = 64, four of them a workgroup), or a
+// workgroup. LOSS: the gradient from the same registers; else the log probabilities,
+// entropy and alternatives.
+template <class T, int NT, int NVEC, bool LOSS>
+__global__ __launch_bounds__(NT == 64 ? kThreads : NT) void token_row_kernel(TokenArgs a) {
+  constexpr int kTeams = NT == 64 ? kThreads / 64 : 1;
+  __shared__ float red[2][NT / 64][2];
+  __shared__ uint64_t red64[NT / 64];
+  __shared__ TopLds<NT> top_lds[LOSS ? 1 : kTeams];
+  const int32_t team_at = NT == 64 ? (int32_t)(threadIdx.x >> 6) : 0;
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  Team<NT> team{red, 0};
+  for (int64_t row = (int64_t)blockIdx.x * kTeams + team_at; row < a.rows;
+       row += (int64_t)gridDim.x * kTeams) {
     const T* x = static_cast<const T*>(a.logits) + row * a.stride;
     bool empty;
     const int32_t target = target_of(a, row, &empty);
-    RowStats st{};
-    if (!empty) st = stats_of(a, x, red);
-    if (threadIdx.x == 0) {
-      if (a.logp_out) a.logp_out[row] = empty ? 0.0f : logp_of(st, a.scale * entry(x, target));
-      if (a.lse_out) a.lse_out[row] = empty ? 0.0f : (st.nan ? NAN : (st.none ? -INFINITY : st.m + st.log_sum));
-      if (a.entropy_out) a.entropy_out[row] = empty ? 0.0f : st.entropy;
+    Held<T, NT, NVEC> held;
+    float top = -INFINITY, S = 1.0f, E = 0.0f, mine = -INFINITY, at_target = 0.0f;
+    if (!empty) {
+      held.load(x, a.V, tid);
+      if (target >= 0) at_target = entry(x, target);   // before a gradient is written there
+      reduce_row(team, held, a.scale, !LOSS && a.entropy_out, top, S, E, mine);
     }
-    uint64_t last = ~(uint64_t)0;
-    for (int32_t i = 0; i < a.k; ++i) {
-      uint64_t best = 0;
-      if (!empty && !st.nan && !st.none) {
-        for (int32_t v = threadIdx.x; v < a.V; v += kThreads) {
-          const float f = entry(x, v);
-          const uint64_t o = order_of(f, v);
-          if (f > -INFINITY && o < last && o > best) best = o;
-        }
-        best = block_max_u64(best, red64);
-        last = best;
-      }
-      if (threadIdx.x == 0) {
-        const int32_t v = best ? (int32_t)~(uint32_t)best : -1;
-        if (a.top_ids) a.top_ids[row * a.k + i] = v;
-        if (a.top_logprobs)
-          a.top_logprobs[row * a.k + i] =
-              best ? logp_of(st, a.scale * entry(x, v)) : (st.nan ? NAN : -INFINITY);
-      }
+    const RowStats st(a.scale, top, S, E);
+    if (tid == 0) {
+      if (a.logp_out) a.logp_out[row] = empty ? 0.0f : st.logp(a.scale * at_target);
+      if (a.lse_out) a.lse_out[row] = empty ? 0.0f : st.lse();
+      if (a.entropy_out) a.entropy_out[row] = empty ? 0.0f : st.entropy();
     }
-    if (a.dlogits) {
-      __syncthreads();   // dlogits may be logits
+    if constexpr (LOSS) {
       T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride;
       const float w = empty ? 0.0f : (a.weights ? a.weights[row] : 1.0f);
-      const float f = st.none ? 0.0f : a.scale * w, inv = 1.0f / st.sum;
-      for (int32_t v = threadIdx.x; v < a.V; v += kThreads) {
-        float out = 0.0f;
-        if (w != 0.0f && st.nan) out = NAN;
-        if (w != 0.0f && !st.nan && !st.none)
-          out = f * (exp_of(a.scale * entry(x, v) - st.m) * inv - (v == target ? 1.0f : 0.0f));
-        put(g, v, out);
-      }
+      write_gradient<T, NT, NVEC>(held, x, g, a.V, tid, target, w, a.scale, st);
+    } else if (a.k > 0) {
+      int32_t found = 0;
+      if (!empty && !st.nan && !st.none)
+        found = top_entries<NT>(team, held, mine, a.k, 0, top_lds[team_at], red64,
+                                [&](int32_t i, uint64_t o) {
+                                  if (a.top_ids) a.top_ids[row * a.k + i] = (int32_t)~(uint32_t)o;
+                                  if (a.top_logprobs)
+                                    a.top_logprobs[row * a.k + i] = st.logp(a.scale * logit_of(o));
+                                });
+      fill_top(a, row, found + tid, NT, !empty && st.nan);
     }
   }
 }
 
+// Rows in parts, where one workgroup's registers do not hold a row, or where there are
+// few rows: every part leaves its sums (relative to its own largest logit), the logit of
+// the target if it has it, and its most likely entries; a second launch joins them.
+constexpr int kPartVecs = 4;
 template <class T>
-__global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a) {
+using PartHeld = Held<T, kThreads, kPartVecs>;
+
+struct Parts {
+  float4* sums;      // [rows][parts]: largest logit, S, E, logit of the target
+  uint64_t* keys;    // [rows][parts][k], the largest first, 0 behind them
+  int32_t n;         // of a row
+};
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void token_part_kernel(TokenArgs a, Parts parts) {
+  __shared__ float red[2][kThreads / 64][2];
+  __shared__ uint64_t red64[kThreads / 64];
+  __shared__ TopLds<kThreads> top_lds;
+  Team<kThreads> team{red, 0};
+  const int32_t tid = threadIdx.x;
+  for (int64_t at = blockIdx.x; at < a.rows * parts.n; at += gridDim.x) {
+    const int64_t row = at / parts.n;
+    const int32_t part = (int32_t)(at - row * parts.n), first = part * PartHeld<T>::kMost;
+    const int32_t n = a.V - first < PartHeld<T>::kMost ? a.V - first : PartHeld<T>::kMost;
+    bool empty;
+    const int32_t target = target_of(a, row, &empty);
+    if (empty) continue;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride + first;
+    PartHeld<T> held;
+    held.load(x, n, tid);
+    float top, S, E, mine;
+    reduce_row(team, held, a.scale, a.entropy_out != nullptr, top, S, E, mine);
+    if (tid == 0)
+      parts.sums[at] = make_float4(top, S, E, target >= first && target < first + n ? entry(x, target - first) : 0.0f);
+    if (a.k > 0) {
+      uint64_t* keys = parts.keys + at * a.k;
+      int32_t found = 0;
+      if (S == S && top != INFINITY && top != -INFINITY)
+        found = top_entries<kThreads>(team, held, mine, a.k, first, top_lds, red64,
+                                      [&](int32_t i, uint64_t o) { keys[i] = o; });
+      if (found + tid < a.k) keys[found + tid] = 0;
+    }
+  }
+}
+
+// The sums of a row from those of its parts; *z: the logit of the target, where there is one.
+template <class T>
+__device__ __forceinline__ RowStats join_parts(const TokenArgs& a, const Parts& parts, int64_t row,
+                                               int32_t target, Team<kThreads>& team, float* z) {
+  const float4* sums = parts.sums + row * parts.n;
+  float top = -INFINITY;
+  for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) top = fmaxf(top, sums[p].x);
+  top = team.max(top);
+  const float m = top == -INFINITY ? 0.0f : a.scale * top;
+  float S = 0.0f, E = 0.0f;
+  for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) {
+    const float4 q = sums[p];
+    if (q.y != 0.0f) {   // 0: all of the part is -inf; NaN counts
+      const float t = (a.scale * q.x - m) * kLog2e, w = __builtin_amdgcn_exp2f(t);
+      S = fmaf(w, q.y, S);
+      E += w * fmaf(q.y, fmaxf(t, -256.0f), q.z);
+    }
+  }
+  team.sum(S, E);
+  *z = target >= 0 ? a.scale * sums[target / PartHeld<T>::kMost].w : 0.0f;
+  return RowStats(a.scale, top, S, E);
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts parts) {
+  __shared__ float red[2][kThreads / 64][2];
+  __shared__ uint64_t red64[kThreads / 64];
+  __shared__ uint64_t list[kListed];
+  __shared__ int32_t count;
+  Team<kThreads> team{red, 0};
+  const int32_t tid = threadIdx.x;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
-    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
-    T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride;
+    bool empty;
+    const int32_t target = target_of(a, row, &empty);
+    float z = 0.0f;
+    RowStats st(a.scale, 0.0f, 1.0f, 0.0f);
+    if (!empty) st = join_parts<T>(a, parts, row, target, team, &z);
+    if (tid == 0) {
+      if (a.logp_out) a.logp_out[row] = empty ? 0.0f : st.logp(z);
+      if (a.lse_out) a.lse_out[row] = empty ? 0.0f : st.lse();
+      if (a.entropy_out) a.entropy_out[row] = empty ? 0.0f : st.entropy();
+    }
+    if (a.k == 0) continue;
+    int32_t found = 0;
+    if (!empty && !st.nan && !st.none) {
+      const uint64_t* keys = parts.keys + row * parts.n * a.k;
+      const int64_t all = (int64_t)parts.n * a.k;
+      const auto put = [&](int32_t i, uint64_t o) {
+        if (a.top_ids) a.top_ids[row * a.k + i] = (int32_t)~(uint32_t)o;
+        if (a.top_logprobs) a.top_logprobs[row * a.k + i] = st.logp(a.scale * logit_of(o));
+      };
+      // The largest of the parts' k-th entries is not above the row's k-th.
+      const auto largest = [&](uint64_t v) {
+        v = wave_max_u64(v);
+        if ((tid & 63) == 0) red64[tid >> 6] = v;
+        __syncthreads();
+        for (int w = 0; w < kThreads / 64; ++w) v = red64[w] > v ? red64[w] : v;
+        __syncthreads();
+        return v;
+      };
+      uint64_t least = 1;
+      for (int32_t p = tid; p < parts.n; p += kThreads) {
+        const uint64_t o = keys[(int64_t)(p + 1) * a.k - 1];
+        least = o > least ? o : least;
+      }
+      if (tid == 0) count = 0;
+      least = largest(least);
+      for (int64_t i = tid; i < all; i += kThreads) {
+        const uint64_t o = keys[i];
+        if (o >= least) {
+          const int32_t at = atomicAdd(&count, 1);
+          if (at < kListed) list[at] = o;
+        }
+      }
+      __syncthreads();
+      const int32_t n = count;
+      if (n <= kListed) {
+        for (int32_t i = tid; i < n; i += kThreads) {
+          const uint64_t own = list[i];
+          int32_t rank = 0;
+#pragma unroll 4
+          for (int32_t j = 0; j < n; ++j) rank += list[j] > own ? 1 : 0;
+          if (rank < a.k) put(rank, own);
+        }
+        found = n < a.k ? n : a.k;
+      } else {
+        uint64_t last = ~(uint64_t)0;
+        for (found = 0; found < a.k; ++found) {
+          uint64_t best = 0;
+          for (int64_t i = tid; i < all; i += kThreads) best = keys[i] < last && keys[i] > best ? keys[i] : best;
+          best = largest(best);
+          if (best == 0) break;
+          if (tid == 0) put(found, best);
+          last = best;
+        }
+      }
+      __syncthreads();
+    }
+    fill_top(a, row, found + tid, kThreads, !empty && st.nan);
+  }
+}
+
+template <class T>
+__global__ __launch_bounds__(kThreads) void token_part_loss_kernel(TokenArgs a, Parts parts) {
+  __shared__ float red[2][kThreads / 64][2];
+  Team<kThreads> team{red, 0};
+  const int32_t tid = threadIdx.x;
+  for (int64_t at = blockIdx.x; at < a.rows * parts.n; at += gridDim.x) {
+    const int64_t row = at / parts.n;
+    const int32_t part = (int32_t)(at - row * parts.n), first = part * PartHeld<T>::kMost;
+    const int32_t n = a.V - first < PartHeld<T>::kMost ? a.V - first : PartHeld<T>::kMost;
+    bool empty;
+    const int32_t target = target_of(a, row, &empty);
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride + first;
+    T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride + first;
+    const float w = empty ? 0.0f : (a.weights ? a.weights[row] : 1.0f);
+    PartHeld<T> held;
+    float z = 0.0f;
+    RowStats st(a.scale, 0.0f, 1.0f, 0.0f);
+    if (!empty) {
+      held.load(x, n, tid);
+      st = join_parts<T>(a, parts, row, target, team, &z);
+    }
+    if (part == 0 && tid == 0 && a.logp_out) a.logp_out[row] = empty ? 0.0f : st.logp(z);
+    write_gradient(held, x, g, n, tid, target - first, w, a.scale, st);
+  }
+}
+
+// dx_v = scale (p_v (g_lse - g_logp - g_H (ln p_v + H)) + g_logp [v = target]): rows, or
+// parts of them, one after the other.
+template <class T, int NT>
+__global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, int32_t parts) {
+  constexpr int kTeams = kThreads / NT;
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  const int32_t team_at = NT == 64 ? (int32_t)(threadIdx.x >> 6) : 0;
+  using H = Held<T, NT, kPartVecs>;
+  for (int64_t at = (int64_t)blockIdx.x * kTeams + team_at; at < a.rows * parts; at += (int64_t)gridDim.x * kTeams) {
+    const int64_t row = at / parts;
+    const int32_t first = (int32_t)(at - row * parts) * H::kMost;
+    const int32_t n = a.V - first < H::kMost ? a.V - first : H::kMost;
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride + first;
+    T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride + first;
     bool empty;
     const int32_t target = target_of(a, row, &empty);
     const float gp = empty || !a.g_logp ? 0.0f : a.g_logp[row];
     const float gl = empty || !a.g_lse ? 0.0f : a.g_lse[row];
     const float ge = empty || !a.g_entropy ? 0.0f : a.g_entropy[row];
     const bool zero = gp == 0.0f && gl == 0.0f && ge == 0.0f;
-    const float lse = zero ? 0.0f : a.lse[row], H = ge != 0.0f ? a.entropy[row] : 0.0f;
-    const bool none = lse == -INFINITY;
-    for (int32_t v = threadIdx.x; v < a.V; v += kThreads) {
-      float out = 0.0f;
-      if (!zero && !none) {
-        const float l = a.scale * entry(x, v) - lse, p = exp_of(l);
-        float q = gl - gp;
-        if (ge != 0.0f && p != 0.0f) q -= ge * (l + H);
-        out = a.scale * (p * q + (v == target ? gp : 0.0f));
-      }
-      put(g, v, out);
+    const float lse = zero ? 0.0f : a.lse[row], H_row = ge != 0.0f ? a.entropy[row] : 0.0f;
+    if (zero || lse == -INFINITY) {
+      write_zeros(g, n, tid, NT);
+      continue;
+    }
+    H held;
+    held.load(x, n, tid);
+    const float q = gl - gp;
+    if (ge == 0.0f) {
+      write_entries(held, x, g, tid, target - first, a.scale * gp,
+                    [&](float v) { return a.scale * (exp_of(a.scale * v - lse) * q); });
+    } else {
+      write_entries(held, x, g, tid, target - first, a.scale * gp, [&](float v) {
+        const float l = a.scale * v - lse, p = exp_of(l);
+        return a.scale * (p * (q - ge * (fmaxf(l, -256.0f) + H_row)));   // 0 for -inf; a NaN is in p
+      });
     }
   }
 }
@@ -241,25 +744,95 @@ TokenArgs common_args(const dpsgd_logits& d, const void* logits) {
 
 uint32_t grid_of(int64_t n) { return (uint32_t)(n < kMostWgs ? n : kMostWgs); }
 
-int launch_rows(const TokenArgs& a, int32_t dtype, hipStream_t stream) {
-  if (dtype == DPSGD_BF16)
-    hipLaunchKernelGGL(token_row_kernel<uint16_t>, dim3(grid_of(a.rows)), dim3(kThreads), 0, stream, a);
+template <class T, bool LOSS>
+int launch_rows_of(const TokenArgs& a, hipStream_t stream) {
+  const int64_t wave4 = Held<T, 64, 4>::kMost;
+  if (a.V <= wave4)
+    hipLaunchKernelGGL((token_row_kernel<T, 64, 4, LOSS>), dim3(grid_of(ceil_div(a.rows, 4))), dim3(kThreads), 0, stream, a);
+  else if (a.V <= 4 * wave4)
+    hipLaunchKernelGGL((token_row_kernel<T, 256, 4, LOSS>), dim3(grid_of(a.rows)), dim3(256), 0, stream, a);
+  else if (a.V <= 16 * wave4)
+    hipLaunchKernelGGL((token_row_kernel<T, 512, 8, LOSS>), dim3(grid_of(a.rows)), dim3(512), 0, stream, a);
+  else if (a.V <= 32 * wave4)
+    hipLaunchKernelGGL((token_row_kernel<T, 1024, 8, LOSS>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
   else
-    hipLaunchKernelGGL(token_row_kernel<float>, dim3(grid_of(a.rows)), dim3(kThreads), 0, stream, a);
+    hipLaunchKernelGGL((token_row_kernel<T, 1024, 16, LOSS>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
+  return check_launch();
+}
+
+int64_t part_entries(int32_t dtype) {
+  return dtype == DPSGD_BF16 ? PartHeld<uint16_t>::kMost : PartHeld<float>::kMost;
+}
+
+// Whether rows are taken in parts: 1024 threads hold 64 vectors of 16 bytes a lane pair.
+bool in_parts(const dpsgd_logits& d) {
+  const int64_t most = d.dtype == DPSGD_BF16 ? Held<uint16_t, 1024, 16>::kMost : Held<float, 1024, 16>::kMost;
+  return d.V > most;
+}
+
+// The workspace: log probabilities of the rows, then the parts' sums and keys.
+struct Plan {
+  size_t sums, keys, bytes;   // offsets
+  int32_t parts;              // 0: whole rows
+};
+
+Plan plan_of(const dpsgd_logits& d, int32_t k) {
+  Plan p{};
+  const size_t rows = (size_t)(d.B * d.T);
+  p.sums = p.keys = p.bytes = round_up(rows * sizeof(float), 16);
+  if (in_parts(d)) {
+    p.parts = (int32_t)ceil_div(d.V, part_entries(d.dtype));
+    p.keys = p.sums + rows * (size_t)p.parts * sizeof(float4);
+    p.bytes = p.keys + rows * (size_t)p.parts * (size_t)k * sizeof(uint64_t);
+  }
+  return p;
+}
+
+template <class T>
+int launch_parts_of(const TokenArgs& a, const Parts& parts, hipStream_t stream) {
+  const uint32_t grid = grid_of(a.rows * parts.n);
+  hipLaunchKernelGGL(token_part_kernel<T>, dim3(grid), dim3(kThreads), 0, stream, a, parts);
+  if (check_launch() != DPSGD_OK) return DPSGD_ERR_HIP;
+  if (a.dlogits)
+    hipLaunchKernelGGL(token_part_loss_kernel<T>, dim3(grid), dim3(kThreads), 0, stream, a, parts);
+  else
+    hipLaunchKernelGGL(token_join_kernel<T>, dim3(grid_of(a.rows)), dim3(kThreads), 0, stream, a, parts);
+  return check_launch();
+}
+
+int launch_rows(const TokenArgs& a, const dpsgd_logits& d, void* workspace, hipStream_t stream) {
+  const Plan p = plan_of(d, a.k);
+  const bool bf16 = d.dtype == DPSGD_BF16;
+  if (p.parts) {
+    char* ws = static_cast<char*>(workspace);
+    const Parts parts{reinterpret_cast<float4*>(ws + p.sums), reinterpret_cast<uint64_t*>(ws + p.keys), p.parts};
+    return bf16 ? launch_parts_of<uint16_t>(a, parts, stream) : launch_parts_of<float>(a, parts, stream);
+  }
+  if (a.dlogits)
+    return bf16 ? launch_rows_of<uint16_t, true>(a, stream) : launch_rows_of<float, true>(a, stream);
+  return bf16 ? launch_rows_of<uint16_t, false>(a, stream) : launch_rows_of<float, false>(a, stream);
+}
+
+template <class T>
+int launch_backward_of(const TokenArgs& a, hipStream_t stream) {
+  const int64_t wave = Held<T, 64, kPartVecs>::kMost, part = PartHeld<T>::kMost;
+  if (a.V <= wave) {
+    hipLaunchKernelGGL((token_backward_kernel<T, 64>), dim3(grid_of(ceil_div(a.rows, 4))), dim3(kThreads), 0, stream, a, 1);
+  } else {
+    const int64_t parts = ceil_div(a.V, part);
+    hipLaunchKernelGGL((token_backward_kernel<T, kThreads>), dim3(grid_of(a.rows * parts)), dim3(kThreads), 0, stream,
+                       a, (int32_t)parts);
+  }
   return check_launch();
 }
 
 }  // namespace
 
-size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k) {
-  (void)k;
-  return round_up((size_t)(d.B * d.T) * sizeof(float), 16);
-}
+size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k) { return plan_of(d, k).bytes; }
 
 int launch_token_logprobs(const dpsgd_logits& d, const void* logits, float* logprobs, float* lse,
                           float* entropy, int32_t k, int64_t* top_ids, float* top_logprobs,
                           void* workspace, hipStream_t stream) {
-  (void)workspace;
   TokenArgs a = common_args(d, logits);
   a.logp_out = logprobs;
   a.lse_out = lse;
@@ -267,7 +840,7 @@ int launch_token_logprobs(const dpsgd_logits& d, const void* logits, float* logp
   a.k = k;
   a.top_ids = top_ids;
   a.top_logprobs = top_logprobs;
-  return launch_rows(a, d.dtype, stream);
+  return launch_rows(a, d, workspace, stream);
 }
 
 int launch_token_backward(const dpsgd_logits& d, const void* logits, const float* lse,
@@ -282,11 +855,7 @@ int launch_token_backward(const dpsgd_logits& d, const void* logits, const float
   a.g_entropy = g_entropy;
   a.dlogits = dlogits;
   a.grad_stride = dlogits_stride;
-  if (d.dtype == DPSGD_BF16)
-    hipLaunchKernelGGL(token_backward_kernel<uint16_t>, dim3(grid_of(a.rows)), dim3(kThreads), 0, stream, a);
-  else
-    hipLaunchKernelGGL(token_backward_kernel<float>, dim3(grid_of(a.rows)), dim3(kThreads), 0, stream, a);
-  return check_launch();
+  return d.dtype == DPSGD_BF16 ? launch_backward_of<uint16_t>(a, stream) : launch_backward_of<float>(a, stream);
 }
 
 int launch_token_loss(const dpsgd_logits& d, const void* logits, const float* weights,
@@ -297,7 +866,7 @@ int launch_token_loss(const dpsgd_logits& d, const void* logits, const float* we
   a.dlogits = dlogits;
   a.grad_stride = dlogits_stride;
   a.logp_out = logprobs ? logprobs : static_cast<float*>(workspace);
-  const int st = launch_rows(a, d.dtype, stream);
+  const int st = launch_rows(a, d, workspace, stream);
   if (st != DPSGD_OK || !losses) return st;
   hipLaunchKernelGGL(token_losses_kernel, dim3(grid_of(ceil_div(d.B, 4))), dim3(kThreads), 0,
                      stream, a, a.logp_out, losses, d.B, d.T);
