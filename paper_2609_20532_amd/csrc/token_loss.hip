@@ -19,6 +19,7 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 constexpr int64_t kMostWgs = 1 << 20;
+constexpr int64_t kFewRows = 64;
 
 struct TokenArgs {
   const void* logits;
@@ -98,6 +99,10 @@ __device__ __forceinline__ uint64_t wave_max_u64(uint64_t v) {
   return v;
 }
 
+// Vectors are worked on one after the other: interleaved, their intermediate values do
+// not fit the registers beside the row, and there are waves enough to fill the pauses.
+__device__ __forceinline__ void one_by_one() { __builtin_amdgcn_sched_barrier(0); }
+
 // n entries in a row from an address of any alignment, in the registers of NT
 // threads: vectors of 16 bytes between the first and the last 16-byte boundary, and
 // the entries before and after them, one a thread. Places without an entry hold -inf.
@@ -120,7 +125,7 @@ struct Held {
     for (int j = 0; j < NVEC; ++j) {
 #pragma unroll
       for (uint32_t& w : raw[j].w) w = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
-      if (j * NT + tid < vecs) raw[j].load(x + head + (j * NT + tid) * VE);
+      if (tid < vecs - j * NT) raw[j].load(x + head + j * NT * VE + (uint32_t)(tid * VE));
     }
     edge = edge_at >= 0 ? entry(x, edge_at) : -INFINITY;
   }
@@ -136,11 +141,29 @@ struct Held {
 #pragma unroll
         for (int c = 0; c < VE; ++c) f(x[c]);
       }
+      one_by_one();
     }
     f(edge);
   }
 
-  // f(x, place in the row) for the entries x >= least.
+  // The largest entry of the thread in each quarter of its vectors; the one beside the
+  // vectors counts to the first.
+  __device__ __forceinline__ void quarter_maxima(float (&g)[4]) const {
+    static_assert(NVEC % 4 == 0, "");
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      g[q] = q == 0 ? edge : -INFINITY;
+#pragma unroll
+      for (int j = q * NVEC / 4; j < (q + 1) * NVEC / 4; ++j) {
+        float x[VE];
+        raw[j].widen(x);
+#pragma unroll
+        for (int c = 0; c < VE; ++c) g[q] = fmaxf(g[q], x[c]);
+      }
+    }
+  }
+
+  // f(x, place in the row) for the entries x >= least, which are few.
   template <class F>
   __device__ __forceinline__ void each_from(float least, int32_t tid, F f) const {
 #pragma unroll
@@ -148,17 +171,31 @@ struct Held {
       if (j * NT + tid < vecs) {
         float x[VE];
         raw[j].widen(x);
+        uint32_t which = 0;
 #pragma unroll
-        for (int c = 0; c < VE; ++c)
-          if (x[c] >= least) f(x[c], head + (j * NT + tid) * VE + c);
+        for (int c = 0; c < VE; ++c) which |= x[c] >= least ? 1u << c : 0u;
+        while (which) {
+          const int32_t at = __builtin_ctz(which);
+          which &= which - 1;
+          float v = x[0];
+#pragma unroll
+          for (int c = 1; c < VE; ++c) v = c == at ? x[c] : v;
+          f(v, head + (j * NT + tid) * VE + at);
+        }
       }
+      one_by_one();
     }
     if (edge >= least && edge_at >= 0) f(edge, edge_at);
   }
 
-  __device__ __forceinline__ void keep_raw() {
+  // Nothing that was formed from the entries before is held on to: the next pass forms
+  // it again, and only the entries stay in registers.
+  __device__ __forceinline__ void entries_alone() {
 #pragma unroll
-    for (int j = 0; j < NVEC; ++j) raw[j].keep_raw();
+    for (int j = 0; j < NVEC; ++j) {
+#pragma unroll
+      for (uint32_t& w : raw[j].w) asm volatile("" : "+v"(w));
+    }
   }
 };
 
@@ -269,11 +306,12 @@ struct RowStats {
 };
 
 template <class Tm, class H>
-__device__ __forceinline__ void reduce_row(Tm& team, const H& held, float scale, bool entropy,
+__device__ __forceinline__ void reduce_row(Tm& team, H& held, float scale, bool entropy,
                                            float& top, float& S, float& E, float& mine) {
   mine = -INFINITY;
   held.each([&](float x) { mine = fmaxf(mine, x); });
   top = team.max(mine);
+  held.entries_alone();
   const Exponents ex(scale, top);
   if (ex.near) {
     if (entropy) sums_of<true, true>(held, ex, S, E); else sums_of<true, false>(held, ex, S, E);
@@ -281,21 +319,139 @@ __device__ __forceinline__ void reduce_row(Tm& team, const H& held, float scale,
     if (entropy) sums_of<false, true>(held, ex, S, E); else sums_of<false, false>(held, ex, S, E);
   }
   team.sum(S, E);
+  held.entries_alone();
   E = fmaf(-ex.off, S, E);
   const float back = __builtin_amdgcn_exp2f(-ex.off);
   S *= back;
   E *= back;
 }
 
-constexpr int kListed = 1024;       // candidates that a workgroup's list holds
-constexpr int kListedWave = 256;    // that a wave's list holds
+// S and E as sums_of's for a row of any length in one pass over memory, no entry held:
+// every thread has a running reference R (base 2, at least what makes its largest
+// exponent so far 0) and sums relative to it, rescaled once a batch of vectors. R is
+// kept within 2^20: entries below are 0 beside any row's largest that is not; where the
+// largest is outside, *near is false and the sums say nothing.
+template <class T, int NT>
+struct Running {
+  static constexpr int VE = 16 / (int)sizeof(T);
+  static constexpr int kBatch = 4;
+  float top = -INFINITY, R = -1048576.0f, S = 0.0f, E = 0.0f;
+
+  template <bool ENTROPY, int N>
+  __device__ __forceinline__ void add(const float (&x)[N], float c) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) top = fmaxf(top, x[k]);
+    const float R1 = fminf(fmaxf(top * c, -1048576.0f), 1048576.0f), d = R - R1;
+    const float w = __builtin_amdgcn_exp2f(d);
+    if constexpr (ENTROPY) E = w * fmaf(d, S, E);
+    S *= w;
+    R = R1;
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+      const float t = fmaf(x[k], c, -R), p = __builtin_amdgcn_exp2f(t);
+      S += p;
+      if constexpr (ENTROPY) E = fmaf(p, fmaxf(t, -256.0f), E);
+    }
+  }
+
+  template <bool ENTROPY>
+  __device__ __forceinline__ void row(const T* x, int32_t n, int32_t tid, float c) {
+    int32_t head = (int32_t)((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / (int32_t)sizeof(T);
+    head = head < n ? head : n;
+    const int32_t vecs = (n - head) / VE, tail = n - head - vecs * VE;
+    const int32_t edge_at = tid < head ? tid : (tid - head < tail ? n - tail + tid - head : -1);
+    const float edge[1] = {edge_at >= 0 ? entry(x, edge_at) : -INFINITY};
+    const T* body = x + head;
+    int32_t j = tid;
+    for (; j + (kBatch - 1) * NT < vecs; j += kBatch * NT) {
+      Raw<T, VE> raw[kBatch];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) raw[b].load(body + (int64_t)(j + b * NT) * VE);
+      float f[kBatch * VE];
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        float g[VE];
+        raw[b].widen(g);
+#pragma unroll
+        for (int k = 0; k < VE; ++k) f[b * VE + k] = g[k];
+      }
+      add<ENTROPY>(f, c);
+    }
+    for (; j < vecs; j += NT) {
+      float f[VE];
+      load_vec<VE>(body + (int64_t)j * VE, f);
+      add<ENTROPY>(f, c);
+    }
+    if (edge_at >= 0) add<ENTROPY>(edge, c);
+  }
+
+  // The row's, in every thread: relative to the exact largest entry.
+  __device__ __forceinline__ bool join(Team<NT>& team, float c) {
+    top = team.max(top);
+    const float top_c = top * c, Rf = fminf(fmaxf(top_c, -1048576.0f), 1048576.0f);
+    const bool near = fabsf(top_c) <= 1048576.0f;
+    const float off = near ? fmaf(top, c, -top_c) : 0.0f, d = (R - Rf) - off;
+    const float w = __builtin_amdgcn_exp2f(d);
+    E = w == 0.0f ? 0.0f : w * fmaf(d, S, E);
+    S = w == 0.0f && S == S ? 0.0f : w * S;
+    team.sum(S, E);
+    return near;
+  }
+};
+
+// The same sums where the largest entry is far from 0 (or there is none), by exponents
+// of the rounded products.
+template <class T, int NT>
+__device__ __forceinline__ void far_sums(Team<NT>& team, const T* x, int32_t n, int32_t tid, float scale,
+                                         float top, float& S, float& E) {
+  const Exponents ex(scale, top);
+  S = E = 0.0f;
+  for (int32_t v = tid; v < n; v += NT) {
+    const float t = ex.template at<false>(entry(x, v)), p = __builtin_amdgcn_exp2f(t);
+    S += p;
+    E = fmaf(p, fmaxf(t, -256.0f), E);
+  }
+  team.sum(S, E);
+}
+
+// One row a team (as below), nothing but sums asked for.
+template <class T, int NT, bool ENTROPY>
+__global__ __launch_bounds__(kThreads) void token_sums_kernel(TokenArgs a) {
+  constexpr int kTeams = kThreads / NT;
+  __shared__ float red[2][NT / 64][2];
+  const int32_t team_at = NT == 64 ? __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)) : 0;
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  Team<NT> team{red, 0};
+  for (int64_t row = (int64_t)blockIdx.x * kTeams + team_at; row < a.rows; row += (int64_t)gridDim.x * kTeams) {
+    const T* x = static_cast<const T*>(a.logits) + row * a.stride;
+    bool empty;
+    const int32_t target = target_of(a, row, &empty);
+    Running<T, NT> run;
+    float at_target = 0.0f;
+    run.S = empty ? 1.0f : 0.0f;
+    if (!empty) {
+      if (target >= 0) at_target = entry(x, target);
+      run.template row<ENTROPY>(x, a.V, tid, a.scale * kLog2e);
+      if (!run.join(team, a.scale * kLog2e)) far_sums(team, x, a.V, tid, a.scale, run.top, run.S, run.E);
+    }
+    if (tid == 0) {
+      const RowStats st(a.scale, run.top, run.S, run.E);
+      if (a.logp_out) a.logp_out[row] = empty ? 0.0f : st.logp(a.scale * at_target);
+      if (a.lse_out) a.lse_out[row] = empty ? 0.0f : st.lse();
+      if (a.entropy_out) a.entropy_out[row] = empty ? 0.0f : st.entropy();
+    }
+  }
+}
+
+constexpr int kListed = 2048;       // candidates that a workgroup's list holds
+constexpr int kListedWave = 512;    // that a wave's list holds
 
 // Where the most likely entries of a row are collected.
 template <int NT>
 struct TopLds {
   static constexpr int kMost = NT == 64 ? kListedWave : kListed;
   uint64_t key[kMost];
-  uint32_t group[64];
+  alignas(16) uint32_t group[256];
   uint32_t least;
   int32_t count;
 };
@@ -306,66 +462,87 @@ __device__ __forceinline__ float logit_of(uint64_t order) {
   return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o);
 }
 
-// The k largest entries in order: put(i, order) for i < the number that there are.
-// The threads' largest ones, joined to 64 groups, give a bound: the k-th largest of
-// the groups' is not above the k-th largest entry, and few entries are above it. Those
-// are listed, and each finds its place by counting the larger ones. `first` is added to
-// the entries' places. Where the list is too short (many equal or sorted logits) the
-// entries are taken one by one.
-template <int NT, class H, class P>
-__device__ __forceinline__ int32_t top_entries(Team<NT>& team, const H& held, float mine, int32_t k,
-                                               int32_t first, TopLds<NT>& lds, uint64_t* red64, P put) {
-  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
-  constexpr int kLanes = NT / 64;   // threads of a group
-  uint32_t g = order_bits(mine);
-#pragma unroll
-  for (int off = 1; off < kLanes; off <<= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)g, off, 64);
-    g = o > g ? o : g;
+// put(i, order) for the k largest of n different keys in LDS, in order; returns their
+// number. Every key finds its place by counting the larger ones.
+template <int NT, class P>
+__device__ __forceinline__ int32_t put_in_order(const uint64_t* keys, int32_t n, int32_t k, int32_t tid, P put) {
+  for (int32_t i = tid; i < n; i += NT) {
+    const uint64_t own = keys[i];
+    int32_t rank = 0;
+#pragma unroll 8
+    for (int32_t j = 0; j < n; ++j) rank += keys[j] > own ? 1 : 0;
+    if (rank < k) put(rank, own);
   }
-  if (tid % kLanes == 0) lds.group[tid / kLanes] = g;
+  return n < k ? n : k;
+}
+
+// The k largest entries in order: put(i, order) for i < the number that there are.
+// The entries are in 256 groups (a vector's places of one lane, the places of one, two
+// or four neighbouring lanes); at least k of the groups' largest ones are not below the
+// k-th largest of them, so entries below it are none of the k. Of V unordered entries
+// about 256 ln(256 / (256 - k)) are left, 21 for k = 20 and 74 for k = 64: they are
+// listed and put in order. The bound is found in its upper 16 bits, by one wave, from
+// the highest bit down. `first` is added to the entries' places. Where the list is too
+// short (many equal or sorted logits) the n_row entries at x are searched once for each
+// alternative.
+template <int NT, class T, class H, class P>
+__device__ __forceinline__ int32_t top_entries(Team<NT>& team, const H& held, const T* x, int32_t n_row,
+                                               float mine, int32_t k, int32_t first, TopLds<NT>& lds,
+                                               uint64_t* red64, P put) {
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  if constexpr (NT == 64) {
+    float g[4];
+    held.quarter_maxima(g);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) lds.group[tid * 4 + j] = order_bits(g[j]);
+  } else {
+    constexpr int kLanes = NT / 256;   // threads of a group
+    uint32_t g = order_bits(mine);
+#pragma unroll
+    for (int off = 1; off < kLanes; off <<= 1) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)g, off, 64);
+      g = o > g ? o : g;
+    }
+    if (tid % kLanes == 0) lds.group[tid / kLanes] = g;
+  }
   if (tid == 0) lds.count = 0;
   team.barrier();
   if (tid < 64) {
-    const uint32_t own = lds.group[tid];
-    int rank = 0;
+    const uint4 g = reinterpret_cast<const uint4*>(lds.group)[tid];
+    uint32_t least = 0;
 #pragma unroll
-    for (int j = 0; j < 64; ++j) {
-      const uint32_t o = (uint32_t)__builtin_amdgcn_readlane((int)own, j);
-      rank += o > own || (o == own && j < tid) ? 1 : 0;
+    for (int bit = 31; bit >= 16; --bit) {
+      const uint32_t t = least | 1u << bit;
+      const int n = __popcll(__ballot(g.x >= t)) + __popcll(__ballot(g.y >= t)) +
+                    __popcll(__ballot(g.z >= t)) + __popcll(__ballot(g.w >= t));
+      if (n >= k) least = t;
     }
-    if (rank == k - 1) lds.least = own;
+    if (tid == 0) lds.least = least;
   }
   team.barrier();
   // Entries of -inf are none.
   const uint32_t none = order_bits(-INFINITY);
   const uint32_t least = lds.least > none ? lds.least : none + 1;
   if (order_bits(mine) >= least) {
-    held.each_from(logit_of((uint64_t)least << 32), tid, [&](float x, int32_t v) {
+    held.each_from(logit_of((uint64_t)least << 32), tid, [&](float f, int32_t v) {
       const int32_t at = atomicAdd(&lds.count, 1);
-      if (at < TopLds<NT>::kMost) lds.key[at] = order_of(x, first + v);
+      if (at < TopLds<NT>::kMost) lds.key[at] = order_of(f, first + v);
     });
   }
   team.barrier();
   const int32_t n = lds.count;
   int32_t found;
   if (n <= TopLds<NT>::kMost) {
-    for (int32_t i = tid; i < n; i += NT) {
-      const uint64_t own = lds.key[i];
-      int32_t rank = 0;
-#pragma unroll 4
-      for (int32_t j = 0; j < n; ++j) rank += lds.key[j] > own ? 1 : 0;
-      if (rank < k) put(rank, own);
-    }
-    found = n < k ? n : k;
+    found = put_in_order<NT>(lds.key, n, k, tid, put);
   } else {
     uint64_t last = ~(uint64_t)0;
     for (found = 0; found < k; ++found) {
       uint64_t best = 0;
-      held.each_from(-3.402823466e38f, tid, [&](float x, int32_t v) {
-        const uint64_t o = order_of(x, first + v);
-        if (o < last && o > best) best = o;
-      });
+      for (int32_t v = tid; v < n_row; v += NT) {
+        const float f = entry(x, v);
+        const uint64_t o = order_of(f, first + v);
+        if (f != -INFINITY && o < last && o > best) best = o;
+      }
       best = wave_max_u64(best);
       if constexpr (NT > 64) {
         if ((threadIdx.x & 63) == 0) red64[threadIdx.x >> 6] = best;
@@ -423,7 +600,7 @@ __device__ __forceinline__ void write_entries(const Held<T, NT, NVEC>& held, con
 #pragma unroll
         for (int c = 0; c < VE; ++c) v[c] += c == rel % VE ? add : 0.0f;
       }
-      T* to = g + held.head + (j * NT + tid) * VE;
+      T* to = g + held.head + j * NT * VE + (uint32_t)(tid * VE);
       if (same) {
         store_vec<VE>(to, v);
       } else {
@@ -431,6 +608,7 @@ __device__ __forceinline__ void write_entries(const Held<T, NT, NVEC>& held, con
         for (int c = 0; c < VE; ++c) put(to, c, v[c]);
       }
     }
+    one_by_one();
   }
   if (held.edge_at >= 0) put(g, held.edge_at, value(held.edge) + (held.edge_at == target ? add : 0.0f));
 }
@@ -455,12 +633,12 @@ __device__ __forceinline__ void write_gradient(const Held<T, NT, NVEC>& held, co
 // workgroup. LOSS: the gradient from the same registers; else the log probabilities,
 // entropy and alternatives.
 template <class T, int NT, int NVEC, bool LOSS>
-__global__ __launch_bounds__(NT == 64 ? kThreads : NT) void token_row_kernel(TokenArgs a) {
+__global__ __launch_bounds__(NT == 64 ? kThreads : NT, NVEC > 8 || (NVEC == 8 && !LOSS) ? 4 : 8) void token_row_kernel(TokenArgs a) {
   constexpr int kTeams = NT == 64 ? kThreads / 64 : 1;
   __shared__ float red[2][NT / 64][2];
   __shared__ uint64_t red64[NT / 64];
   __shared__ TopLds<NT> top_lds[LOSS ? 1 : kTeams];
-  const int32_t team_at = NT == 64 ? (int32_t)(threadIdx.x >> 6) : 0;
+  const int32_t team_at = NT == 64 ? __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)) : 0;
   const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
   Team<NT> team{red, 0};
   for (int64_t row = (int64_t)blockIdx.x * kTeams + team_at; row < a.rows;
@@ -488,7 +666,7 @@ __global__ __launch_bounds__(NT == 64 ? kThreads : NT) void token_row_kernel(Tok
     } else if (a.k > 0) {
       int32_t found = 0;
       if (!empty && !st.nan && !st.none)
-        found = top_entries<NT>(team, held, mine, a.k, 0, top_lds[team_at], red64,
+        found = top_entries<NT>(team, held, x, a.V, mine, a.k, 0, top_lds[team_at], red64,
                                 [&](int32_t i, uint64_t o) {
                                   if (a.top_ids) a.top_ids[row * a.k + i] = (int32_t)~(uint32_t)o;
                                   if (a.top_logprobs)
@@ -510,6 +688,7 @@ struct Parts {
   float4* sums;      // [rows][parts]: largest logit, S, E, logit of the target
   uint64_t* keys;    // [rows][parts][k], the largest first, 0 behind them
   int32_t n;         // of a row
+  int32_t size;      // entries of a part (the last one of a row may have fewer)
 };
 
 template <class T>
@@ -521,8 +700,8 @@ __global__ __launch_bounds__(kThreads) void token_part_kernel(TokenArgs a, Parts
   const int32_t tid = threadIdx.x;
   for (int64_t at = blockIdx.x; at < a.rows * parts.n; at += gridDim.x) {
     const int64_t row = at / parts.n;
-    const int32_t part = (int32_t)(at - row * parts.n), first = part * PartHeld<T>::kMost;
-    const int32_t n = a.V - first < PartHeld<T>::kMost ? a.V - first : PartHeld<T>::kMost;
+    const int32_t part = (int32_t)(at - row * parts.n), first = part * parts.size;
+    const int32_t n = a.V - first < parts.size ? a.V - first : parts.size;
     bool empty;
     const int32_t target = target_of(a, row, &empty);
     if (empty) continue;
@@ -537,7 +716,7 @@ __global__ __launch_bounds__(kThreads) void token_part_kernel(TokenArgs a, Parts
       uint64_t* keys = parts.keys + at * a.k;
       int32_t found = 0;
       if (S == S && top != INFINITY && top != -INFINITY)
-        found = top_entries<kThreads>(team, held, mine, a.k, first, top_lds, red64,
+        found = top_entries<kThreads>(team, held, x, n, mine, a.k, first, top_lds, red64,
                                       [&](int32_t i, uint64_t o) { keys[i] = o; });
       if (found + tid < a.k) keys[found + tid] = 0;
     }
@@ -563,7 +742,7 @@ __device__ __forceinline__ RowStats join_parts(const TokenArgs& a, const Parts& 
     }
   }
   team.sum(S, E);
-  *z = target >= 0 ? a.scale * sums[target / PartHeld<T>::kMost].w : 0.0f;
+  *z = target >= 0 ? a.scale * sums[target / parts.size].w : 0.0f;
   return RowStats(a.scale, top, S, E);
 }
 
@@ -621,14 +800,7 @@ __global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts
       __syncthreads();
       const int32_t n = count;
       if (n <= kListed) {
-        for (int32_t i = tid; i < n; i += kThreads) {
-          const uint64_t own = list[i];
-          int32_t rank = 0;
-#pragma unroll 4
-          for (int32_t j = 0; j < n; ++j) rank += list[j] > own ? 1 : 0;
-          if (rank < a.k) put(rank, own);
-        }
-        found = n < a.k ? n : a.k;
+        found = put_in_order<kThreads>(list, n, a.k, tid, put);
       } else {
         uint64_t last = ~(uint64_t)0;
         for (found = 0; found < a.k; ++found) {
@@ -653,8 +825,8 @@ __global__ __launch_bounds__(kThreads) void token_part_loss_kernel(TokenArgs a, 
   const int32_t tid = threadIdx.x;
   for (int64_t at = blockIdx.x; at < a.rows * parts.n; at += gridDim.x) {
     const int64_t row = at / parts.n;
-    const int32_t part = (int32_t)(at - row * parts.n), first = part * PartHeld<T>::kMost;
-    const int32_t n = a.V - first < PartHeld<T>::kMost ? a.V - first : PartHeld<T>::kMost;
+    const int32_t part = (int32_t)(at - row * parts.n), first = part * parts.size;
+    const int32_t n = a.V - first < parts.size ? a.V - first : parts.size;
     bool empty;
     const int32_t target = target_of(a, row, &empty);
     const T* x = static_cast<const T*>(a.logits) + row * a.stride + first;
@@ -678,7 +850,7 @@ template <class T, int NT>
 __global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, int32_t parts) {
   constexpr int kTeams = kThreads / NT;
   const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
-  const int32_t team_at = NT == 64 ? (int32_t)(threadIdx.x >> 6) : 0;
+  const int32_t team_at = NT == 64 ? __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)) : 0;
   using H = Held<T, NT, kPartVecs>;
   for (int64_t at = (int64_t)blockIdx.x * kTeams + team_at; at < a.rows * parts; at += (int64_t)gridDim.x * kTeams) {
     const int64_t row = at / parts;
@@ -744,9 +916,25 @@ TokenArgs common_args(const dpsgd_logits& d, const void* logits) {
 
 uint32_t grid_of(int64_t n) { return (uint32_t)(n < kMostWgs ? n : kMostWgs); }
 
+template <class T>
+int launch_sums_of(const TokenArgs& a, hipStream_t stream) {
+  const bool wave = a.V <= Held<T, 64, 4>::kMost;
+  const uint32_t grid = grid_of(wave ? ceil_div(a.rows, 4) : a.rows);
+  if (wave && a.entropy_out)
+    hipLaunchKernelGGL((token_sums_kernel<T, 64, true>), dim3(grid), dim3(kThreads), 0, stream, a);
+  else if (wave)
+    hipLaunchKernelGGL((token_sums_kernel<T, 64, false>), dim3(grid), dim3(kThreads), 0, stream, a);
+  else if (a.entropy_out)
+    hipLaunchKernelGGL((token_sums_kernel<T, kThreads, true>), dim3(grid), dim3(kThreads), 0, stream, a);
+  else
+    hipLaunchKernelGGL((token_sums_kernel<T, kThreads, false>), dim3(grid), dim3(kThreads), 0, stream, a);
+  return check_launch();
+}
+
 template <class T, bool LOSS>
 int launch_rows_of(const TokenArgs& a, hipStream_t stream) {
   const int64_t wave4 = Held<T, 64, 4>::kMost;
+  if (!LOSS && a.k == 0) return launch_sums_of<T>(a, stream);
   if (a.V <= wave4)
     hipLaunchKernelGGL((token_row_kernel<T, 64, 4, LOSS>), dim3(grid_of(ceil_div(a.rows, 4))), dim3(kThreads), 0, stream, a);
   else if (a.V <= 4 * wave4)
@@ -754,7 +942,7 @@ int launch_rows_of(const TokenArgs& a, hipStream_t stream) {
   else if (a.V <= 16 * wave4)
     hipLaunchKernelGGL((token_row_kernel<T, 512, 8, LOSS>), dim3(grid_of(a.rows)), dim3(512), 0, stream, a);
   else if (a.V <= 32 * wave4)
-    hipLaunchKernelGGL((token_row_kernel<T, 1024, 8, LOSS>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
+    hipLaunchKernelGGL((token_row_kernel<T, 512, 16, LOSS>), dim3(grid_of(a.rows)), dim3(512), 0, stream, a);
   else
     hipLaunchKernelGGL((token_row_kernel<T, 1024, 16, LOSS>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
   return check_launch();
@@ -764,24 +952,29 @@ int64_t part_entries(int32_t dtype) {
   return dtype == DPSGD_BF16 ? PartHeld<uint16_t>::kMost : PartHeld<float>::kMost;
 }
 
-// Whether rows are taken in parts: 1024 threads hold 64 vectors of 16 bytes a lane pair.
-bool in_parts(const dpsgd_logits& d) {
+// Whether rows are taken in parts: where no workgroup holds a row (sums alone need none
+// to), and for few long rows, for which a workgroup a row would leave the card idle.
+bool in_parts(const dpsgd_logits& d, int32_t k, bool loss) {
   const int64_t most = d.dtype == DPSGD_BF16 ? Held<uint16_t, 1024, 16>::kMost : Held<float, 1024, 16>::kMost;
-  return d.V > most;
+  if (d.B * d.T <= kFewRows && d.V > 2 * part_entries(d.dtype)) return true;
+  return (loss || k > 0) && d.V > most;
 }
 
 // The workspace: log probabilities of the rows, then the parts' sums and keys.
 struct Plan {
   size_t sums, keys, bytes;   // offsets
-  int32_t parts;              // 0: whole rows
+  int32_t parts, size;        // parts of a row (0: whole rows) and their entries
 };
 
-Plan plan_of(const dpsgd_logits& d, int32_t k) {
+Plan plan_of(const dpsgd_logits& d, int32_t k, bool loss) {
   Plan p{};
   const size_t rows = (size_t)(d.B * d.T);
   p.sums = p.keys = p.bytes = round_up(rows * sizeof(float), 16);
-  if (in_parts(d)) {
-    p.parts = (int32_t)ceil_div(d.V, part_entries(d.dtype));
+  if (in_parts(d, k, loss)) {
+    // Equal parts, of whole vectors.
+    const int64_t n = ceil_div(d.V, part_entries(d.dtype));
+    p.size = (int32_t)round_up((size_t)ceil_div(d.V, n), 64);
+    p.parts = (int32_t)ceil_div(d.V, p.size);
     p.keys = p.sums + rows * (size_t)p.parts * sizeof(float4);
     p.bytes = p.keys + rows * (size_t)p.parts * (size_t)k * sizeof(uint64_t);
   }
@@ -801,11 +994,11 @@ int launch_parts_of(const TokenArgs& a, const Parts& parts, hipStream_t stream) 
 }
 
 int launch_rows(const TokenArgs& a, const dpsgd_logits& d, void* workspace, hipStream_t stream) {
-  const Plan p = plan_of(d, a.k);
+  const Plan p = plan_of(d, a.k, a.dlogits != nullptr);
   const bool bf16 = d.dtype == DPSGD_BF16;
   if (p.parts) {
     char* ws = static_cast<char*>(workspace);
-    const Parts parts{reinterpret_cast<float4*>(ws + p.sums), reinterpret_cast<uint64_t*>(ws + p.keys), p.parts};
+    const Parts parts{reinterpret_cast<float4*>(ws + p.sums), reinterpret_cast<uint64_t*>(ws + p.keys), p.parts, p.size};
     return bf16 ? launch_parts_of<uint16_t>(a, parts, stream) : launch_parts_of<float>(a, parts, stream);
   }
   if (a.dlogits)
@@ -828,7 +1021,9 @@ int launch_backward_of(const TokenArgs& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k) { return plan_of(d, k).bytes; }
+size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k) {
+  return plan_of(d, k, k == 0).bytes;   // with k = 0 for both calls
+}
 
 int launch_token_logprobs(const dpsgd_logits& d, const void* logits, float* logprobs, float* lse,
                           float* entropy, int32_t k, int64_t* top_ids, float* top_logprobs,

@@ -471,7 +471,8 @@ def _types():
     if not _codes:
         import torch
         _codes.update({torch.float32: DPSGD_F32, torch.bfloat16: DPSGD_BF16, torch.int32: "i32",
-                       torch.int64: "i64", torch.uint8: "u8", "f32": torch.float32})
+                       torch.int64: "i64", torch.uint8: "u8", "f32": torch.float32,
+                       "bf16": torch.bfloat16, "u8": torch.uint8, "i64": torch.int64})
     return _codes
 
 
@@ -690,13 +691,43 @@ def dpsgd_global_clip_multi(layers, grads, outs, max_norm: float, norm_out=None,
 # -------------------------------------- between and behind the blocks
 
 
-def _here(name, t):
-    """Raises ValueError unless t is on the current device, whose stream the calls use."""
+_device_of = None   # torch's current device, once CUDA is initialised
+
+
+def _device():
+    """The current device, whose stream the calls use; None where there is none."""
+    global _device_of
+    if _device_of is not None:
+        return _device_of()
+    import torch
+    if not torch.cuda.is_available():
+        return None
+    torch.cuda.init()
+    _device_of = torch._C._cuda_getDevice
+    return _device_of()
+
+
+def _refuse(name, t, shape, dtype, here):
+    """Raises ValueError with what is wrong about t."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
-    import torch
-    if t.device.index != torch.cuda.current_device():
+    if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, which is not the current device")
+    if t.dtype is not dtype:
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
+
+
+def _take(name, t, shape, dtype, here):
+    """The address of t, or None; raises ValueError unless it is a contiguous tensor on
+    the device `here` of this shape and torch type."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, here)
+    return t.data_ptr()
 
 
 def _logit_rows(name, t):
@@ -704,6 +735,8 @@ def _logit_rows(name, t):
     if t.dim() != 3 or t.numel() == 0:
         raise ValueError(f"{name} must be [B, T, V] with no empty axis")
     B, T, V = t.shape
+    if t.is_contiguous():
+        return B, T, V, V
     sB, sT, sV = t.stride()
     stride = sT if T > 1 else (sB if B > 1 else V)
     if (V > 1 and sV != 1) or stride < V or (B > 1 and T > 1 and sB != T * sT):
@@ -716,26 +749,29 @@ def make_logits(logits, targets=None, scale: float = 1.0) -> dpsgd_logits:
     x[:, -1:] is taken as it lies) and the token of each position, targets [B, T] (int32
     or int64, contiguous; one outside [0, V) is an empty position), or None. scale is 1 /
     temperature. The descriptor keeps targets alive, and is for logits of this layout."""
-    _here("logits", logits)
+    here = _device()
+    if logits.get_device() != here:
+        _refuse("logits", logits, logits.shape, logits.dtype, here)
     B, T, V, stride = _logit_rows("logits", logits)
-    at, code = None, "i64"
+    code, index, at = _dtype_of(logits), DPSGD_I64, None
     if targets is not None:
-        code = _types().get(targets.dtype)
-        if code != "i32" and code != "i64":
-            raise ValueError("targets must be [B, T], int32 or int64")
-        _here("targets", targets)
-        at = _want("targets", targets, (B, T))
-    desc = dpsgd_logits(at, B, T, V, stride, DPSGD_I64 if code == "i64" else DPSGD_I32,
-                        _dtype_of(logits), scale)
+        got = _codes.get(targets.dtype)
+        if got != "i64":
+            if got != "i32":
+                raise ValueError("targets must be [B, T], int32 or int64")
+            index = DPSGD_I32
+        at = _take("targets", targets, (B, T), targets.dtype, here)
+    desc = dpsgd_logits(at, B, T, V, stride, index, code, scale)
     desc.keep = targets
     return desc
 
 
-def _want_logits(name, t, desc, stride=None):
+def _take_logits(name, t, desc, here, stride=None):
     """The address of t, rows like the descriptor's, and the entries from row to row."""
-    _here(name, t)
+    if t.get_device() != here:
+        _refuse(name, t, t.shape, t.dtype, here)
     B, T, V, s = _logit_rows(name, t)
-    if (B, T, V) != (desc.B, desc.T, desc.V) or (stride is not None and s != stride):
+    if B != desc.B or T != desc.T or V != desc.V or (stride is not None and s != stride):
         raise ValueError(f"{name} must be [{desc.B}, {desc.T}, {desc.V}] as the descriptor has it")
     if _dtype_of(t) != desc.dtype:
         raise ValueError(f"{name} has another dtype than the descriptor")
@@ -749,19 +785,18 @@ def dpsgd_token_workspace_bytes(desc: dpsgd_logits, k: int = 0) -> int:
 def dpsgd_token_logprobs(desc: dpsgd_logits, logits, logprobs=None, lse=None, entropy=None,
                          top_ids=None, top_logprobs=None, workspace=None, stream=None):
     """Any of the outputs; top_ids (int64) and top_logprobs are [B, T, k]."""
-    lib = _lib or load()
-    rows, k = (desc.B, desc.T), 0
-    for t in (top_ids, top_logprobs):
-        if t is not None:
-            k = t.shape[-1]
-            if k == 0:
-                raise ValueError("no alternatives: leave top_ids and top_logprobs out")
-    p, _ = _want_logits("logits", logits, desc, desc.stride)
+    lib, here = _lib or load(), _device()
+    f32, some = _types()["f32"], top_ids if top_logprobs is None else top_logprobs
+    k = 0 if some is None else some.shape[-1]
+    if some is not None and k == 0:
+        raise ValueError("no alternatives: leave top_ids and top_logprobs out")
+    rows, tops = (desc.B, desc.T), (desc.B, desc.T, k)
     st = lib.dpsgd_token_logprobs(
-        desc, p, _may_want("logprobs", logprobs, rows, DPSGD_F32),
-        _may_want("lse", lse, rows, DPSGD_F32), _may_want("entropy", entropy, rows, DPSGD_F32), k,
-        _may_want("top_ids", top_ids, (*rows, k), "i64"),
-        _may_want("top_logprobs", top_logprobs, (*rows, k), DPSGD_F32), *_workspace(workspace),
+        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
+        _take("logprobs", logprobs, rows, f32, here), _take("lse", lse, rows, f32, here),
+        _take("entropy", entropy, rows, f32, here), k,
+        _take("top_ids", top_ids, tops, _codes["i64"], here),
+        _take("top_logprobs", top_logprobs, tops, f32, here), *_workspace(workspace),
         _stream(stream))
     _check("dpsgd_token_logprobs", st)
 
@@ -770,30 +805,29 @@ def dpsgd_token_logprobs_backward(desc: dpsgd_logits, logits, lse, dlogits, entr
                                   grad_logprobs=None, grad_lse=None, grad_entropy=None,
                                   stream=None):
     """dlogits may be logits."""
-    lib = _lib or load()
-    rows = (desc.B, desc.T)
-    p, _ = _want_logits("logits", logits, desc, desc.stride)
-    g, g_stride = _want_logits("dlogits", dlogits, desc)
+    lib, here = _lib or load(), _device()
+    f32, rows = _types()["f32"], (desc.B, desc.T)
+    g, g_stride = _take_logits("dlogits", dlogits, desc, here)
     st = lib.dpsgd_token_logprobs_backward(
-        desc, p, _want("lse", lse, rows, DPSGD_F32),
-        _may_want("entropy", entropy, rows, DPSGD_F32),
-        _may_want("grad_logprobs", grad_logprobs, rows, DPSGD_F32),
-        _may_want("grad_lse", grad_lse, rows, DPSGD_F32),
-        _may_want("grad_entropy", grad_entropy, rows, DPSGD_F32), g, g_stride, _stream(stream))
+        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
+        _take("lse", lse, rows, f32, here), _take("entropy", entropy, rows, f32, here),
+        _take("grad_logprobs", grad_logprobs, rows, f32, here),
+        _take("grad_lse", grad_lse, rows, f32, here),
+        _take("grad_entropy", grad_entropy, rows, f32, here), g, g_stride, _stream(stream))
     _check("dpsgd_token_logprobs_backward", st)
 
 
 def dpsgd_token_loss(desc: dpsgd_logits, logits, dlogits, losses=None, weights=None, logprobs=None,
                      workspace=None, stream=None):
     """Per-example losses [B] and the gradient of their sum; dlogits may be logits."""
-    lib = _lib or load()
-    rows = (desc.B, desc.T)
-    p, _ = _want_logits("logits", logits, desc, desc.stride)
-    g, g_stride = _want_logits("dlogits", dlogits, desc)
+    lib, here = _lib or load(), _device()
+    f32, B = _types()["f32"], desc.B
+    rows = (B, desc.T)
+    g, g_stride = _take_logits("dlogits", dlogits, desc, here)
     st = lib.dpsgd_token_loss(
-        desc, p, _may_want("weights", weights, rows, DPSGD_F32),
-        _may_want("losses", losses, (desc.B,), DPSGD_F32),
-        _may_want("logprobs", logprobs, rows, DPSGD_F32), g, g_stride, *_workspace(workspace),
+        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
+        _take("weights", weights, rows, f32, here), _take("losses", losses, (B,), f32, here),
+        _take("logprobs", logprobs, rows, f32, here), g, g_stride, *_workspace(workspace),
         _stream(stream))
     _check("dpsgd_token_loss", st)
 
@@ -804,45 +838,48 @@ def make_residual_norm(x, kind: str = "layer", gamma=None, beta=None, gate=None,
     """Descriptor of the residual sum and norms over rows like x's, [B, ..., C] (every
     axis between the first and the last is a position). kind: a name of ROW_NORMS. gate
     is [C] or, one for each example, [B, C]. The descriptor keeps the parameters alive."""
-    shape, n = x.shape, x.numel()
+    shape, n, here = x.shape, x.numel(), _device()
     if len(shape) < 2 or n == 0:
         raise ValueError("x must be [B, ..., C] with no empty axis")
     if kind not in ROW_NORMS:
         raise ValueError(f"kind must be one of {sorted(ROW_NORMS)}")
-    B, C = shape[0], shape[-1]
+    B, C, code = shape[0], shape[-1], _dtype_of(x)
+    f32, c = _codes["f32"], (C,)
     each = gate is not None and gate.dim() == 2
-    affine = (gamma, beta, post_gamma, post_beta)
-    for name, t in zip(("gamma", "beta", "post_gamma", "post_beta", "gate"), (*affine, gate)):
-        if t is not None:
-            _here(name, t)
     desc = dpsgd_residual_norm(
-        B, n // (B * C), C, *(_may_want(name, t, (C,), DPSGD_F32) for name, t in
-                              zip(("gamma", "beta", "post_gamma", "post_beta"), affine)),
-        _may_want("gate", gate, (B, C) if each else (C,), DPSGD_F32), int(each), int(bool(post)),
-        ROW_NORMS[kind], _dtype_of(x), residual_scale, eps)
-    desc.keep = (*affine, gate)
+        B, n // (B * C), C, _take("gamma", gamma, c, f32, here), _take("beta", beta, c, f32, here),
+        _take("post_gamma", post_gamma, c, f32, here), _take("post_beta", post_beta, c, f32, here),
+        _take("gate", gate, (B, C) if each else c, f32, here), each, bool(post), ROW_NORMS[kind],
+        code, residual_scale, eps)
+    desc.keep = (gamma, beta, post_gamma, post_beta, gate)
     return desc
 
 
-def _may_want_rows(name, t, desc):
-    if t is None:
-        return None
-    _here(name, t)
-    return _want_rows(name, t, desc.B, desc.C, desc.B * desc.S * desc.C, desc.dtype)
+def _row_taker(desc, here):
+    """A function that gives the address of rows like the descriptor's, [B, ..., C]."""
+    B, C = desc.B, desc.C
+    n, dtype = B * desc.S * C, _types()["bf16" if desc.dtype == DPSGD_BF16 else "f32"]
 
+    def take(name, t):
+        if t is None:
+            return None
+        if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
+            _refuse(name, t, t.shape, dtype, here)
+        shape = t.shape
+        if shape[0] != B or shape[-1] != C or t.numel() != n:
+            raise ValueError(f"{name} must be [{B}, ({n // (B * C)} positions), {C}], not {list(shape)}")
+        return t.data_ptr()
 
-def _want_stats(stats, desc):
-    return _may_want("stats", stats, (desc.B, desc.S, 4), DPSGD_F32)
+    return take
 
 
 def dpsgd_residual_norm_forward(desc: dpsgd_residual_norm, x, block, r, y, stats=None, stream=None):
     """block None: r = residual_scale x; r None: not written. stats: [B, S, 4]."""
-    lib = _lib or load()
-    _types()
+    lib, here = _lib or load(), _device()
+    rows = _row_taker(desc, here)
     st = lib.dpsgd_residual_norm_forward(
-        desc, _may_want_rows("x", x, desc), _may_want_rows("block", block, desc),
-        _may_want_rows("r", r, desc), _may_want_rows("y", y, desc), _want_stats(stats, desc),
-        _stream(stream))
+        desc, rows("x", x), rows("block", block), rows("r", r), rows("y", y),
+        _take("stats", stats, (desc.B, desc.S, 4), _codes["f32"], here), _stream(stream))
     _check("dpsgd_residual_norm_forward", st)
 
 
@@ -855,16 +892,17 @@ def dpsgd_residual_norm_backward(desc: dpsgd_residual_norm, block, r, dy, dr, st
                                  dpost_gamma=None, dpost_beta=None, workspace=None, stream=None):
     """The gradients of the affine parameters are per example ([B, C]); affine_layer
     makes layers of them. Any of the results may be left out (dblock with block)."""
-    lib = _lib or load()
-    _types()
-    affine = (desc.B, desc.C)
+    lib, here = _lib or load(), _device()
+    rows = _row_taker(desc, here)
+    f32, affine = _codes["f32"], (desc.B, desc.C)
     st = lib.dpsgd_residual_norm_backward(
-        desc, *(_may_want_rows(name, t, desc) for name, t in
-                (("block", block), ("r", r), ("dy", dy), ("dr", dr))), _want_stats(stats, desc),
-        _may_want_rows("dx", dx, desc), _may_want_rows("dblock", dblock, desc),
-        *(_may_want(name, t, affine, DPSGD_F32) for name, t in
-          (("dgamma", dgamma), ("dbeta", dbeta), ("dgate", dgate), ("dpost_gamma", dpost_gamma),
-           ("dpost_beta", dpost_beta))), *_workspace(workspace), _stream(stream))
+        desc, rows("block", block), rows("r", r), rows("dy", dy), rows("dr", dr),
+        _take("stats", stats, (desc.B, desc.S, 4), f32, here), rows("dx", dx),
+        rows("dblock", dblock), _take("dgamma", dgamma, affine, f32, here),
+        _take("dbeta", dbeta, affine, f32, here), _take("dgate", dgate, affine, f32, here),
+        _take("dpost_gamma", dpost_gamma, affine, f32, here),
+        _take("dpost_beta", dpost_beta, affine, f32, here), *_workspace(workspace),
+        _stream(stream))
     _check("dpsgd_residual_norm_backward", st)
 
 
@@ -881,51 +919,52 @@ def make_states8(layers, device="cuda"):
     return ms, vs, exps
 
 
-def _tensors(name, tensors, sizes, dtype):
-    """The addresses of contiguous tensors on the current device with this torch dtype and
-    these numbers of entries."""
-    if len(tensors) != len(sizes):
-        raise ValueError(f"{name}: {len(sizes)} tensors expected, not {len(tensors)}")
-    import torch
-    arr, here = (ctypes.c_void_p * len(sizes))(), -1
-    for k, (t, n) in enumerate(zip(tensors, sizes)):
-        if t.dtype is not dtype or not t.is_cuda or t.numel() != n or not t.is_contiguous():
-            raise ValueError(f"{name}[{k}] must be a contiguous {dtype} device tensor of {n} entries")
-        here = torch.cuda.current_device() if here < 0 else here
-        if t.device.index != here:
-            raise ValueError(f"{name}[{k}] is on {t.device}, which is not the current device")
-        arr[k] = t.data_ptr()
-    return arr
+def _tensors(name, tensors, sizes, dtype, here):
+    """The addresses of contiguous tensors on the device `here` with this torch dtype and
+    these numbers of entries. Whole lists at a time: a step of many small tensors is bound
+    by these checks."""
+    n = len(sizes)
+    if len(tensors) != n:
+        raise ValueError(f"{name}: {n} tensors expected, not {len(tensors)}")
+    if ([t.numel() for t in tensors] != sizes or [t.dtype for t in tensors].count(dtype) != n
+            or [t.get_device() for t in tensors].count(here) != n
+            or not all([t.is_contiguous() for t in tensors])):
+        for k, (t, size) in enumerate(zip(tensors, sizes)):
+            if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
+                _refuse(f"{name}[{k}]", t, t.shape, dtype, here)
+            if t.numel() != size:
+                raise ValueError(f"{name}[{k}] must have {size} entries, not {t.numel()}")
+    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
 
 
-def _states8(exp_avgs, exp_avg_sqs, exponents, sizes):
-    import torch
+def _states8(exp_avgs, exp_avg_sqs, exponents, sizes, here):
+    u8 = _types()["u8"]
     blocks = [2 * -(-n // DPSGD_STATE_BLOCK) for n in sizes]
-    return (_tensors("exp_avgs", exp_avgs, sizes, torch.uint8),
-            _tensors("exp_avg_sqs", exp_avg_sqs, sizes, torch.uint8),
-            _tensors("exponents", exponents, blocks, torch.uint8))
+    return (_tensors("exp_avgs", exp_avgs, sizes, u8, here),
+            _tensors("exp_avg_sqs", exp_avg_sqs, sizes, u8, here),
+            _tensors("exponents", exponents, blocks, u8, here))
 
 
 def dpsgd_noise_adamw8_multi(layers, grads, params, exp_avgs, exp_avg_sqs, exponents, sigma, C,
                              seed, step, scale, opt, round_seed=None, noisy_outs=None,
                              stream=None):
     """round_seed: of stochastic rounding of the moments; None rounds to nearest."""
-    lib = _lib or load()
-    import torch
+    lib, here, f32 = _lib or load(), _device(), _types()["f32"]
     arr, n = _array(layers)
     sizes = _sizes(layers)
     noisy = None
     if noisy_outs is not None:
-        there = [k for k, t in enumerate(noisy_outs) if t is not None]
-        _tensors("noisy_outs", [noisy_outs[k] for k in there], [sizes[k] for k in there], torch.float32)
         if len(noisy_outs) != n:
             raise ValueError(f"noisy_outs: {n} entries expected, not {len(noisy_outs)}")
+        for k, t in enumerate(noisy_outs):
+            if t is not None:
+                _tensors("noisy_outs", [t], [sizes[k]], f32, here)
         noisy = _ptr_array(noisy_outs)
     st = lib.dpsgd_noise_adamw8_multi(
-        arr, n, _tensors("grads", grads, sizes, torch.float32),
-        _tensors("params", params, sizes, torch.float32),
-        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes), noisy, sigma, C, seed, step, scale,
-        ctypes.byref(opt), DPSGD_ROUND_NEAREST if round_seed is None else DPSGD_ROUND_STOCHASTIC,
+        arr, n, _tensors("grads", grads, sizes, f32, here),
+        _tensors("params", params, sizes, f32, here),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here), noisy, sigma, C, seed, step,
+        scale, ctypes.byref(opt), DPSGD_ROUND_NEAREST if round_seed is None else DPSGD_ROUND_STOCHASTIC,
         0 if round_seed is None else round_seed, _stream(stream))
     _check("dpsgd_noise_adamw8_multi", st)
 
@@ -933,29 +972,30 @@ def dpsgd_noise_adamw8_multi(layers, grads, params, exp_avgs, exp_avg_sqs, expon
 def dpsgd_adamw8_pack_multi(layers, exp_avgs_in, exp_avg_sqs_in, exp_avgs, exp_avg_sqs, exponents,
                             stream=None):
     """float32 moments to 8 bits."""
-    lib = _lib or load()
-    import torch
+    lib, here, f32 = _lib or load(), _device(), _types()["f32"]
     arr, n = _array(layers)
     sizes = _sizes(layers)
     st = lib.dpsgd_adamw8_pack_multi(
-        arr, n, _tensors("exp_avgs_in", exp_avgs_in, sizes, torch.float32),
-        _tensors("exp_avg_sqs_in", exp_avg_sqs_in, sizes, torch.float32),
-        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes), _stream(stream))
+        arr, n, _tensors("exp_avgs_in", exp_avgs_in, sizes, f32, here),
+        _tensors("exp_avg_sqs_in", exp_avg_sqs_in, sizes, f32, here),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here), _stream(stream))
     _check("dpsgd_adamw8_pack_multi", st)
 
 
 def dpsgd_adamw8_unpack_multi(layers, exp_avgs, exp_avg_sqs, exponents, exp_avgs_out,
                               exp_avg_sqs_out, stream=None):
     """The moments that 8-bit states stand for, all float32 or all bfloat16 (both exact)."""
-    lib = _lib or load()
+    lib, here = _lib or load(), _device()
     arr, n = _array(layers)
     sizes = _sizes(layers)
+    if len(exp_avgs_out) != n:
+        raise ValueError(f"exp_avgs_out: {n} tensors expected, not {len(exp_avgs_out)}")
     dtype = exp_avgs_out[0].dtype
     code = _dtype_of(exp_avgs_out[0])
     st = lib.dpsgd_adamw8_unpack_multi(
-        arr, n, *_states8(exp_avgs, exp_avg_sqs, exponents, sizes),
-        _tensors("exp_avgs_out", exp_avgs_out, sizes, dtype),
-        _tensors("exp_avg_sqs_out", exp_avg_sqs_out, sizes, dtype), code, _stream(stream))
+        arr, n, *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here),
+        _tensors("exp_avgs_out", exp_avgs_out, sizes, dtype, here),
+        _tensors("exp_avg_sqs_out", exp_avg_sqs_out, sizes, dtype, here), code, _stream(stream))
     _check("dpsgd_adamw8_unpack_multi", st)
 
 

@@ -308,21 +308,38 @@ def test_binding_refuses_what_the_library_cannot_see():
     with pytest.raises(ValueError):
         dpsgd.dpsgd_adamw8_pack_multi(L, [x], [x], m, v, exps)
     with pytest.raises(ValueError):
-        dpsgd._tensors("m", m, [15, 2], torch.uint8)
+        dpsgd._tensors("m", m, [15, 2], torch.uint8, -1)
 
 
 class _Elsewhere:
-    """A tensor of another device, as far as the check looks."""
+    """A tensor of another device, as far as the checks look."""
     is_cuda = True
+    device = "cuda:1"
+    dtype = "f32"
+    shape = (2, 3)
 
-    class device:
-        index = 1
+    def get_device(self):
+        return 1
+
+    def is_contiguous(self):
+        return True
+
+    def numel(self):
+        return 6
+
+    def data_ptr(self):
+        return 64
 
 
-def test_tensors_of_another_device_are_refused(monkeypatch):
-    import torch
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    with pytest.raises(ValueError, match="not the current device"):
-        dpsgd._here("x", _Elsewhere)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
-    dpsgd._here("x", _Elsewhere)
+def test_tensors_of_another_device_are_refused():
+    t = _Elsewhere()
+    assert dpsgd._take("x", t, (2, 3), "f32", 1) == 64 and dpsgd._take("x", None, (2, 3), "f32", 1) is None
+    assert list(dpsgd._tensors("x", [t], [6], "f32", 1)) == [64]
+    for call in (lambda: dpsgd._take("x", t, (2, 3), "f32", 0), lambda: dpsgd._tensors("x", [t], [6], "f32", 0)):
+        with pytest.raises(ValueError, match="not the current device"):
+            call()
+    for bad in (lambda: dpsgd._take("x", t, (3, 2), "f32", 1), lambda: dpsgd._take("x", t, (2, 3), "i32", 1),
+                lambda: dpsgd._tensors("x", [t], [7], "f32", 1), lambda: dpsgd._tensors("x", [t, t], [6], "f32", 1),
+                lambda: dpsgd._tensors("x", [t, t], [6, 5], "f32", 1)):
+        with pytest.raises(ValueError):
+            bad()
