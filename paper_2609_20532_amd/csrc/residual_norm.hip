@@ -39,7 +39,9 @@ struct RnArgs {
   const float* post_beta;
   const float* gate;
   float* grads[kGrads];  // [B][C], or null
-  float* partials;       // [B][chunks][kGrads][C]
+  float* partials;       // [n_grads][B][chunks][C]
+  int32_t n_grads;       // gradients that are asked for: which of them, and their places
+  int32_t which[kGrads], place[kGrads];
   int64_t rows;          // B S
   int64_t S;
   int32_t C, log;        // log2 of the threads of a row
@@ -47,6 +49,8 @@ struct RnArgs {
   int32_t chunks;        // backward: workgroups of an example
   int32_t gate_per_example, post, layer;
   float alpha, eps, inv_C;
+  uint32_t magic;   // division by S
+  int32_t shift;
 };
 
 // Sums of K values over the threads of each row, in all of them. For rows of more
@@ -130,6 +134,12 @@ __device__ __forceinline__ void round_to(float (&x)[V]) {
   }
 }
 
+// 1 / sqrt(x): the hardware's, and a step of Newton's iteration.
+__device__ __forceinline__ float inverse_root(float x) {
+  const float y = __builtin_amdgcn_rsqf(x), e = fmaf(-x * y, y, 1.0f);
+  return fmaf(0.5f * y, e, y);
+}
+
 // Mean (0 without `layer`) and rstd of a row in registers, channels past the end 0.
 template <int V, int NV>
 __device__ __forceinline__ float2 row_stats(const float (&x)[NV][V], const Channels<V, NV>& ch,
@@ -141,27 +151,40 @@ __device__ __forceinline__ float2 row_stats(const float (&x)[NV][V], const Chann
 #pragma unroll
       for (int c = 0; c < V; ++c) s[0] += x[j][c];
     row_sum<1>(s, a.log, lds, slot);
-    mean = s[0] / (float)a.C;
+    mean = s[0] * a.inv_C;
     s[0] = 0.0f;
-  }
 #pragma unroll
-  for (int j = 0; j < NV; ++j) {
-    if (ch.has(j)) {
+    for (int j = 0; j < NV; ++j) {
+      float t = 0.0f;
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         const float d = x[j][c] - mean;
-        s[0] = fmaf(d, d, s[0]);
+        t = fmaf(d, d, t);
       }
+      s[0] += ch.has(j) ? t : 0.0f;
     }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) s[0] = fmaf(x[j][c], x[j][c], s[0]);
   }
   row_sum<1>(s, a.log, lds, slot);
-  return make_float2(mean, 1.0f / sqrtf(s[0] / (float)a.C + a.eps));
+  return make_float2(mean, inverse_root(fmaf(s[0], a.inv_C, a.eps)));
 }
 
-template <class T, int V, int NV, int MOST>
+// Which of the workgroup's rows a thread has. WIDE: a row has whole waves, so that its
+// addresses are the same for a wave (and are kept in scalar registers).
+template <bool WIDE>
+__device__ __forceinline__ int group_of(int log) {
+  const int g = (int)threadIdx.x >> log;
+  return WIDE ? __builtin_amdgcn_readfirstlane(g) : g;
+}
+
+template <class T, int V, int NV, int MOST, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
   __shared__ float lds[2][kWaves][2];
-  const int group = (int)threadIdx.x >> a.log, groups = (int)blockDim.x >> a.log;
+  const int group = group_of<WIDE>(a.log), groups = (int)blockDim.x >> a.log;
   const int lane = (int)threadIdx.x & ((1 << a.log) - 1);
   const Channels<V, NV> ch{lane * V, V << a.log, a.C};
   int slot = 0;
@@ -171,14 +194,19 @@ __global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
   load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
   load_affine<V, NV>(a.post_beta, 0.0f, ch, pb);
   load_affine<V, NV>(a.gate_per_example ? nullptr : a.gate, 1.0f, ch, gt);
+  uint32_t example = 0xFFFFFFFFu;   // whose gate this is
   for (int i = 0; i < a.iters; ++i) {
-    const int64_t row = ((int64_t)blockIdx.x * a.iters + i) * groups + group;
-    const bool active = row < a.rows;
-    const int64_t at = row * a.C;
+    const uint32_t row = (blockIdx.x * (uint32_t)a.iters + (uint32_t)i) * (uint32_t)groups + (uint32_t)group;
+    const bool active = row < (uint32_t)a.rows;
+    const int64_t at = (int64_t)row * a.C;
     Raw<T, V> rx[NV], rb[NV];
     load_row<T, V, NV>(static_cast<const T*>(a.x) + at, ch, active, rx);
     load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active && a.block, rb);
-    if (a.gate_per_example && active) load_affine<V, NV>(a.gate + row / a.S * a.C, 1.0f, ch, gt);
+    if (a.gate_per_example && active) {
+      const uint32_t e = magic_divide(row, a.magic, a.shift);
+      if (e != example) load_affine<V, NV>(a.gate + (int64_t)e * a.C, 1.0f, ch, gt);
+      example = e;
+    }
     float x[NV][V], u[NV][V];
     widen_row<T, V, NV>(rx, x);
     widen_row<T, V, NV>(rb, u);
@@ -193,7 +221,11 @@ __global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
-      for (int c = 0; c < V; ++c) x[j][c] = ch.has(j) ? fmaf(gt[j][c], u[j][c], a.alpha * x[j][c]) : 0.0f;
+      for (int c = 0; c < V; ++c) x[j][c] = fmaf(gt[j][c], u[j][c], a.alpha * x[j][c]);
+      if (!ch.has(j)) {
+#pragma unroll
+        for (int c = 0; c < V; ++c) x[j][c] = 0.0f;
+      }
       round_to<T, V>(x[j]);
     }
     const float2 st = row_stats<V, NV>(x, ch, a, lds, slot);
@@ -209,24 +241,38 @@ __global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
   }
 }
 
-// One workgroup: some rows of one example, which its groups take in turn.
-template <class T, int V, int NV, int MOST>
+// What a backward call needs: BARE no block's values (no norm of it, no gate's gradient),
+// GATED the block as it is, POST the normed block.
+enum BackKind : int { BARE = 0, GATED = 1, POST = 2 };
+
+// One workgroup: some rows of one example, which its groups take in turn. The block's
+// side has two sums, sum dR v (v: the normed block, or the block) and sum dR: gate and
+// post_gamma are constant over an example, so dgate, dpost_gamma and dpost_beta are
+// these times constants.
+template <class T, int V, int NV, int MOST, int KIND, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   extern __shared__ __align__(16) float rn_lds[];   // [groups][C], where there are several groups
   __shared__ float lds[2][kWaves][2];
-  const int group = (int)threadIdx.x >> a.log, groups = (int)blockDim.x >> a.log;
+  const int group = group_of<WIDE>(a.log), groups = (int)blockDim.x >> a.log;
   const int lane = (int)threadIdx.x & ((1 << a.log) - 1);
   const Channels<V, NV> ch{lane * V, V << a.log, a.C};
   const int64_t example = blockIdx.x / (uint32_t)a.chunks;
   const int32_t chunk = (int32_t)(blockIdx.x - (uint32_t)example * (uint32_t)a.chunks);
-  const bool want_u = a.grads[2] != nullptr, read_block = a.block && (a.post || want_u);
+  const float* gate = a.gate ? a.gate + (a.gate_per_example ? example * a.C : 0) : nullptr;
   int slot = 0;
-  float ga[NV][V], gt[NV][V], pg[NV][V], pb[NV][V];
+  float ga[NV][V], gp[NV][V];   // gamma; gate post_gamma
   load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
-  load_affine<V, NV>(a.gate ? a.gate + (a.gate_per_example ? example * a.C : 0) : nullptr, 1.0f, ch, gt);
-  load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
-  load_affine<V, NV>(a.post_beta, 0.0f, ch, pb);
-  float acc[kGrads][NV][V] = {};
+  load_affine<V, NV>(gate, 1.0f, ch, gp);
+  if constexpr (KIND == POST) {
+    float pg[NV][V];
+    load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int c = 0; c < V; ++c) gp[j][c] *= pg[j][c];
+  }
+  constexpr int kSums = KIND == POST ? 4 : (KIND == GATED ? 3 : 2);
+  float acc[kSums][NV][V] = {};   // dy rh, dy, dR v, dR
   for (int i = 0; i < a.iters; ++i) {
     const int64_t s = ((int64_t)chunk * a.iters + i) * groups + group;
     const bool active = s < a.S;
@@ -235,7 +281,7 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
     load_row<T, V, NV>(static_cast<const T*>(a.x) + at, ch, active, rr);
     load_row<T, V, NV>(static_cast<const T*>(a.dy) + at, ch, active, rdy);
     load_row<T, V, NV>(static_cast<const T*>(a.dr) + at, ch, active && a.dr, rdr);
-    load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active && read_block, rb);
+    if constexpr (KIND != BARE) load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active, rb);
     float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (active) st = reinterpret_cast<const float4*>(a.stats)[row];
     float d[NV][V], vh[NV][V];
@@ -263,32 +309,28 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         dr[j][c] = fmaf(st.y, d[j][c] - fmaf(vh[j][c], m[1], m[0]), dr[j][c]);
+        if (!ch.has(j)) dr[j][c] = 0.0f;
         d[j][c] = a.alpha * dr[j][c];
       }
     }
     if (active && a.r) store_row<T, V, NV>(static_cast<T*>(a.r) + at, ch, d);
     if (!a.y) continue;
-    widen_row<T, V, NV>(rb, vh);
+    if constexpr (KIND != BARE) widen_row<T, V, NV>(rb, vh);
     m[0] = m[1] = 0.0f;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
-        if (!ch.has(j)) dr[j][c] = 0.0f;
-        if (a.post) vh[j][c] = ch.has(j) ? (vh[j][c] - st.z) * st.w : 0.0f;
-        const float u = a.post ? fmaf(vh[j][c], pg[j][c], pb[j][c]) : vh[j][c];
-        acc[2][j][c] = fmaf(dr[j][c], u, acc[2][j][c]);
-        const float du = gt[j][c] * dr[j][c];
-        d[j][c] = du;
-        if (a.post) {
-          acc[3][j][c] = fmaf(du, vh[j][c], acc[3][j][c]);
-          acc[4][j][c] += du;
-          d[j][c] = du * pg[j][c];
+        d[j][c] = gp[j][c] * dr[j][c];
+        if constexpr (KIND == POST) {
+          vh[j][c] = ch.has(j) ? (vh[j][c] - st.z) * st.w : 0.0f;
+          acc[3][j][c] += dr[j][c];
           m[0] += d[j][c];
           m[1] = fmaf(d[j][c], vh[j][c], m[1]);
         }
+        if constexpr (KIND != BARE) acc[2][j][c] = fmaf(dr[j][c], vh[j][c], acc[2][j][c]);
       }
-    if (a.post) {
+    if constexpr (KIND == POST) {
       row_sum<2>(m, a.log, lds, slot);
       m[0] = a.layer ? m[0] * a.inv_C : 0.0f;
       m[1] *= a.inv_C;
@@ -304,18 +346,36 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
 #pragma unroll
   for (int k = 0; k < kGrads; ++k) {
     if (!a.grads[k]) continue;
+    if (k >= (KIND == BARE ? 2 : (KIND == GATED ? 3 : kGrads))) continue;
     float* to = a.chunks == 1 ? a.grads[k] + example * a.C
-                              : a.partials + ((int64_t)blockIdx.x * kGrads + k) * a.C;
-    if (groups == 1) {
+                              : a.partials + ((int64_t)a.place[k] * gridDim.x + blockIdx.x) * a.C;
+    float v[NV][V], f[NV][V];
+    if (k >= 3) load_affine<V, NV>(gate, 1.0f, ch, f);
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (ch.has(j)) store_vec<V>(to + ch.at(j), acc[k][j]);
+    for (int j = 0; j < NV; ++j) {
+      float pg[V], pb[V];
+#pragma unroll
+      for (int c = 0; c < V; ++c) pg[c] = 1.0f, pb[c] = 0.0f;
+      if (KIND == POST && k == 2 && ch.has(j)) {
+        if (a.post_gamma) load_vec<V>(a.post_gamma + ch.at(j), pg);
+        if (a.post_beta) load_vec<V>(a.post_beta + ch.at(j), pb);
+      }
+#pragma unroll
+      for (int c = 0; c < V; ++c) {
+        if constexpr (KIND == POST)
+          v[j][c] = k < 2 ? acc[k < 2 ? k : 0][j][c]
+                          : (k == 2 ? fmaf(pb[c], acc[3][j][c], pg[c] * acc[2][j][c])
+                                    : f[j][c] * acc[k == 3 ? 2 : 3][j][c]);
+        else
+          v[j][c] = acc[k < kSums ? k : 0][j][c];
+      }
+    }
+    if (groups == 1) {
+      store_row<float, V, NV>(to, ch, v);
       continue;
     }
     __syncthreads();
-#pragma unroll
-    for (int j = 0; j < NV; ++j)
-      if (ch.has(j)) store_vec<V>(rn_lds + group * a.C + ch.at(j), acc[k][j]);
+    store_row<float, V, NV>(rn_lds + group * a.C, ch, v);
     __syncthreads();
     for (int c = threadIdx.x; c < a.C; c += blockDim.x) {
       float t = 0.0f;
@@ -325,18 +385,26 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   }
 }
 
-// One thread a channel of an example's gradient: its workgroups' sums in order.
-__global__ __launch_bounds__(kThreads) void rn_join_kernel(RnArgs a, int64_t total) {
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total;
-       i += (int64_t)gridDim.x * kThreads) {
-    const int64_t example = i / (kGrads * a.C);
-    const int32_t rest = (int32_t)(i - example * (kGrads * a.C)), k = rest / a.C;
-    float* to = a.grads[k];
-    if (!to) continue;
-    const float* from = a.partials + example * a.chunks * kGrads * a.C + rest;
-    float t = 0.0f;
-    for (int32_t c = 0; c < a.chunks; ++c) t += from[(int64_t)c * kGrads * a.C];
-    to[example * a.C + rest - k * a.C] = t;
+// The workgroups' sums of an example, 64 channels a workgroup: four threads a channel
+// add every fourth of them, in a fixed order.
+__global__ __launch_bounds__(kThreads) void rn_join_kernel(RnArgs a, int32_t blocks, int64_t wgs) {
+  __shared__ float part[4][64];
+  const int32_t c0 = (int32_t)(blockIdx.x % (uint32_t)blocks) * 64, c = c0 + ((int32_t)threadIdx.x & 63);
+  const uint32_t rest = blockIdx.x / (uint32_t)blocks;
+  const int32_t n = a.n_grads, k = (int32_t)(rest % (uint32_t)n), way = (int32_t)threadIdx.x >> 6;
+  const int64_t example = rest / (uint32_t)n;
+  float t = 0.0f;
+  if (c < a.C) {
+    const float* from = a.partials + ((int64_t)k * wgs + example * a.chunks) * a.C + c;
+#pragma unroll 8
+    for (int32_t i = way; i < a.chunks; i += 4) t += from[(int64_t)i * a.C];
+  }
+  part[way][threadIdx.x & 63] = t;
+  __syncthreads();
+  if (way == 0 && c < a.C) {
+    float* to = a.grads[a.which[k]];
+    to[example * a.C + c] = (part[0][threadIdx.x] + part[1][threadIdx.x]) +
+                            (part[2][threadIdx.x] + part[3][threadIdx.x]);
   }
 }
 
@@ -348,13 +416,13 @@ struct RnPlan {
   int64_t wgs, chunks;
 };
 
-RnPlan plan_rows(const dpsgd_residual_norm& n) {
+RnPlan plan_rows(const dpsgd_residual_norm& n, int elements) {
   RnPlan p{};
   p.V = vec_width(n.C, n.dtype == DPSGD_BF16 ? 8 : 4);
   const int64_t units = n.C / p.V;
-  // As many vectors a thread as 16 elements hold, if that leaves a wave or more; wide
-  // rows of them to keep a row within 1024 threads.
-  p.nv = p.V >= 8 ? 2 : 4;
+  // As many vectors a thread as the elements hold, if that leaves a wave or more; more of
+  // them where a row would be more than 1024 threads.
+  p.nv = elements / p.V > 4 ? 4 : elements / p.V;
   while (p.nv > 1 && units <= 64 * (p.nv / 2)) p.nv /= 2;
   while (units > (int64_t)p.nv * kMostThreads) p.nv *= 2;
   while (((int64_t)p.nv << p.log) < units) ++p.log;
@@ -363,10 +431,17 @@ RnPlan plan_rows(const dpsgd_residual_norm& n) {
   return p;
 }
 
-constexpr int64_t kForwardWgs = 4096, kBackwardWgs = 2048;
+// Elements of a thread. Forward: the work of a row that is the same for all of its
+// threads is spread over more of them with 16 (16384 rows of 4096 in bf16: 105 us, 127
+// with 8). Backward: 16 need 208 registers and spill in rows of 1024 threads (4096 rows
+// of 8192: 110 us, 371 with 16; 175 us for 16384 rows of 4096 either way).
+constexpr int kForwardElements = 16, kBackwardElements = 8;
+// Workgroups that a call is spread over. Backward: each leaves its sums, which are read
+// once more (the same rows of 4096: 175 us with 512, 196 with 1024, 200 with 256).
+constexpr int64_t kForwardWgs = 4096, kBackwardWgs = 512;
 
 RnPlan plan_forward(const dpsgd_residual_norm& n) {
-  RnPlan p = plan_rows(n);
+  RnPlan p = plan_rows(n, kForwardElements);
   const int64_t batches = ceil_div(n.B * n.S, p.groups);
   p.iters = (int)ceil_div(batches, kForwardWgs);
   p.wgs = ceil_div(batches, p.iters);
@@ -374,7 +449,7 @@ RnPlan plan_forward(const dpsgd_residual_norm& n) {
 }
 
 RnPlan plan_backward(const dpsgd_residual_norm& n) {
-  RnPlan p = plan_rows(n);
+  RnPlan p = plan_rows(n, kBackwardElements);
   while (p.threads > 64 && p.groups > 1 && p.groups / 2 >= n.S) {   // few rows: smaller workgroups
     p.threads /= 2;
     p.groups /= 2;
@@ -406,57 +481,64 @@ RnArgs common_args(const dpsgd_residual_norm& n, const RnPlan& p) {
   a.alpha = n.residual_scale;
   a.eps = n.eps;
   a.inv_C = 1.0f / (float)n.C;
+  divide_magic(n.S, &a.magic, &a.shift);
   return a;
 }
 
-template <class T, int V, int NV, bool BACK>
+// FORWARD or a BackKind.
+constexpr int FORWARD = -1;
+
+template <class T, int V, int NV, int MOST, bool WIDE, int KIND>
 void run(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
-  if (p.threads <= kThreads) {
-    if constexpr (BACK)
-      hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, kThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), lds, stream, a);
-    else
-      hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, kThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), 0, stream, a);
-  } else {
-    if constexpr (BACK)
-      hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, kMostThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), lds, stream, a);
-    else
-      hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, kMostThreads>), dim3((uint32_t)p.wgs), dim3(p.threads), 0, stream, a);
-  }
+  const dim3 grid((uint32_t)p.wgs), block(p.threads);
+  if constexpr (KIND == FORWARD)
+    hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, MOST, WIDE>), grid, block, 0, stream, a);
+  else
+    hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, MOST, KIND, WIDE>), grid, block, lds, stream, a);
 }
 
-template <class T, int V, bool BACK>
+template <class T, int V, int NV, int KIND>
+void pick_threads(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+  if (p.threads > 512) return run<T, V, NV, kMostThreads, true, KIND>(p, a, lds, stream);
+  if (p.threads > kThreads) return run<T, V, NV, 512, true, KIND>(p, a, lds, stream);
+  if constexpr (NV == 1)   // rows of less than a wave have one vector a thread
+    if (p.log < 6) return run<T, V, NV, kThreads, false, KIND>(p, a, lds, stream);
+  return run<T, V, NV, kThreads, true, KIND>(p, a, lds, stream);
+}
+
+template <class T, int V, int KIND>
 void pick_vectors(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
   switch (p.nv) {
-    case 1: return run<T, V, 1, BACK>(p, a, lds, stream);
-    case 2: return run<T, V, 2, BACK>(p, a, lds, stream);
+    case 1: return pick_threads<T, V, 1, KIND>(p, a, lds, stream);
+    case 2: return pick_threads<T, V, 2, KIND>(p, a, lds, stream);
     case 4:
-      if constexpr (V <= 4) return run<T, V, 4, BACK>(p, a, lds, stream);
+      if constexpr (V <= 4) return pick_threads<T, V, 4, KIND>(p, a, lds, stream);
       return;
     case 8:
-      if constexpr (V <= 2) return run<T, V, 8, BACK>(p, a, lds, stream);
+      if constexpr (V <= 2) return pick_threads<T, V, 8, KIND>(p, a, lds, stream);
       return;
     case 16:
-      if constexpr (V <= 1) return run<T, V, 16, BACK>(p, a, lds, stream);
+      if constexpr (V <= 1) return pick_threads<T, V, 16, KIND>(p, a, lds, stream);
       return;
   }
 }
 
-template <bool BACK>
+template <int KIND>
 int launch(const dpsgd_residual_norm& n, const RnPlan& p, const RnArgs& a, size_t lds,
            hipStream_t stream) {
   if (!launchable(p.wgs, p.threads)) return DPSGD_ERR_INVALID_ARG;
   if (n.dtype == DPSGD_BF16) {
     switch (p.V) {
-      case 8: pick_vectors<uint16_t, 8, BACK>(p, a, lds, stream); break;
-      case 4: pick_vectors<uint16_t, 4, BACK>(p, a, lds, stream); break;
-      case 2: pick_vectors<uint16_t, 2, BACK>(p, a, lds, stream); break;
-      default: pick_vectors<uint16_t, 1, BACK>(p, a, lds, stream); break;
+      case 8: pick_vectors<uint16_t, 8, KIND>(p, a, lds, stream); break;
+      case 4: pick_vectors<uint16_t, 4, KIND>(p, a, lds, stream); break;
+      case 2: pick_vectors<uint16_t, 2, KIND>(p, a, lds, stream); break;
+      default: pick_vectors<uint16_t, 1, KIND>(p, a, lds, stream); break;
     }
   } else {
     switch (p.V) {
-      case 4: pick_vectors<float, 4, BACK>(p, a, lds, stream); break;
-      case 2: pick_vectors<float, 2, BACK>(p, a, lds, stream); break;
-      default: pick_vectors<float, 1, BACK>(p, a, lds, stream); break;
+      case 4: pick_vectors<float, 4, KIND>(p, a, lds, stream); break;
+      case 2: pick_vectors<float, 2, KIND>(p, a, lds, stream); break;
+      default: pick_vectors<float, 1, KIND>(p, a, lds, stream); break;
     }
   }
   return check_launch();
@@ -479,7 +561,7 @@ int launch_residual_norm_forward(const dpsgd_residual_norm& n, const void* x, co
   a.r = r;
   a.y = y;
   a.stats = stats;
-  return launch<false>(n, p, a, 0, stream);
+  return launch<FORWARD>(n, p, a, 0, stream);
 }
 
 int launch_residual_norm_backward(const dpsgd_residual_norm& n, const void* block, const void* r,
@@ -496,17 +578,20 @@ int launch_residual_norm_backward(const dpsgd_residual_norm& n, const void* bloc
   a.r = dx;
   a.y = dblock;
   a.partials = static_cast<float*>(workspace);
-  bool any = false;
   for (int k = 0; k < kGrads; ++k) {
     a.grads[k] = grads[k];
-    any = any || grads[k];
+    if (!grads[k]) continue;
+    a.place[k] = a.n_grads;
+    a.which[a.n_grads++] = k;
   }
-  const size_t lds = any && p.groups > 1 ? (size_t)p.groups * (size_t)n.C * sizeof(float) : 0;
-  const int st = launch<true>(n, p, a, lds, stream);
-  if (st != DPSGD_OK || !any || p.chunks == 1) return st;
-  const int64_t total = n.B * kGrads * n.C, wgs = ceil_div(total, kThreads);
-  hipLaunchKernelGGL(rn_join_kernel, dim3((uint32_t)(wgs < 65536 ? wgs : 65536)), dim3(kThreads), 0,
-                     stream, a, total);
+  const size_t lds = a.n_grads && p.groups > 1 ? (size_t)p.groups * (size_t)n.C * sizeof(float) : 0;
+  const int st = n.post ? launch<POST>(n, p, a, lds, stream)
+                 : grads[2] ? launch<GATED>(n, p, a, lds, stream)
+                                : launch<BARE>(n, p, a, lds, stream);
+  if (st != DPSGD_OK || !a.n_grads || p.chunks == 1) return st;
+  const int64_t blocks = ceil_div(n.C, 64), wgs = n.B * a.n_grads * blocks;
+  if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
+  hipLaunchKernelGGL(rn_join_kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, a, (int32_t)blocks, p.wgs);
   return check_launch();
 }
 
