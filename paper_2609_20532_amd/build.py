@@ -1,5 +1,6 @@
 """Build the gfx950 HIP library ``libdpsgd.so`` and the CPU verifier library
-``libdpsgd_verifier.so`` in-tree.
+``libdpsgd_verifier.so`` in-tree, and the binding's ``_marshal`` module (addresses of
+lists of tensors).
 
 Usage: ``python -m paper_2609_20532_amd.build`` (or ``build()`` from Python).
 Every HIP source is compiled for gfx950 only. Packed fp32 instructions are
@@ -23,6 +24,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdpsgd.so")
 VERIFIER_LIB = os.path.join(PKG, "libdpsgd_verifier.so")
 VERIFIER_SOURCES = ["verifier.cpp"]
+MARSHAL_LIB = os.path.join(PKG, "_marshal.so")
 OBJ_DIR = os.path.join(PKG, "_build")
 SOURCES = ["api.hip", "noise.hip", "norms.hip", "ghost.hip", "gram32.hip", "gemm.hip", "gemm_any.hip", "gemm_tr.hip", "gemm_wide.hip",
            "skinny.hip", "api_model.hip", "embedding.hip", "group_norm.hip", "global_clip.hip",
@@ -77,14 +79,41 @@ def build_verifier(verbose: bool = False) -> str:
     return VERIFIER_LIB
 
 
+def build_marshal(verbose: bool = False) -> str:
+    """Compile the Python module ``_marshal`` against the Python and torch that run this."""
+    import sysconfig
+
+    import torch
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        raise RuntimeError("no C++ compiler found for the marshalling module")
+    base = os.path.dirname(torch.__file__)
+    tmp = MARSHAL_LIB + ".tmp"
+    cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
+           "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           os.path.join(CSRC, "marshal.cpp"), "-L", os.path.join(base, "lib"), "-ltorch_python",
+           "-ltorch_cpu", "-lc10", "-o", tmp]
+    res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    if res.returncode != 0:
+        raise RuntimeError(f"build of the marshalling module failed:\n{res.stdout}")
+    if verbose and res.stdout.strip():
+        print(res.stdout)
+    os.replace(tmp, MARSHAL_LIB)
+    return MARSHAL_LIB
+
+
 def build(verbose: bool = False) -> str:
     """Compile every HIP source and link ``libdpsgd.so`` (and build the verifier
-    library); returns the path of ``libdpsgd.so``."""
+    library and the marshalling module); returns the path of ``libdpsgd.so``."""
     os.makedirs(OBJ_DIR, exist_ok=True)
-    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+    with concurrent.futures.ThreadPoolExecutor(max_workers=len(SOURCES) + 2) as ex:
+        mar = ex.submit(build_marshal, verbose)
         ver = ex.submit(build_verifier, verbose)
         objs = list(ex.map(lambda s: _compile(s, verbose), SOURCES))
         ver.result()
+        mar.result()
     tmp = LIB + ".tmp"
     cmd = [hipcc_path(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

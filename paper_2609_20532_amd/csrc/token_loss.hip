@@ -476,13 +476,27 @@ __device__ __forceinline__ int32_t put_in_order(const uint64_t* keys, int32_t n,
   return n < k ? n : k;
 }
 
+// The upper 16 bits of the k-th largest of 256 group maxima, by one wave, from the
+// highest bit down.
+__device__ __forceinline__ void bound_of_groups(const uint32_t* group, int32_t k, int32_t lane, uint32_t* to) {
+  const uint4 g = reinterpret_cast<const uint4*>(group)[lane];
+  uint32_t least = 0;
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) {
+    const uint32_t t = least | 1u << bit;
+    const int n = __popcll(__ballot(g.x >= t)) + __popcll(__ballot(g.y >= t)) +
+                  __popcll(__ballot(g.z >= t)) + __popcll(__ballot(g.w >= t));
+    if (n >= k) least = t;
+  }
+  if (lane == 0) *to = least;
+}
+
 // The k largest entries in order: put(i, order) for i < the number that there are.
 // The entries are in 256 groups (a vector's places of one lane, the places of one, two
 // or four neighbouring lanes); at least k of the groups' largest ones are not below the
 // k-th largest of them, so entries below it are none of the k. Of V unordered entries
 // about 256 ln(256 / (256 - k)) are left, 21 for k = 20 and 74 for k = 64: they are
-// listed and put in order. The bound is found in its upper 16 bits, by one wave, from
-// the highest bit down. `first` is added to the entries' places. Where the list is too
+// listed and put in order. `first` is added to the entries' places. Where the list is too
 // short (many equal or sorted logits) the n_row entries at x are searched once for each
 // alternative.
 template <int NT, class T, class H, class P>
@@ -507,18 +521,7 @@ __device__ __forceinline__ int32_t top_entries(Team<NT>& team, const H& held, co
   }
   if (tid == 0) lds.count = 0;
   team.barrier();
-  if (tid < 64) {
-    const uint4 g = reinterpret_cast<const uint4*>(lds.group)[tid];
-    uint32_t least = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-      const uint32_t t = least | 1u << bit;
-      const int n = __popcll(__ballot(g.x >= t)) + __popcll(__ballot(g.y >= t)) +
-                    __popcll(__ballot(g.z >= t)) + __popcll(__ballot(g.w >= t));
-      if (n >= k) least = t;
-    }
-    if (tid == 0) lds.least = least;
-  }
+  if (tid < 64) bound_of_groups(lds.group, k, tid, &lds.least);
   team.barrier();
   // Entries of -inf are none.
   const uint32_t none = order_bits(-INFINITY);
@@ -750,8 +753,7 @@ template <class T>
 __global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts parts) {
   __shared__ float red[2][kThreads / 64][2];
   __shared__ uint64_t red64[kThreads / 64];
-  __shared__ uint64_t list[kListed];
-  __shared__ int32_t count;
+  __shared__ TopLds<kThreads> lists;
   Team<kThreads> team{red, 0};
   const int32_t tid = threadIdx.x;
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
@@ -774,7 +776,6 @@ __global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts
         if (a.top_ids) a.top_ids[row * a.k + i] = (int32_t)~(uint32_t)o;
         if (a.top_logprobs) a.top_logprobs[row * a.k + i] = st.logp(a.scale * logit_of(o));
       };
-      // The largest of the parts' k-th entries is not above the row's k-th.
       const auto largest = [&](uint64_t v) {
         v = wave_max_u64(v);
         if ((tid & 63) == 0) red64[tid >> 6] = v;
@@ -783,24 +784,34 @@ __global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts
         __syncthreads();
         return v;
       };
-      uint64_t least = 1;
-      for (int32_t p = tid; p < parts.n; p += kThreads) {
-        const uint64_t o = keys[(int64_t)(p + 1) * a.k - 1];
-        least = o > least ? o : least;
-      }
-      if (tid == 0) count = 0;
-      least = largest(least);
+      // The bound again, with the parts' best entries, second best ones and so on each in a
+      // group of its own.
+      const auto key = [&](int64_t i) {
+        const int64_t r = i / parts.n;
+        return keys[(i - r * parts.n) * a.k + r];
+      };
+      uint32_t g = 0;
       for (int64_t i = tid; i < all; i += kThreads) {
-        const uint64_t o = keys[i];
+        const uint32_t o = (uint32_t)(key(i) >> 32);
+        g = o > g ? o : g;
+      }
+      lists.group[tid] = g;
+      if (tid == 0) lists.count = 0;
+      __syncthreads();
+      if (tid < 64) bound_of_groups(lists.group, a.k, tid, &lists.least);
+      __syncthreads();
+      const uint64_t least = lists.least ? (uint64_t)lists.least << 32 : 1;
+      for (int64_t i = tid; i < all; i += kThreads) {
+        const uint64_t o = key(i);
         if (o >= least) {
-          const int32_t at = atomicAdd(&count, 1);
-          if (at < kListed) list[at] = o;
+          const int32_t at = atomicAdd(&lists.count, 1);
+          if (at < kListed) lists.key[at] = o;
         }
       }
       __syncthreads();
-      const int32_t n = count;
+      const int32_t n = lists.count;
       if (n <= kListed) {
-        found = put_in_order<kThreads>(list, n, a.k, tid, put);
+        found = put_in_order<kThreads>(lists.key, n, a.k, tid, put);
       } else {
         uint64_t last = ~(uint64_t)0;
         for (found = 0; found < a.k; ++found) {
@@ -884,21 +895,27 @@ __global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, i
   }
 }
 
-// losses[i] = -sum_t w logp, one wave an example.
+// losses[i] = -sum_t w logp, a team an example.
+template <int NT>
 __global__ __launch_bounds__(kThreads) void token_losses_kernel(TokenArgs a, const float* logp,
                                                                 float* losses, int64_t B, int64_t T) {
-  const int lane = threadIdx.x & 63;
-  for (int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); i < B; i += (int64_t)gridDim.x * 4) {
-    float s = 0.0f;
-    for (int64_t t = lane; t < T; t += 64) {
+  constexpr int kTeams = kThreads / NT;
+  __shared__ float red[2][NT / 64][2];
+  Team<NT> team{red, 0};
+  const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
+  const int32_t team_at = NT == 64 ? (int32_t)(threadIdx.x >> 6) : 0;
+  for (int64_t i = (int64_t)blockIdx.x * kTeams + team_at; i < B; i += (int64_t)gridDim.x * kTeams) {
+    float s = 0.0f, none = 0.0f;
+#pragma unroll 4
+    for (int64_t t = tid; t < T; t += NT) {
       const int64_t row = i * T + t;
       bool empty;
       target_of(a, row, &empty);
-      const float w = empty ? 0.0f : (a.weights ? a.weights[row] : 1.0f);
-      if (w != 0.0f) s = fmaf(-w, logp[row], s);
+      const float w = a.weights ? a.weights[row] : 1.0f, lp = logp[row];
+      if (!empty && w != 0.0f) s = fmaf(-w, lp, s);
     }
-    s = wave_total(s);
-    if (lane == 0) losses[i] = s;
+    team.sum(s, none);
+    if (tid == 0) losses[i] = s;
   }
 }
 
@@ -941,10 +958,10 @@ int launch_rows_of(const TokenArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL((token_row_kernel<T, 256, 4, LOSS>), dim3(grid_of(a.rows)), dim3(256), 0, stream, a);
   else if (a.V <= 16 * wave4)
     hipLaunchKernelGGL((token_row_kernel<T, 512, 8, LOSS>), dim3(grid_of(a.rows)), dim3(512), 0, stream, a);
-  else if (a.V <= 32 * wave4)
+  else if (!LOSS || a.V <= 32 * wave4)
     hipLaunchKernelGGL((token_row_kernel<T, 512, 16, LOSS>), dim3(grid_of(a.rows)), dim3(512), 0, stream, a);
-  else
-    hipLaunchKernelGGL((token_row_kernel<T, 1024, 16, LOSS>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
+  else if constexpr (LOSS)
+    hipLaunchKernelGGL((token_row_kernel<T, 1024, 16, true>), dim3(grid_of(a.rows)), dim3(1024), 0, stream, a);
   return check_launch();
 }
 
@@ -953,11 +970,16 @@ int64_t part_entries(int32_t dtype) {
 }
 
 // Whether rows are taken in parts: where no workgroup holds a row (sums alone need none
-// to), and for few long rows, for which a workgroup a row would leave the card idle.
+// to), and for few long rows, for which a workgroup a row would leave the card idle (8
+// rows of 50257 in bf16: loss 7.4 us, 8.7 by whole rows; 64: 9.0 and 9.6; 128: 11.6
+// and 10.7). Alternatives take parts where a row would be 1024 threads and one workgroup
+// a CU (2048 rows of 131072 in bf16, k = 5: 145 us, 187 by whole rows); a loss, which
+// would read its logits twice, does not (289 and 233).
 bool in_parts(const dpsgd_logits& d, int32_t k, bool loss) {
-  const int64_t most = d.dtype == DPSGD_BF16 ? Held<uint16_t, 1024, 16>::kMost : Held<float, 1024, 16>::kMost;
+  const bool bf16 = d.dtype == DPSGD_BF16;
   if (d.B * d.T <= kFewRows && d.V > 2 * part_entries(d.dtype)) return true;
-  return (loss || k > 0) && d.V > most;
+  if (loss) return d.V > (bf16 ? Held<uint16_t, 1024, 16>::kMost : Held<float, 1024, 16>::kMost);
+  return k > 0 && d.V > (bf16 ? Held<uint16_t, 512, 16>::kMost : Held<float, 512, 16>::kMost);
 }
 
 // The workspace: log probabilities of the rows, then the parts' sums and keys.
@@ -1022,7 +1044,8 @@ int launch_backward_of(const TokenArgs& a, hipStream_t stream) {
 }  // namespace
 
 size_t token_workspace_bytes(const dpsgd_logits& d, int32_t k) {
-  return plan_of(d, k, k == 0).bytes;   // with k = 0 for both calls
+  const size_t bytes = plan_of(d, k, false).bytes, loss = k == 0 ? plan_of(d, 0, true).bytes : 0;
+  return bytes > loss ? bytes : loss;
 }
 
 int launch_token_logprobs(const dpsgd_logits& d, const void* logits, float* logprobs, float* lse,
@@ -1063,8 +1086,12 @@ int launch_token_loss(const dpsgd_logits& d, const void* logits, const float* we
   a.logp_out = logprobs ? logprobs : static_cast<float*>(workspace);
   const int st = launch_rows(a, d, workspace, stream);
   if (st != DPSGD_OK || !losses) return st;
-  hipLaunchKernelGGL(token_losses_kernel, dim3(grid_of(ceil_div(d.B, 4))), dim3(kThreads), 0,
-                     stream, a, a.logp_out, losses, d.B, d.T);
+  if (d.T <= 128)
+    hipLaunchKernelGGL(token_losses_kernel<64>, dim3(grid_of(ceil_div(d.B, 4))), dim3(kThreads), 0,
+                       stream, a, a.logp_out, losses, d.B, d.T);
+  else
+    hipLaunchKernelGGL(token_losses_kernel<kThreads>, dim3(grid_of(d.B)), dim3(kThreads), 0, stream,
+                       a, a.logp_out, losses, d.B, d.T);
   return check_launch();
 }
 

@@ -919,22 +919,38 @@ def make_states8(layers, device="cuda"):
     return ms, vs, exps
 
 
+_marshal = None   # the module of csrc/marshal.cpp
+_scalar_codes = {}   # its code of a torch type
+
+
+def _load_marshal():
+    global _marshal
+    import torch  # noqa: F401  (whose libraries the module links against)
+    try:
+        from . import _marshal as module
+    except ImportError as e:
+        raise RuntimeError("paper_2609_20532_amd/_marshal.so is missing: build it with "
+                           "`python -m paper_2609_20532_amd.build`") from e
+    _scalar_codes.update({torch.uint8: 0, torch.float32: 6, torch.bfloat16: 15})
+    _marshal = module
+    return module
+
+
 def _tensors(name, tensors, sizes, dtype, here):
     """The addresses of contiguous tensors on the device `here` with this torch dtype and
-    these numbers of entries. Whole lists at a time: a step of many small tensors is bound
-    by these checks."""
-    n = len(sizes)
-    if len(tensors) != n:
-        raise ValueError(f"{name}: {n} tensors expected, not {len(tensors)}")
-    if ([t.numel() for t in tensors] != sizes or [t.dtype for t in tensors].count(dtype) != n
-            or [t.get_device() for t in tensors].count(here) != n
-            or not all([t.is_contiguous() for t in tensors])):
+    these numbers of entries."""
+    m, n = _marshal or _load_marshal(), len(sizes)
+    arr = (ctypes.c_void_p * n)()
+    if here is None or not m.addresses(tensors, sizes, _scalar_codes[dtype], here, arr):
+        if len(tensors) != n:
+            raise ValueError(f"{name}: {n} tensors expected, not {len(tensors)}")
         for k, (t, size) in enumerate(zip(tensors, sizes)):
             if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
                 _refuse(f"{name}[{k}]", t, t.shape, dtype, here)
             if t.numel() != size:
                 raise ValueError(f"{name}[{k}] must have {size} entries, not {t.numel()}")
-    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+        raise ValueError(f"{name} must be contiguous {dtype} device tensors")
+    return arr
 
 
 def _states8(exp_avgs, exp_avg_sqs, exponents, sizes, here):

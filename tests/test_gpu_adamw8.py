@@ -311,3 +311,29 @@ def test_mean_of_stochastic_rounding(dp):
     # An entry's deviation is below a step of 1/8 each time it moves: after 20 steps its
     # standard deviation is below 0.1, the mean's below 2e-4; six of them.
     assert abs(means[9] - 0.999 ** steps) <= 1.2e-3
+
+
+def test_binding_refuses_wrong_tensors(dp):
+    torch = _torch()
+    shapes = [(8, 16), (3, 5)]
+    t = Tensors(dp, shapes, [_state(s, k) for k, s in enumerate(shapes)])
+
+    def call(at, k, tensor):
+        lists = [list(x) for x in t.lists()]
+        lists[at][k] = tensor
+        dp.dpsgd_noise_adamw8_multi(t.layers, *lists, 0.0, 1.0, 0, 0, 1.0, dp.make_adamw(1e-3))
+
+    before = t.numpy(0) + t.numpy(1)
+    wrong = [(0, 1, torch.zeros(3, 4, device="cuda")), (0, 0, torch.zeros(8, 16)),
+             (1, 0, torch.zeros(16, 8, device="cuda").t()), (1, 1, torch.zeros(3, 5, dtype=torch.bfloat16, device="cuda")),
+             (2, 0, torch.zeros(8, 16, device="cuda")), (3, 1, torch.zeros(3, 6, dtype=torch.uint8, device="cuda")),
+             (4, 0, torch.zeros(2, 2, dtype=torch.uint8, device="cuda"))]
+    for at, k, tensor in wrong:
+        with pytest.raises(ValueError):
+            call(at, k, tensor)
+    with pytest.raises(ValueError):
+        dp.dpsgd_adamw8_unpack_multi(t.layers, t.m, t.v, t.exps, t.params[:1], t.params)
+    with pytest.raises(dp.DpsgdError):   # off 16 bytes
+        call(0, 1, torch.zeros(17, device="cuda")[1:16].view(3, 5))
+    torch.cuda.synchronize()
+    assert all(np.array_equal(a, b) for a, b in zip(before, t.numpy(0) + t.numpy(1)))
