@@ -707,27 +707,49 @@ def _device():
     return _device_of()
 
 
-def _refuse(name, t, shape, dtype, here):
+_marshal = None   # the module of csrc/marshal.cpp
+_F32, _BF16, _U8, _I32, _I64 = 6, 15, 0, 3, 4   # its codes of types
+_scalar_codes = {}   # by torch type
+
+
+def _load_marshal():
+    global _marshal
+    import torch  # noqa: F401  (whose libraries the module links against)
+    try:
+        from . import _marshal as module
+    except ImportError as e:
+        raise RuntimeError("paper_2609_20532_amd/_marshal.so is missing: build it with "
+                           "`python -m paper_2609_20532_amd.build`") from e
+    _scalar_codes.update({torch.float32: _F32, torch.bfloat16: _BF16, torch.uint8: _U8,
+                          torch.int32: _I32, torch.int64: _I64})
+    _marshal = module
+    return module
+
+
+def _refuse(name, t, shape, code, here):
     """Raises ValueError with what is wrong about t."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if t.get_device() != here:
         raise ValueError(f"{name} is on {t.device}, which is not the current device")
-    if t.dtype is not dtype:
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if _scalar_codes.get(t.dtype) != code:
+        raise ValueError(f"{name} must not be {t.dtype}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    if len(shape) == 4 and shape[0] == -1:
+        shape = (shape[1], f"({shape[3] // (shape[1] * shape[2])} positions)", shape[2])
     raise ValueError(f"{name} must be {list(shape)}, not {list(t.shape)}")
 
 
-def _take(name, t, shape, dtype, here):
-    """The address of t, or None; raises ValueError unless it is a contiguous tensor on
-    the device `here` of this shape and torch type."""
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.get_device() != here or t.shape != shape or not t.is_contiguous():
-        _refuse(name, t, shape, dtype, here)
-    return t.data_ptr()
+def _take(here, names, *spec):
+    """The addresses of tensors (None for None); raises ValueError unless they are
+    contiguous tensors on the device `here`. spec: tensor, shape, type code, in turn; the
+    shape (-1, B, C, n) stands for [B, ..., C] with n entries."""
+    m = _marshal or _load_marshal()
+    got = m.take(-2 if here is None else here, *spec)
+    if type(got) is int:
+        _refuse(names[got], *spec[3 * got:3 * got + 3], here)
+    return got
 
 
 def _logit_rows(name, t):
@@ -744,38 +766,52 @@ def _logit_rows(name, t):
     return B, T, V, stride
 
 
+def _logits_of(name, t, here):
+    """Address, B, T, V, entries from row to row and type code of logits."""
+    got = (_marshal or _load_marshal()).logits(-2 if here is None else here, t)
+    if got is None:
+        _logit_rows(name, t)
+        _refuse(name, t, t.shape, _scalar_codes.get(t.dtype), here)
+    return got
+
+
 def make_logits(logits, targets=None, scale: float = 1.0) -> dpsgd_logits:
     """Descriptor of logits [B, T, V] (float32 or bfloat16; a view such as x[..., :V] or
     x[:, -1:] is taken as it lies) and the token of each position, targets [B, T] (int32
     or int64, contiguous; one outside [0, V) is an empty position), or None. scale is 1 /
     temperature. The descriptor keeps targets alive, and is for logits of this layout."""
     here = _device()
-    if logits.get_device() != here:
-        _refuse("logits", logits, logits.shape, logits.dtype, here)
-    B, T, V, stride = _logit_rows("logits", logits)
-    code, index, at = _dtype_of(logits), DPSGD_I64, None
+    _, B, T, V, stride, code = _logits_of("logits", logits, here)
+    if code != _F32 and code != _BF16:
+        raise ValueError(f"float32 or bfloat16 expected, not {logits.dtype}")
+    at, index = None, _I64
     if targets is not None:
-        got = _codes.get(targets.dtype)
-        if got != "i64":
-            if got != "i32":
-                raise ValueError("targets must be [B, T], int32 or int64")
-            index = DPSGD_I32
-        at = _take("targets", targets, (B, T), targets.dtype, here)
-    desc = dpsgd_logits(at, B, T, V, stride, index, code, scale)
+        index = _scalar_codes.get(targets.dtype)
+        if index != _I64 and index != _I32:
+            raise ValueError("targets must be [B, T], int32 or int64")
+        at, = _take(here, ("targets",), targets, (B, T), index)
+    desc = dpsgd_logits(at, B, T, V, stride, DPSGD_I64 if index == _I64 else DPSGD_I32,
+                        DPSGD_F32 if code == _F32 else DPSGD_BF16, scale)
     desc.keep = targets
     return desc
 
 
-def _take_logits(name, t, desc, here, stride=None):
+def _take_logits(name, t, desc, here):
     """The address of t, rows like the descriptor's, and the entries from row to row."""
-    if t.get_device() != here:
-        _refuse(name, t, t.shape, t.dtype, here)
-    B, T, V, s = _logit_rows(name, t)
-    if B != desc.B or T != desc.T or V != desc.V or (stride is not None and s != stride):
+    p, B, T, V, stride, code = _logits_of(name, t, here)
+    if B != desc.B or T != desc.T or V != desc.V:
         raise ValueError(f"{name} must be [{desc.B}, {desc.T}, {desc.V}] as the descriptor has it")
-    if _dtype_of(t) != desc.dtype:
+    if code != (_BF16 if desc.dtype == DPSGD_BF16 else _F32):
         raise ValueError(f"{name} has another dtype than the descriptor")
-    return t.data_ptr(), s
+    return p, stride
+
+
+def _described(logits, desc, here):
+    """The address of the descriptor's logits."""
+    p, stride = _take_logits("logits", logits, desc, here)
+    if stride != desc.stride:
+        raise ValueError("logits have their rows elsewhere than the descriptor says")
+    return p
 
 
 def dpsgd_token_workspace_bytes(desc: dpsgd_logits, k: int = 0) -> int:
@@ -786,18 +822,17 @@ def dpsgd_token_logprobs(desc: dpsgd_logits, logits, logprobs=None, lse=None, en
                          top_ids=None, top_logprobs=None, workspace=None, stream=None):
     """Any of the outputs; top_ids (int64) and top_logprobs are [B, T, k]."""
     lib, here = _lib or load(), _device()
-    f32, some = _types()["f32"], top_ids if top_logprobs is None else top_logprobs
+    some = top_ids if top_logprobs is None else top_logprobs
     k = 0 if some is None else some.shape[-1]
     if some is not None and k == 0:
         raise ValueError("no alternatives: leave top_ids and top_logprobs out")
-    rows, tops = (desc.B, desc.T), (desc.B, desc.T, k)
-    st = lib.dpsgd_token_logprobs(
-        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
-        _take("logprobs", logprobs, rows, f32, here), _take("lse", lse, rows, f32, here),
-        _take("entropy", entropy, rows, f32, here), k,
-        _take("top_ids", top_ids, tops, _codes["i64"], here),
-        _take("top_logprobs", top_logprobs, tops, f32, here), *_workspace(workspace),
-        _stream(stream))
+    p, rows = _described(logits, desc, here), (desc.B, desc.T)
+    tops = (*rows, k)
+    lp, ls, en, ids, lps = _take(
+        here, ("logprobs", "lse", "entropy", "top_ids", "top_logprobs"), logprobs, rows, _F32,
+        lse, rows, _F32, entropy, rows, _F32, top_ids, tops, _I64, top_logprobs, tops, _F32)
+    st = lib.dpsgd_token_logprobs(desc, p, lp, ls, en, k, ids, lps, *_workspace(workspace),
+                                  _stream(stream))
     _check("dpsgd_token_logprobs", st)
 
 
@@ -806,14 +841,13 @@ def dpsgd_token_logprobs_backward(desc: dpsgd_logits, logits, lse, dlogits, entr
                                   stream=None):
     """dlogits may be logits."""
     lib, here = _lib or load(), _device()
-    f32, rows = _types()["f32"], (desc.B, desc.T)
-    g, g_stride = _take_logits("dlogits", dlogits, desc, here)
-    st = lib.dpsgd_token_logprobs_backward(
-        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
-        _take("lse", lse, rows, f32, here), _take("entropy", entropy, rows, f32, here),
-        _take("grad_logprobs", grad_logprobs, rows, f32, here),
-        _take("grad_lse", grad_lse, rows, f32, here),
-        _take("grad_entropy", grad_entropy, rows, f32, here), g, g_stride, _stream(stream))
+    p, rows = _described(logits, desc, here), (desc.B, desc.T)
+    ls, en, gp, gl, ge = _take(
+        here, ("lse", "entropy", "grad_logprobs", "grad_lse", "grad_entropy"), lse, rows, _F32,
+        entropy, rows, _F32, grad_logprobs, rows, _F32, grad_lse, rows, _F32, grad_entropy, rows, _F32)
+    st = lib.dpsgd_token_logprobs_backward(desc, p, ls, en, gp, gl, ge,
+                                           *_take_logits("dlogits", dlogits, desc, here),
+                                           _stream(stream))
     _check("dpsgd_token_logprobs_backward", st)
 
 
@@ -821,14 +855,12 @@ def dpsgd_token_loss(desc: dpsgd_logits, logits, dlogits, losses=None, weights=N
                      workspace=None, stream=None):
     """Per-example losses [B] and the gradient of their sum; dlogits may be logits."""
     lib, here = _lib or load(), _device()
-    f32, B = _types()["f32"], desc.B
+    p, B = _described(logits, desc, here), desc.B
     rows = (B, desc.T)
-    g, g_stride = _take_logits("dlogits", dlogits, desc, here)
-    st = lib.dpsgd_token_loss(
-        desc, _take_logits("logits", logits, desc, here, desc.stride)[0],
-        _take("weights", weights, rows, f32, here), _take("losses", losses, (B,), f32, here),
-        _take("logprobs", logprobs, rows, f32, here), g, g_stride, *_workspace(workspace),
-        _stream(stream))
+    w, loss, lp = _take(here, ("weights", "losses", "logprobs"), weights, rows, _F32, losses, (B,),
+                        _F32, logprobs, rows, _F32)
+    st = lib.dpsgd_token_loss(desc, p, w, loss, lp, *_take_logits("dlogits", dlogits, desc, here),
+                              *_workspace(workspace), _stream(stream))
     _check("dpsgd_token_loss", st)
 
 
@@ -844,43 +876,29 @@ def make_residual_norm(x, kind: str = "layer", gamma=None, beta=None, gate=None,
     if kind not in ROW_NORMS:
         raise ValueError(f"kind must be one of {sorted(ROW_NORMS)}")
     B, C, code = shape[0], shape[-1], _dtype_of(x)
-    f32, c = _codes["f32"], (C,)
     each = gate is not None and gate.dim() == 2
-    desc = dpsgd_residual_norm(
-        B, n // (B * C), C, _take("gamma", gamma, c, f32, here), _take("beta", beta, c, f32, here),
-        _take("post_gamma", post_gamma, c, f32, here), _take("post_beta", post_beta, c, f32, here),
-        _take("gate", gate, (B, C) if each else c, f32, here), each, bool(post), ROW_NORMS[kind],
-        code, residual_scale, eps)
+    c = (C,)
+    at = _take(here, ("gamma", "beta", "post_gamma", "post_beta", "gate"), gamma, c, _F32, beta, c, _F32,
+               post_gamma, c, _F32, post_beta, c, _F32, gate, (B, C) if each else c, _F32)
+    desc = dpsgd_residual_norm(B, n // (B * C), C, *at, each, bool(post), ROW_NORMS[kind], code,
+                               residual_scale, eps)
     desc.keep = (gamma, beta, post_gamma, post_beta, gate)
     return desc
 
 
-def _row_taker(desc, here):
-    """A function that gives the address of rows like the descriptor's, [B, ..., C]."""
-    B, C = desc.B, desc.C
-    n, dtype = B * desc.S * C, _types()["bf16" if desc.dtype == DPSGD_BF16 else "f32"]
-
-    def take(name, t):
-        if t is None:
-            return None
-        if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
-            _refuse(name, t, t.shape, dtype, here)
-        shape = t.shape
-        if shape[0] != B or shape[-1] != C or t.numel() != n:
-            raise ValueError(f"{name} must be [{B}, ({n // (B * C)} positions), {C}], not {list(shape)}")
-        return t.data_ptr()
-
-    return take
+def _layout_of(desc):
+    """Shape (for _take) and type code of rows like the descriptor's, and B, S, C."""
+    B, S, C = desc.B, desc.S, desc.C
+    return (-1, B, C, B * S * C), _BF16 if desc.dtype == DPSGD_BF16 else _F32, B, S, C
 
 
 def dpsgd_residual_norm_forward(desc: dpsgd_residual_norm, x, block, r, y, stats=None, stream=None):
     """block None: r = residual_scale x; r None: not written. stats: [B, S, 4]."""
     lib, here = _lib or load(), _device()
-    rows = _row_taker(desc, here)
-    st = lib.dpsgd_residual_norm_forward(
-        desc, rows("x", x), rows("block", block), rows("r", r), rows("y", y),
-        _take("stats", stats, (desc.B, desc.S, 4), _codes["f32"], here), _stream(stream))
-    _check("dpsgd_residual_norm_forward", st)
+    rows, code, B, S, _ = _layout_of(desc)
+    at = _take(here, ("x", "block", "r", "y", "stats"), x, rows, code, block, rows, code, r, rows,
+               code, y, rows, code, stats, (B, S, 4), _F32)
+    _check("dpsgd_residual_norm_forward", lib.dpsgd_residual_norm_forward(desc, *at, _stream(stream)))
 
 
 def dpsgd_residual_norm_workspace_bytes(desc: dpsgd_residual_norm) -> int:
@@ -893,16 +911,13 @@ def dpsgd_residual_norm_backward(desc: dpsgd_residual_norm, block, r, dy, dr, st
     """The gradients of the affine parameters are per example ([B, C]); affine_layer
     makes layers of them. Any of the results may be left out (dblock with block)."""
     lib, here = _lib or load(), _device()
-    rows = _row_taker(desc, here)
-    f32, affine = _codes["f32"], (desc.B, desc.C)
-    st = lib.dpsgd_residual_norm_backward(
-        desc, rows("block", block), rows("r", r), rows("dy", dy), rows("dr", dr),
-        _take("stats", stats, (desc.B, desc.S, 4), f32, here), rows("dx", dx),
-        rows("dblock", dblock), _take("dgamma", dgamma, affine, f32, here),
-        _take("dbeta", dbeta, affine, f32, here), _take("dgate", dgate, affine, f32, here),
-        _take("dpost_gamma", dpost_gamma, affine, f32, here),
-        _take("dpost_beta", dpost_beta, affine, f32, here), *_workspace(workspace),
-        _stream(stream))
+    rows, code, B, S, C = _layout_of(desc)
+    one = (B, C)
+    at = _take(here, ("block", "r", "dy", "dr", "stats", "dx", "dblock", "dgamma", "dbeta", "dgate",
+                      "dpost_gamma", "dpost_beta"), block, rows, code, r, rows, code, dy, rows, code,
+               dr, rows, code, stats, (B, S, 4), _F32, dx, rows, code, dblock, rows, code, dgamma, one,
+               _F32, dbeta, one, _F32, dgate, one, _F32, dpost_gamma, one, _F32, dpost_beta, one, _F32)
+    st = lib.dpsgd_residual_norm_backward(desc, *at, *_workspace(workspace), _stream(stream))
     _check("dpsgd_residual_norm_backward", st)
 
 
@@ -919,23 +934,6 @@ def make_states8(layers, device="cuda"):
     return ms, vs, exps
 
 
-_marshal = None   # the module of csrc/marshal.cpp
-_scalar_codes = {}   # its code of a torch type
-
-
-def _load_marshal():
-    global _marshal
-    import torch  # noqa: F401  (whose libraries the module links against)
-    try:
-        from . import _marshal as module
-    except ImportError as e:
-        raise RuntimeError("paper_2609_20532_amd/_marshal.so is missing: build it with "
-                           "`python -m paper_2609_20532_amd.build`") from e
-    _scalar_codes.update({torch.uint8: 0, torch.float32: 6, torch.bfloat16: 15})
-    _marshal = module
-    return module
-
-
 def _tensors(name, tensors, sizes, dtype, here):
     """The addresses of contiguous tensors on the device `here` with this torch dtype and
     these numbers of entries."""
@@ -946,7 +944,7 @@ def _tensors(name, tensors, sizes, dtype, here):
             raise ValueError(f"{name}: {n} tensors expected, not {len(tensors)}")
         for k, (t, size) in enumerate(zip(tensors, sizes)):
             if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
-                _refuse(f"{name}[{k}]", t, t.shape, dtype, here)
+                _refuse(f"{name}[{k}]", t, t.shape, _scalar_codes[dtype], here)
             if t.numel() != size:
                 raise ValueError(f"{name}[{k}] must have {size} entries, not {t.numel()}")
         raise ValueError(f"{name} must be contiguous {dtype} device tensors")

@@ -312,33 +312,31 @@ def test_binding_refuses_what_the_library_cannot_see():
 
 
 class _Elsewhere:
-    """A tensor of another device, as far as the checks look."""
+    """A tensor of another device, as far as the refusal looks."""
     is_cuda = True
     device = "cuda:1"
-    dtype = "f32"
-    shape = (2, 3)
 
     def get_device(self):
         return 1
 
-    def is_contiguous(self):
-        return True
-
-    def numel(self):
-        return 6
-
-    def data_ptr(self):
-        return 64
-
 
 def test_tensors_of_another_device_are_refused():
-    t = _Elsewhere()
-    assert dpsgd._take("x", t, (2, 3), "f32", 1) == 64 and dpsgd._take("x", None, (2, 3), "f32", 1) is None
+    import torch
+    m = dpsgd._load_marshal()
     with pytest.raises(ValueError, match="not the current device"):
-        dpsgd._take("x", t, (2, 3), "f32", 0)
-    for shape, dtype in (((3, 2), "f32"), ((2, 3), "i32")):
-        with pytest.raises(ValueError):
-            dpsgd._take("x", t, shape, dtype, 1)
+        dpsgd._refuse("x", _Elsewhere(), (2, 3), dpsgd._F32, 0)
+    with pytest.raises(ValueError, match="device tensor"):
+        dpsgd._take(0, ("y", "x"), None, (2,), dpsgd._F32, torch.zeros(2), (2,), dpsgd._F32)
+    with pytest.raises(ValueError, match="device tensor"):
+        dpsgd._take(None, ("x",), torch.zeros(2), (2,), dpsgd._F32)
+    assert dpsgd._take(0, ("x",), None, (2,), dpsgd._F32) == (None,)
+    assert m.take(0) == () and m.take(0, 5, (2,), 6) == 0 and m.take(0, None, 0, 0, torch.zeros(1), (1,), 6) == 1
+    for bad in ((), (0, None), ("a",), (0, torch.zeros(1), (1,), "f")):
+        with pytest.raises(TypeError):
+            m.take(*bad)
+    assert m.logits(0, torch.zeros(1, 2, 3)) is None and m.logits(0, 5) is None
+    with pytest.raises(TypeError):
+        m.logits(0)
 
 
 def test_lists_of_tensors():
