@@ -29,8 +29,11 @@ namespace {
 
 constexpr int kStateBlock = DPSGD_STATE_BLOCK;
 static_assert(kStateBlock == 4 * 64, "a wave takes a block, four entries a lane");
-constexpr int kBlocksPerWave = 4;   // blocks whose loads are in flight together
-constexpr int kBlocksPerWg = kBlocksPerWave * kThreads / 64;
+// Blocks of a wave, whose loads are in flight together: 4, or 1 where the tensors of a
+// launch are small and its time is that of one wave (kFewBlocks: 8 waves a CU).
+constexpr int kManyBlocks = 4;
+constexpr int64_t kFewBlocks = 2048;
+constexpr int blocks_per_wg(int per_wave) { return per_wave * kThreads / 64; }
 constexpr int kTopM = 15, kTopV = 31;      // code exponents that stand for the block's
 constexpr uint32_t kLowM = 32, kLowV = 48; // lowest block exponents
 constexpr uint32_t kNotFinite = 255;
@@ -180,7 +183,7 @@ __device__ __forceinline__ uint32_t largest_bits(const float (&x)[4]) {
   return b;
 }
 
-template <bool STOCHASTIC>
+template <bool STOCHASTIC, int kBlocksPerWave>
 __global__ __launch_bounds__(kThreads) void noise_adamw8_kernel(Adam8Args a) {
   const Seg8& s = seg_of(a, blockIdx.x);
   const int lane = threadIdx.x & 63;
@@ -246,6 +249,7 @@ __global__ __launch_bounds__(kThreads) void noise_adamw8_kernel(Adam8Args a) {
 }
 
 __global__ __launch_bounds__(kThreads) void adamw8_pack_kernel(Adam8Args a) {
+  constexpr int kBlocksPerWave = kManyBlocks;
   const Seg8& s = seg_of(a, blockIdx.x);
   const int lane = threadIdx.x & 63;
   const int64_t first = ((int64_t)(blockIdx.x - s.wg_begin) * (kThreads / 64) + (threadIdx.x >> 6)) *
@@ -298,7 +302,7 @@ __device__ __forceinline__ void store_values(T* p, int64_t e, int64_t n, const f
   }
 }
 
-template <class T>
+template <class T, int kBlocksPerWave>
 __global__ __launch_bounds__(kThreads) void adamw8_unpack_kernel(UnpackArgs a) {
   const UnpackSeg& s = seg_of(a, blockIdx.x);
   const int lane = threadIdx.x & 63;
@@ -328,7 +332,16 @@ __global__ __launch_bounds__(kThreads) void adamw8_unpack_kernel(UnpackArgs a) {
   }
 }
 
-int64_t wgs_of(int64_t numel) { return ceil_div(ceil_div(numel, kStateBlock), kBlocksPerWg); }
+int64_t wgs_of(int64_t numel, int per_wave) {
+  return ceil_div(ceil_div(numel, kStateBlock), blocks_per_wg(per_wave));
+}
+
+// Blocks of a wave for a launch over n tensors.
+int blocks_per_wave(const dpsgd_layer* layers, int n) {
+  int64_t blocks = 0;
+  for (int l = 0; l < n; ++l) blocks += ceil_div(layers[l].d_out * layers[l].d_in, kStateBlock);
+  return blocks <= kFewBlocks ? 1 : kManyBlocks;
+}
 
 }  // namespace
 
@@ -359,19 +372,25 @@ int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* co
     args.inv_sqrt_bc2 = (float)(1.0 / sqrt(bc2));
     args.eps = opt.eps;
     args.decay = (float)(1.0 - (double)opt.lr * (double)opt.weight_decay);
+    const int per_wave = blocks_per_wave(layers + base, n);
     int64_t wgs = 0;
     for (int l = 0; l < n; ++l) {
       const dpsgd_layer& L = layers[base + l];
       args.seg[l] = Seg8{grads[base + l], params[base + l], ms[base + l], vs[base + l],
                          exps[base + l], noisy ? noisy[base + l] : nullptr, L.d_out * L.d_in,
                          L.tensor_id, (uint32_t)wgs};
-      wgs += wgs_of(L.d_out * L.d_in);
+      wgs += wgs_of(L.d_out * L.d_in, per_wave);
     }
     if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
-    if (rounding == DPSGD_ROUND_STOCHASTIC)
-      hipLaunchKernelGGL(noise_adamw8_kernel<true>, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
+    const dim3 grid((uint32_t)wgs), block(kThreads);
+    if (rounding == DPSGD_ROUND_STOCHASTIC && per_wave == 1)
+      hipLaunchKernelGGL((noise_adamw8_kernel<true, 1>), grid, block, 0, stream, args);
+    else if (rounding == DPSGD_ROUND_STOCHASTIC)
+      hipLaunchKernelGGL((noise_adamw8_kernel<true, kManyBlocks>), grid, block, 0, stream, args);
+    else if (per_wave == 1)
+      hipLaunchKernelGGL((noise_adamw8_kernel<false, 1>), grid, block, 0, stream, args);
     else
-      hipLaunchKernelGGL(noise_adamw8_kernel<false>, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
+      hipLaunchKernelGGL((noise_adamw8_kernel<false, kManyBlocks>), grid, block, 0, stream, args);
     if (check_launch() != DPSGD_OK) return DPSGD_ERR_HIP;
   }
   return DPSGD_OK;
@@ -389,7 +408,7 @@ int launch_adamw8_pack(const dpsgd_layer* layers, int n_layers, const float* con
       const dpsgd_layer& L = layers[base + l];
       args.seg[l] = Seg8{ms_in[base + l], const_cast<float*>(vs_in[base + l]), ms[base + l],
                          vs[base + l], exps[base + l], nullptr, L.d_out * L.d_in, 0, (uint32_t)wgs};
-      wgs += wgs_of(L.d_out * L.d_in);
+      wgs += wgs_of(L.d_out * L.d_in, kManyBlocks);
     }
     if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
     hipLaunchKernelGGL(adamw8_pack_kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
@@ -405,18 +424,24 @@ int launch_adamw8_unpack(const dpsgd_layer* layers, int n_layers, const uint8_t*
     const int n = n_layers - base < kMaxLayersPerLaunch ? n_layers - base : kMaxLayersPerLaunch;
     UnpackArgs args{};
     args.n_seg = n;
+    const int per_wave = blocks_per_wave(layers + base, n);
     int64_t wgs = 0;
     for (int l = 0; l < n; ++l) {
       const dpsgd_layer& L = layers[base + l];
       args.seg[l] = UnpackSeg{ms[base + l], vs[base + l], exps[base + l], ms_out[base + l],
                               vs_out[base + l], L.d_out * L.d_in, (uint32_t)wgs};
-      wgs += wgs_of(L.d_out * L.d_in);
+      wgs += wgs_of(L.d_out * L.d_in, per_wave);
     }
     if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
-    if (out_dtype == DPSGD_BF16)
-      hipLaunchKernelGGL(adamw8_unpack_kernel<uint16_t>, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
+    const dim3 grid((uint32_t)wgs), block(kThreads);
+    if (out_dtype == DPSGD_BF16 && per_wave == 1)
+      hipLaunchKernelGGL((adamw8_unpack_kernel<uint16_t, 1>), grid, block, 0, stream, args);
+    else if (out_dtype == DPSGD_BF16)
+      hipLaunchKernelGGL((adamw8_unpack_kernel<uint16_t, kManyBlocks>), grid, block, 0, stream, args);
+    else if (per_wave == 1)
+      hipLaunchKernelGGL((adamw8_unpack_kernel<float, 1>), grid, block, 0, stream, args);
     else
-      hipLaunchKernelGGL(adamw8_unpack_kernel<float>, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
+      hipLaunchKernelGGL((adamw8_unpack_kernel<float, kManyBlocks>), grid, block, 0, stream, args);
     if (check_launch() != DPSGD_OK) return DPSGD_ERR_HIP;
   }
   return DPSGD_OK;
