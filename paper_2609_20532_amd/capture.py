@@ -19,7 +19,8 @@ cross-entropy of example i) gives every example's rows of ``G`` at once,
 because the examples of a batch do not interact. torch runs the model's own
 forward and backward (it is the producer of the captured tensors, not part
 of the DP-SGD step); the captured tensors then go through the library's
-entry points like any other layer.
+entry points like any other layer. With ``own=1`` the residual sums with the
+layer norms behind them, the loss and its gradient are the library's as well.
 
 Weights are random (no checkpoints here). The adapter's B matrix is drawn
 non-zero (a trained adapter's is; the usual zero initialisation would make
@@ -114,19 +115,60 @@ class Block(nn.Module):
                 list(self.ln2.parameters()):
             p.requires_grad_(False)
 
-    def forward(self, x):
-        B, T, d = x.shape
+    def attention(self, y):
+        """The attention's output for normed rows y."""
+        B, T, d = y.shape
         h = self.n_head
-        qkv = self.c_attn(self.ln1(x))
+        qkv = self.c_attn(y)
         q, k, v = qkv.split(d, dim=2)
         q = q.view(B, T, h, d // h).transpose(1, 2)
         k = k.view(B, T, h, d // h).transpose(1, 2)
         v = v.view(B, T, h, d // h).transpose(1, 2)
         y = F.scaled_dot_product_attention(q, k, v, is_causal=True)
-        y = y.transpose(1, 2).contiguous().view(B, T, d)
-        x = x + self.c_proj(y)
-        x = x + self.proj(F.gelu(self.fc(self.ln2(x)), approximate="tanh"))
-        return x
+        return self.c_proj(y.transpose(1, 2).contiguous().view(B, T, d))
+
+    def mlp(self, y):
+        return self.proj(F.gelu(self.fc(y), approximate="tanh"))
+
+    def forward(self, x):
+        x = x + self.attention(self.ln1(x))
+        return x + self.mlp(self.ln2(x))
+
+
+class _ResidualNorm(torch.autograd.Function):
+    """r = x + block and y = layer norm of r, with frozen parameters; without a block y
+    alone, the norm of x."""
+
+    @staticmethod
+    def forward(ctx, x, block, gamma, beta, eps):
+        from . import dpsgd
+        x = x.contiguous()
+        block = None if block is None else block.contiguous()
+        desc = dpsgd.make_residual_norm(x, "layer", gamma, beta, eps=eps)
+        r = None if block is None else torch.empty_like(x)
+        y = torch.empty_like(x)
+        stats = torch.empty(desc.B, desc.S, 4, device=x.device)
+        dpsgd.dpsgd_residual_norm_forward(desc, x, block, r, y, stats)
+        ctx.desc, ctx.has_block = desc, block is not None
+        ctx.save_for_backward(x if r is None else r, stats)
+        ctx.set_materialize_grads(False)
+        return y if r is None else (r, y)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        from . import dpsgd
+        r, stats = ctx.saved_tensors
+        dr, dy = grads if ctx.has_block else (None, grads[0])
+        dy = torch.zeros_like(r) if dy is None else dy.contiguous()
+        dr = None if dr is None else dr.contiguous()
+        dx = torch.empty_like(r) if ctx.needs_input_grad[0] else None
+        dblock = torch.empty_like(r) if ctx.has_block else None
+        ws = torch.empty(dpsgd.dpsgd_residual_norm_workspace_bytes(ctx.desc), dtype=torch.uint8,
+                         device=r.device)
+        # Without a norm or a gate of it the block's values are not read: r stands for them.
+        dpsgd.dpsgd_residual_norm_backward(ctx.desc, r if ctx.has_block else None, r, dy, dr, stats,
+                                           dx=dx, dblock=dblock, workspace=ws)
+        return dx, dblock, None, None, None
 
 
 class GPT2LoRA(nn.Module):
@@ -167,15 +209,50 @@ class GPT2LoRA(nn.Module):
         return ce.view(B, T - 1).mean(dim=1)
 
 
-def capture(model: GPT2LoRA, tokens: torch.Tensor) -> tuple[list[CapturedLayer], torch.Tensor]:
+    def own_logits(self, tokens: torch.Tensor) -> torch.Tensor:
+        """The logits [B, T, vocab], with every residual sum and the layer norm behind it
+        in one call of the library."""
+        T = tokens.shape[1]
+        x = self.wte[tokens] + self.wpe[:T]
+
+        def norm(x, block, ln):
+            return _ResidualNorm.apply(x, block, ln.weight, ln.bias, ln.eps)
+
+        y = norm(x, None, self.blocks[0].ln1)
+        for k, blk in enumerate(self.blocks):
+            x, y = norm(x, blk.attention(y), blk.ln2)
+            last = k + 1 == len(self.blocks)
+            x, y = norm(x, blk.mlp(y), self.ln_f if last else self.blocks[k + 1].ln1)
+        return F.linear(y, self.wte)
+
+    def own_backward(self, tokens: torch.Tensor) -> torch.Tensor:
+        """The losses of per_example_loss, and the backward pass of their sum: norms, loss
+        and the logits' gradient (which takes the logits' place) are the library's."""
+        from .text_conv import token_loss
+        B, T = tokens.shape
+        logits = self.own_logits(tokens)
+        # The token after each position; the last position has none.
+        targets = torch.cat([tokens[:, 1:], tokens.new_full((B, 1), -1)], dim=1)
+        weights = torch.full((B, T), 1.0 / (T - 1), device=tokens.device)
+        losses, dlogits = token_loss(logits.detach(), targets, weights)
+        logits.backward(dlogits)
+        return losses
+
+
+def capture(model: GPT2LoRA, tokens: torch.Tensor,
+            own: bool = False) -> tuple[list[CapturedLayer], torch.Tensor]:
     """One forward and one backward of sum_i L_i; returns the captured layers
     (two per block, in block order: lora_A then lora_B) and the per-example
-    losses. No parameter gradient is kept (.grad is cleared)."""
+    losses. No parameter gradient is kept (.grad is cleared). own: residual
+    sums, norms and the loss by the library (on the device), else by torch."""
     model.rec.items.clear()
     model.rec.on = True
     try:
-        losses = model.per_example_loss(tokens)
-        losses.sum().backward()
+        if own:
+            losses = model.own_backward(tokens)
+        else:
+            losses = model.per_example_loss(tokens)
+            losses.sum().backward()
     finally:
         model.rec.on = False
     for _, p in model.trainable():
@@ -194,7 +271,8 @@ def synthetic_tokens(cfg: GPT2Config, B: int, T: int, seed: int, device) -> torc
     return torch.randint(0, cfg.vocab, (B, T), generator=gen).to(device)
 
 
-def bench(B: int = 64, T: int = 128, steps: int = 10, warmup: int = 3, dtype: str = "f32") -> dict:
+def bench(B: int = 64, T: int = 128, steps: int = 10, warmup: int = 3, dtype: str = "f32",
+          own: bool = False) -> dict:
     """Times, on cuda:0, one capture (forward + backward of the GPT-2-small
     LoRA model) and the DP-SGD step on the captured tensors (per-example norms,
     clip + clipped sum, noise), each averaged over ``steps`` repetitions; the
@@ -215,7 +293,7 @@ def bench(B: int = 64, T: int = 128, steps: int = 10, warmup: int = 3, dtype: st
     for it in range(warmup + steps):
         e0, e1 = events()
         e0.record()
-        layers, _ = capture(model, tokens)
+        layers, _ = capture(model, tokens, own)
         e1.record()
         if dtype == "bf16":
             layers = [CapturedLayer(L.name, L.A.to(torch.bfloat16), L.G.to(torch.bfloat16), L.param)
@@ -242,7 +320,7 @@ def bench(B: int = 64, T: int = 128, steps: int = 10, warmup: int = 3, dtype: st
                    for L in layers)
     c, s, sp = float(np.mean(cap_ms)), float(np.mean(step_ms)), float(np.mean(sep_ms))
     return {"model": "GPT-2 small shape, LoRA r=4 alpha=8 on every c_attn (24 trainable matrices)",
-            "B": B, "T": T, "dtype": dtype, "capture_ms": c, "dp_step_ms": s,
+            "B": B, "T": T, "dtype": dtype, "own": own, "capture_ms": c, "dp_step_ms": s,
             "dp_step_ms_separate_calls": sp,
             "dp_step_fraction": s / (c + s), "captured_bytes": in_bytes,
             "dp_step_input_gbs": in_bytes / (s * 1e-3) / 1e9,
@@ -255,4 +333,5 @@ if __name__ == "__main__":
 
     args = dict(a.split("=", 1) for a in sys.argv[1:])
     print(json.dumps(bench(B=int(args.get("B", 64)), T=int(args.get("T", 128)),
-                           dtype=args.get("dtype", "f32"))), flush=True)
+                           dtype=args.get("dtype", "f32"),
+                           own=args.get("own", "0") == "1")), flush=True)

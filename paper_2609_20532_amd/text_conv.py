@@ -18,8 +18,10 @@ a bias. Group norm acts within an example, so that per-example gradients exist (
 A step is the paper's: norms over all of it, clipped sums, noise and the average; then
 one norm over the noisy gradient bounds it (``dpsgd_global_clip_multi``) and AdamW takes
 it. torch runs the convolutions' and the classifier's products and their backward; the
-lookup, group norms and everything after the backward are the library's. Weights and
-texts are random (no dataset here).
+lookup, group norms and everything after the backward are the library's. The loss with
+its gradient (``dpsgd_token_loss``) and AdamW with 8-bit moments
+(``dpsgd_noise_adamw8_multi``) can be, too: ``loss=own moments=8bit``. Weights and texts
+are random (no dataset here).
 """
 
 from __future__ import annotations
@@ -116,9 +118,10 @@ class TextConv:
     def embedding(self, ids) -> dpsgd.dpsgd_embedding:
         return dpsgd.make_embedding(ids, self.params["table"].shape, math.sqrt(self.cfg.d))
 
-    def backward(self, ids, labels):
+    def backward(self, ids, labels, own_loss: bool = False):
         """Losses [B], and what the step needs of one backward pass of their sum: the
-        layers (name, activations, output gradients) and the rows' gradients."""
+        layers (name, activations, output gradients) and the rows' gradients. own_loss:
+        the loss and its gradient by ``dpsgd_token_loss``, else by torch."""
         cfg, p = self.cfg, self.params
         B = ids.shape[0]
         record = {"rows": {}}
@@ -136,8 +139,12 @@ class TextConv:
         pooled = (x * there).sum(1) / there.sum(1).clamp(min=1.0)
         logits = F.linear(pooled, p["head"], p["bias"].view(-1))
         head = _tap(logits)
-        losses = F.cross_entropy(logits, labels, reduction="none")
-        losses.sum().backward()
+        if own_loss:
+            losses, dlogits = token_loss(logits.detach().unsqueeze(1), labels.unsqueeze(1))
+            logits.backward(dlogits.squeeze(1))
+        else:
+            losses = F.cross_entropy(logits, labels, reduction="none")
+            losses.sum().backward()
         ones = torch.ones(B, device=ids.device)
         out = []
         for k, (name, a, g) in enumerate(layers):
@@ -149,6 +156,16 @@ class TextConv:
         return losses.detach(), out, record["rows"]["rows"]
 
 
+def token_loss(logits, targets, weights=None):
+    """Per-example losses [B] of logits [B, T, V] (weights [B, T]; None: 1) and the gradient
+    of their sum, which takes the logits' place."""
+    losses = torch.empty(logits.shape[0], device=logits.device)
+    desc = dpsgd.make_logits(logits, targets)
+    ws = torch.empty(dpsgd.dpsgd_token_workspace_bytes(desc), dtype=torch.uint8, device=logits.device)
+    dpsgd.dpsgd_token_loss(desc, logits, logits, losses=losses, weights=weights, workspace=ws)
+    return losses, logits
+
+
 def _tap(t):
     """A list that the backward pass leaves t's gradient in."""
     got = []
@@ -157,19 +174,28 @@ def _tap(t):
 
 
 class PrivateTrainer:
-    """The private step over a TextConv's parameters, its buffers and AdamW's moments."""
+    """The private step over a TextConv's parameters, its buffers and AdamW's moments:
+    float32 (8 bytes a parameter), or with moments="8bit" 2 bytes a parameter, rounded
+    stochastically. own_loss as in TextConv.backward."""
 
     def __init__(self, model: TextConv, C: float, sigma: float, seed: int, lr: float = 1e-3,
-                 max_norm: float = math.inf, weight_decay: float = 0.01):
+                 max_norm: float = math.inf, weight_decay: float = 0.01, moments: str = "float32",
+                 own_loss: bool = False):
         dpsgd.load()
+        if moments not in ("float32", "8bit"):
+            raise ValueError("moments must be 'float32' or '8bit'")
+        self.moments, self.own_loss = moments, own_loss
         self.model, self.C, self.sigma, self.seed = model, C, sigma, seed
         self.lr, self.max_norm, self.weight_decay = lr, max_norm, weight_decay
         self.names = list(model.params)
         self.shapes = [dpsgd.shape_layer(1, 1, p.shape[1], p.shape[0], dpsgd.DPSGD_F32, k)
                        for k, p in enumerate(model.params.values())]
         dev = model.params["table"].device
-        self.grads, self.m, self.v = ([torch.zeros_like(p) for p in model.params.values()]
-                                      for _ in range(3))
+        self.grads = [torch.zeros_like(p) for p in model.params.values()]
+        if moments == "8bit":
+            self.m, self.v, self.exponents = dpsgd.make_states8(self.shapes, dev)
+        else:
+            self.m, self.v = ([torch.zeros_like(p) for p in model.params.values()] for _ in range(2))
         self.norm = torch.empty(1, device=dev)   # of the noisy gradient, before clipping
         self.clip_ws = torch.empty(dpsgd.dpsgd_global_norm_workspace_bytes(self.shapes),
                                    dtype=torch.uint8, device=dev)
@@ -178,7 +204,7 @@ class PrivateTrainer:
     def sums(self, ids, labels):
         """Losses, squared per-example norms over every parameter, clip factors; the
         clipped sums are in self.grads."""
-        losses, layers, rows = self.model.backward(ids, labels)
+        losses, layers, rows = self.model.backward(ids, labels, self.own_loss)
         by_name = dict(zip(self.names, range(len(self.names))))
         Ls = [dpsgd.make_layer(A, G, by_name[name]) for name, A, G in layers]
         dev, B = ids.device, ids.shape[0]
@@ -210,9 +236,15 @@ class PrivateTrainer:
                                       workspace=self.clip_ws)
         self.t += 1
         opt = dpsgd.make_adamw(self.lr, weight_decay=self.weight_decay, t=self.t)
+        params = list(self.model.params.values())
         # The noise is in the gradient already: sigma 0 adds none.
-        dpsgd.dpsgd_noise_adamw_multi(self.shapes, self.grads, list(self.model.params.values()),
-                                      self.m, self.v, 0.0, self.C, self.seed, self.t, 1.0, opt)
+        if self.moments == "8bit":
+            dpsgd.dpsgd_noise_adamw8_multi(self.shapes, self.grads, params, self.m, self.v,
+                                           self.exponents, 0.0, self.C, self.seed, self.t, 1.0, opt,
+                                           round_seed=self.seed)
+        else:
+            dpsgd.dpsgd_noise_adamw_multi(self.shapes, self.grads, params, self.m, self.v, 0.0,
+                                          self.C, self.seed, self.t, 1.0, opt)
         return losses
 
 
@@ -230,10 +262,12 @@ def synthetic_texts(cfg: TextConvConfig, B: int, T: int, seed: int, device):
     return ids.to(device), labels.to(device)
 
 
-def bench(B: int = 128, T: int = 256, steps: int = 20, sigma: float = 0.5) -> dict:
+def bench(B: int = 128, T: int = 256, steps: int = 20, sigma: float = 0.5,
+          moments: str = "float32", own_loss: bool = False) -> dict:
     """Trains on cuda:0; returns the first and the last loss and the time of a step."""
     cfg = TextConvConfig()
-    trainer = PrivateTrainer(TextConv(cfg), C=1.0, sigma=sigma, seed=7, max_norm=1.0)
+    trainer = PrivateTrainer(TextConv(cfg), C=1.0, sigma=sigma, seed=7, max_norm=1.0,
+                             moments=moments, own_loss=own_loss)
     batches = [synthetic_texts(cfg, B, T, k, "cuda") for k in range(4)]
     losses = [float(trainer.step(*batches[0]).mean())]
     torch.cuda.synchronize()
@@ -246,7 +280,7 @@ def bench(B: int = 128, T: int = 256, steps: int = 20, sigma: float = 0.5) -> di
     losses.append(float(last.mean()))
     return {"model": "text convolution, group norm, every parameter private", "B": B, "T": T,
             "parameters": sum(p.numel() for p in trainer.model.params.values()),
-            "loss_first": losses[0], "loss_last": losses[-1], "steps": steps,
+            "loss_first": losses[0], "loss_last": losses[-1], "steps": steps, "moments": moments,
             "gradient_norm": float(trainer.norm), "ms_per_step": e0.elapsed_time(e1) / steps}
 
 
@@ -257,4 +291,6 @@ if __name__ == "__main__":
     args = dict(a.split("=", 1) for a in sys.argv[1:])
     print(json.dumps(bench(B=int(args.get("B", 128)), T=int(args.get("T", 256)),
                            steps=int(args.get("steps", 20)),
-                           sigma=float(args.get("sigma", 0.5)))), flush=True)
+                           sigma=float(args.get("sigma", 0.5)),
+                           moments=args.get("moments", "float32"),
+                           own_loss=args.get("loss", "torch") == "own")), flush=True)
