@@ -134,8 +134,10 @@ __device__ __forceinline__ void round_to(float (&x)[V]) {
   }
 }
 
-// 1 / sqrt(x): the hardware's, and a step of Newton's iteration.
+// 1 / sqrt(x): the hardware's, and a step of Newton's iteration, which needs x far from
+// both ends of float32.
 __device__ __forceinline__ float inverse_root(float x) {
+  if (!(x > 0x1p-100f && x < 0x1p100f)) return 1.0f / sqrtf(x);
   const float y = __builtin_amdgcn_rsqf(x), e = fmaf(-x * y, y, 1.0f);
   return fmaf(0.5f * y, e, y);
 }

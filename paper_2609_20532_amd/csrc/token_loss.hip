@@ -258,7 +258,8 @@ struct Exponents {
 
   __device__ __forceinline__ Exponents(float scale_, float top) {
     scale = scale_;
-    m = top == -INFINITY ? 0.0f : scale * top;
+    m = scale * top;
+    if (m == -INFINITY) m = 0.0f;
     c = scale * kLog2e;
     top_c = top * c;
     near = fabsf(top_c) <= 1048576.0f;
@@ -292,8 +293,8 @@ struct RowStats {
     m = scale * top;
     S = S_;
     E = E_;
-    nan = !(S == S) || top == INFINITY;
-    none = !nan && top == -INFINITY;
+    nan = !(S == S) || m == INFINITY;
+    none = !nan && m == -INFINITY;
     log_S = logf(S);
   }
   __device__ __forceinline__ float lse() const { return nan ? NAN : (none ? -INFINITY : m + log_S); }
@@ -718,7 +719,7 @@ __global__ __launch_bounds__(kThreads) void token_part_kernel(TokenArgs a, Parts
     if (a.k > 0) {
       uint64_t* keys = parts.keys + at * a.k;
       int32_t found = 0;
-      if (S == S && top != INFINITY && top != -INFINITY)
+      if (S == S && top != INFINITY && top != -INFINITY)   // what the row is, the join says
         found = top_entries<kThreads>(team, held, x, n, mine, a.k, first, top_lds, red64,
                                       [&](int32_t i, uint64_t o) { keys[i] = o; });
       if (found + tid < a.k) keys[found + tid] = 0;
@@ -734,7 +735,8 @@ __device__ __forceinline__ RowStats join_parts(const TokenArgs& a, const Parts& 
   float top = -INFINITY;
   for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) top = fmaxf(top, sums[p].x);
   top = team.max(top);
-  const float m = top == -INFINITY ? 0.0f : a.scale * top;
+  float m = a.scale * top;
+  if (m == -INFINITY) m = 0.0f;
   float S = 0.0f, E = 0.0f;
   for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) {
     const float4 q = sums[p];

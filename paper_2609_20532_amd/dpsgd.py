@@ -752,6 +752,13 @@ def _take(here, names, *spec):
     return got
 
 
+def _room(workspace, here):
+    """Address and bytes of a workspace on the device `here`."""
+    if workspace is not None and workspace.get_device() != here:
+        _refuse("workspace", workspace, workspace.shape, None, here)
+    return _workspace(workspace)
+
+
 def _logit_rows(name, t):
     """B, T, V and the entries from a row to the next of logits [B, T, V]."""
     if t.dim() != 3 or t.numel() == 0:
@@ -831,7 +838,7 @@ def dpsgd_token_logprobs(desc: dpsgd_logits, logits, logprobs=None, lse=None, en
     lp, ls, en, ids, lps = _take(
         here, ("logprobs", "lse", "entropy", "top_ids", "top_logprobs"), logprobs, rows, _F32,
         lse, rows, _F32, entropy, rows, _F32, top_ids, tops, _I64, top_logprobs, tops, _F32)
-    st = lib.dpsgd_token_logprobs(desc, p, lp, ls, en, k, ids, lps, *_workspace(workspace),
+    st = lib.dpsgd_token_logprobs(desc, p, lp, ls, en, k, ids, lps, *_room(workspace, here),
                                   _stream(stream))
     _check("dpsgd_token_logprobs", st)
 
@@ -860,7 +867,7 @@ def dpsgd_token_loss(desc: dpsgd_logits, logits, dlogits, losses=None, weights=N
     w, loss, lp = _take(here, ("weights", "losses", "logprobs"), weights, rows, _F32, losses, (B,),
                         _F32, logprobs, rows, _F32)
     st = lib.dpsgd_token_loss(desc, p, w, loss, lp, *_take_logits("dlogits", dlogits, desc, here),
-                              *_workspace(workspace), _stream(stream))
+                              *_room(workspace, here), _stream(stream))
     _check("dpsgd_token_loss", st)
 
 
@@ -917,7 +924,7 @@ def dpsgd_residual_norm_backward(desc: dpsgd_residual_norm, block, r, dy, dr, st
                       "dpost_gamma", "dpost_beta"), block, rows, code, r, rows, code, dy, rows, code,
                dr, rows, code, stats, (B, S, 4), _F32, dx, rows, code, dblock, rows, code, dgamma, one,
                _F32, dbeta, one, _F32, dgate, one, _F32, dpost_gamma, one, _F32, dpost_beta, one, _F32)
-    st = lib.dpsgd_residual_norm_backward(desc, *at, *_workspace(workspace), _stream(stream))
+    st = lib.dpsgd_residual_norm_backward(desc, *at, *_room(workspace, here), _stream(stream))
     _check("dpsgd_residual_norm_backward", st)
 
 

@@ -287,6 +287,28 @@ def test_rows_of_one_value_and_of_nan(dp):
     assert bool(torch.isnan(out["dx"][1, 2]).all())
 
 
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_rows_of_extreme_sizes(dp, kind):
+    """Rows whose squares leave float32 at either end: the norm's 1 / sqrt is 0 (of
+    infinity) or that of eps, never NaN."""
+    torch = _torch()
+    c, p = _case(1, 4, 96, "f32", 8, 0, False, beta=False)
+    sign = torch.ones(96, device="cuda")
+    sign[1::2] = -1.0
+    for row, size in enumerate((1e25, 1e-25, 1e-42, 1.0)):
+        c["x"][0, row], c["block"][0, row] = sign * size, 0.0
+    desc = _desc(dp, c, p, kind, False, alpha=1.0, eps=1e-40)
+    r, y, st = _forward(dp, c, desc)
+    assert torch.equal(r, c["x"]) and bool(torch.isfinite(y).all())
+    gamma = p["gamma"]
+    assert bool((st[0, 0, 1] == 0).all()) and bool((y[0, 0] == 0).all())
+    # The squares of 1e-25 and below are 0 beside eps in float32.
+    for row, size in ((1, 1e-25), (2, 1e-42)):
+        ref = sign * float(np.float32(size)) * 1e20 * gamma
+        assert float(((y[0, row] - ref).abs() / ref.abs()).max()) <= 1e-3
+    assert float((y[0, 3] - sign * gamma).abs().max()) <= 32 * U
+
+
 def test_same_bits_on_another_stream_and_in_a_graph(dp):
     torch = _torch()
     c, p = _case(3, 200, 768, "bf16", 2, 2, True)

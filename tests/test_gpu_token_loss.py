@@ -171,6 +171,48 @@ def test_special_rows(dp, V, dtype):
     check_backward(dp, x, targets, 0.75, 1)
 
 
+@pytest.mark.parametrize("V", [7, 900, 9001, 140001])
+def test_scales_that_leave_float32(dp, V):
+    """z = scale x beyond float32: +inf makes a row NaN, -inf is a masked token, and a row
+    of nothing else has no distribution; products far from 0 keep their order."""
+    torch = _torch()
+    rng = np.random.default_rng(V)
+    base = rng.standard_normal(V).astype(np.float32)
+    rows = {"over": base.copy(), "under": base * np.float32(0.1), "all under": np.full(V, -2.0e38, np.float32),
+            "all under but one": np.full(V, -2.0e38, np.float32), "zeros": np.zeros(V, np.float32),
+            "large": base * np.float32(3.0e35)}
+    rows["over"][V // 2] = 2.0e38
+    rows["under"][V // 3] = -2.0e38
+    rows["all under but one"][1] = -1.0e37
+    x = _tensor(np.stack(list(rows.values()))[None], "f32")
+    targets = np.full((1, len(rows)), V // 3)
+    for scale in (8.0, 1.0):
+        # The products in float32, as they are defined.
+        with np.errstate(over="ignore"):
+            z = np.float32(scale) * x.cpu().numpy()[0]
+        for k in (0, 3):
+            _, out = run_logprobs(dp, x, torch.from_numpy(targets).cuda(), scale, k)
+            lp, lse, h, ids, lps = lo.token_logprobs(z.astype(np.float64), targets[0], 1.0, k)
+            _, L, E = _bounds(z.astype(np.float64), 1.0)
+            _close(_wide(out["logprobs"])[0], lp, L * U, "logprobs")
+            _close(_wide(out["lse"])[0], lse, L * U, "lse")
+            _close(_wide(out["entropy"])[0], h, E * U, "entropy")
+            if k:
+                for i, name in enumerate(rows):
+                    if name not in ("under", "all under but one"):   # whose z are -inf where x is not
+                        assert np.array_equal(out["top_ids"].cpu().numpy()[0, i], ids[i]), name
+        desc = dp.make_logits(x, torch.from_numpy(targets).cuda(), scale)
+        dx = torch.empty_like(x)
+        dp.dpsgd_token_loss(desc, x, dx, workspace=_ws(dp, desc))
+        with np.errstate(over="ignore"):
+            ref = scale * lo.token_gradient(z.astype(np.float64), targets[0], 1.0, g_logp=-np.ones(len(rows)))
+        got = _wide(dx)[0]
+        for i, name in enumerate(rows):
+            K, L, _ = _bounds(z[i:i + 1].astype(np.float64), 1.0)
+            p = np.abs(ref[i]) + (np.arange(V) == V // 3) * scale
+            _close(got[i], ref[i], p * (2 * (K + L) + 8) * U, name)
+
+
 def test_no_targets(dp):
     x = _logits(2, 3, 517, "bf16", 3)
     _, out = run_logprobs(dp, x, None, 1.0, 4)
