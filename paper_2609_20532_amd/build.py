@@ -91,7 +91,7 @@ def build_marshal(verbose: bool = False) -> str:
     tmp = MARSHAL_LIB + ".tmp"
     cmd = [cxx, "-O2", "-std=c++17", "-fPIC", "-shared",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
+           "-I", INCLUDE, "-I", sysconfig.get_paths()["include"], "-isystem", os.path.join(base, "include"),
            "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
            os.path.join(CSRC, "marshal.cpp"), "-L", os.path.join(base, "lib"), "-ltorch_python",
            "-ltorch_cpu", "-lc10", "-o", tmp]

@@ -7,48 +7,52 @@
 
 #include <cstdint>
 
+#include "dpsgd.h"
+
 namespace {
 
 bool plain(const at::Tensor& v, long device) {
   return v.is_cuda() && v.get_device() == device && v.layout() == at::kStrided;
 }
 
-// addresses(tensors, sizes, element, device, to): whether every tensor of the list is
-// a contiguous CUDA tensor on `device` with sizes[k] entries and the type code
-// `element`; their addresses are written to the buffer `to` (8 bytes each).
+// addresses(tensors, layers, per_block, element, device, to): whether every tensor of
+// the list is a contiguous CUDA tensor on `device` with the type code `element` and, for
+// layer k of the buffer `layers` (dpsgd_layer), d_out d_in entries, or with per_block 2
+// for every 256 of them; their addresses are written to the buffer `to` (8 bytes each).
 PyObject* addresses(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
-  if (n_args != 5) {
-    PyErr_SetString(PyExc_TypeError, "addresses(tensors, sizes, element, device, to)");
+  if (n_args != 6) {
+    PyErr_SetString(PyExc_TypeError, "addresses(tensors, layers, per_block, element, device, to)");
     return nullptr;
   }
   PyObject* tensors = PySequence_Fast(args[0], "tensors must be a list");
   if (!tensors) return nullptr;
-  PyObject* sizes = PySequence_Fast(args[1], "sizes must be a list");
-  if (!sizes) {
-    Py_DECREF(tensors);
-    return nullptr;
-  }
   PyObject* answer = nullptr;
-  Py_buffer to{};
-  const long element = PyLong_AsLong(args[2]), device = PyLong_AsLong(args[3]);
-  if (!PyErr_Occurred() && PyObject_GetBuffer(args[4], &to, PyBUF_WRITABLE) == 0) {
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(tensors);
-    bool good = n == PySequence_Fast_GET_SIZE(sizes) && n * 8 <= to.len;
-    for (Py_ssize_t k = 0; good && k < n; ++k) {
-      PyObject* t = PySequence_Fast_GET_ITEM(tensors, k);
-      const long long size = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(sizes, k));
-      good = THPVariable_Check(t) && !PyErr_Occurred();
-      if (!good) break;
-      const at::Tensor& v = THPVariable_Unpack(t);
-      good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous() &&
-             v.numel() == size;
-      if (good) static_cast<uint64_t*>(to.buf)[k] = reinterpret_cast<uint64_t>(v.data_ptr());
+  Py_buffer layers{}, to{};
+  const long per_block = PyLong_AsLong(args[2]), element = PyLong_AsLong(args[3]),
+             device = PyLong_AsLong(args[4]);
+  if (!PyErr_Occurred() && PyObject_GetBuffer(args[1], &layers, PyBUF_SIMPLE) == 0) {
+    if (PyObject_GetBuffer(args[5], &to, PyBUF_WRITABLE) == 0) {
+      const Py_ssize_t n = PySequence_Fast_GET_SIZE(tensors);
+      bool good = n * (Py_ssize_t)sizeof(dpsgd_layer) == layers.len && n * 8 <= to.len;
+      for (Py_ssize_t k = 0; good && k < n; ++k) {
+        PyObject* t = PySequence_Fast_GET_ITEM(tensors, k);
+        good = THPVariable_Check(t);
+        if (!good) break;
+        const dpsgd_layer& L = static_cast<const dpsgd_layer*>(layers.buf)[k];
+        // Sizes that the library refuses are not multiplied here.
+        const bool small = L.d_in >= 1 && L.d_out >= 1 && L.d_in < (INT64_C(1) << 31) && L.d_out < (INT64_C(1) << 31);
+        const int64_t entries = small ? L.d_in * L.d_out : -1;
+        const at::Tensor& v = THPVariable_Unpack(t);
+        good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous() &&
+               v.numel() == (per_block ? 2 * ((entries + DPSGD_STATE_BLOCK - 1) / DPSGD_STATE_BLOCK) : entries);
+        if (good) static_cast<uint64_t*>(to.buf)[k] = reinterpret_cast<uint64_t>(v.data_ptr());
+      }
+      PyBuffer_Release(&to);
+      answer = PyBool_FromLong(good);
     }
-    PyBuffer_Release(&to);
-    if (!PyErr_Occurred()) answer = PyBool_FromLong(good);
+    PyBuffer_Release(&layers);
   }
   Py_DECREF(tensors);
-  Py_DECREF(sizes);
   return answer;
 }
 

@@ -31,6 +31,7 @@ struct TokenArgs {
   const float* g_logp;
   const float* g_lse;
   const float* g_entropy;
+  float* losses;              // [rows], of examples of one position
   float* logp_out;            // the outputs may be null
   float* lse_out;
   float* entropy_out;
@@ -305,6 +306,9 @@ struct RowStats {
     return nan ? NAN : (none ? -INFINITY : (z - m) - log_S);
   }
 };
+
+// What a position adds to its example's loss.
+__device__ __forceinline__ float loss_of(float w, float logp) { return w != 0.0f ? -w * logp : 0.0f; }
 
 template <class Tm, class H>
 __device__ __forceinline__ void reduce_row(Tm& team, H& held, float scale, bool entropy,
@@ -666,6 +670,7 @@ __global__ __launch_bounds__(NT == 64 ? kThreads : NT, NVEC > 8 || (NVEC == 8 &&
     if constexpr (LOSS) {
       T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride;
       const float w = empty ? 0.0f : (a.weights ? a.weights[row] : 1.0f);
+      if (a.losses && tid == 0) a.losses[row] = loss_of(w, st.logp(a.scale * at_target));
       write_gradient<T, NT, NVEC>(held, x, g, a.V, tid, target, w, a.scale, st);
     } else if (a.k > 0) {
       int32_t found = 0;
@@ -853,6 +858,7 @@ __global__ __launch_bounds__(kThreads) void token_part_loss_kernel(TokenArgs a, 
       st = join_parts<T>(a, parts, row, target, team, &z);
     }
     if (part == 0 && tid == 0 && a.logp_out) a.logp_out[row] = empty ? 0.0f : st.logp(z);
+    if (part == 0 && tid == 0 && a.losses) a.losses[row] = loss_of(w, st.logp(z));
     write_gradient(held, x, g, n, tid, target - first, w, a.scale, st);
   }
 }
@@ -897,7 +903,7 @@ __global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, i
   }
 }
 
-// losses[i] = -sum_t w logp, a team an example.
+// losses[i] = -sum_t w logp, a team an example (T = 1: the rows' kernels write them).
 template <int NT>
 __global__ __launch_bounds__(kThreads) void token_losses_kernel(TokenArgs a, const float* logp,
                                                                 float* losses, int64_t B, int64_t T) {
@@ -1085,9 +1091,10 @@ int launch_token_loss(const dpsgd_logits& d, const void* logits, const float* we
   a.weights = weights;
   a.dlogits = dlogits;
   a.grad_stride = dlogits_stride;
-  a.logp_out = logprobs ? logprobs : static_cast<float*>(workspace);
+  a.losses = d.T == 1 ? losses : nullptr;
+  a.logp_out = logprobs || !losses || d.T == 1 ? logprobs : static_cast<float*>(workspace);
   const int st = launch_rows(a, d, workspace, stream);
-  if (st != DPSGD_OK || !losses) return st;
+  if (st != DPSGD_OK || !losses || d.T == 1) return st;
   if (d.T <= 128)
     hipLaunchKernelGGL(token_losses_kernel<64>, dim3(grid_of(ceil_div(d.B, 4))), dim3(kThreads), 0,
                        stream, a, a.logp_out, losses, d.B, d.T);

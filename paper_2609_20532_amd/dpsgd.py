@@ -941,50 +941,50 @@ def make_states8(layers, device="cuda"):
     return ms, vs, exps
 
 
-def _tensors(name, tensors, sizes, dtype, here):
-    """The addresses of contiguous tensors on the device `here` with this torch dtype and
-    these numbers of entries."""
-    m, n = _marshal or _load_marshal(), len(sizes)
-    arr = (ctypes.c_void_p * n)()
-    if here is None or not m.addresses(tensors, sizes, _scalar_codes[dtype], here, arr):
+def _tensors(name, tensors, layers, n, code, here, per_block=0):
+    """The addresses of contiguous tensors on the device `here`, one for each of the n
+    descriptors in the ctypes array `layers`, with this type code and d_out d_in entries
+    (or a pair for every block of them)."""
+    m, arr = _marshal or _load_marshal(), (ctypes.c_void_p * n)()
+    if not m.addresses(tensors, layers, per_block, code, -2 if here is None else here, arr):
         if len(tensors) != n:
             raise ValueError(f"{name}: {n} tensors expected, not {len(tensors)}")
-        for k, (t, size) in enumerate(zip(tensors, sizes)):
-            if t.dtype is not dtype or t.get_device() != here or not t.is_contiguous():
-                _refuse(f"{name}[{k}]", t, t.shape, _scalar_codes[dtype], here)
+        for k, t in enumerate(tensors):
+            size = layers[k].d_in * layers[k].d_out
+            if per_block:
+                size = 2 * -(-size // DPSGD_STATE_BLOCK)
+            if t.get_device() != here or not t.is_contiguous() or _scalar_codes.get(t.dtype) != code:
+                _refuse(f"{name}[{k}]", t, t.shape, code, here)
             if t.numel() != size:
                 raise ValueError(f"{name}[{k}] must have {size} entries, not {t.numel()}")
-        raise ValueError(f"{name} must be contiguous {dtype} device tensors")
+        raise ValueError(f"{name} must be contiguous device tensors")
     return arr
 
 
-def _states8(exp_avgs, exp_avg_sqs, exponents, sizes, here):
-    u8 = _types()["u8"]
-    blocks = [2 * -(-n // DPSGD_STATE_BLOCK) for n in sizes]
-    return (_tensors("exp_avgs", exp_avgs, sizes, u8, here),
-            _tensors("exp_avg_sqs", exp_avg_sqs, sizes, u8, here),
-            _tensors("exponents", exponents, blocks, u8, here))
+def _states8(exp_avgs, exp_avg_sqs, exponents, layers, n, here):
+    return (_tensors("exp_avgs", exp_avgs, layers, n, _U8, here),
+            _tensors("exp_avg_sqs", exp_avg_sqs, layers, n, _U8, here),
+            _tensors("exponents", exponents, layers, n, _U8, here, 1))
 
 
 def dpsgd_noise_adamw8_multi(layers, grads, params, exp_avgs, exp_avg_sqs, exponents, sigma, C,
                              seed, step, scale, opt, round_seed=None, noisy_outs=None,
                              stream=None):
     """round_seed: of stochastic rounding of the moments; None rounds to nearest."""
-    lib, here, f32 = _lib or load(), _device(), _types()["f32"]
+    lib, here = _lib or load(), _device()
     arr, n = _array(layers)
-    sizes = _sizes(layers)
     noisy = None
     if noisy_outs is not None:
         if len(noisy_outs) != n:
             raise ValueError(f"noisy_outs: {n} entries expected, not {len(noisy_outs)}")
         for k, t in enumerate(noisy_outs):
             if t is not None:
-                _tensors("noisy_outs", [t], [sizes[k]], f32, here)
+                _tensors("noisy_outs", [t], (dpsgd_layer * 1)(arr[k]), 1, _F32, here)
         noisy = _ptr_array(noisy_outs)
     st = lib.dpsgd_noise_adamw8_multi(
-        arr, n, _tensors("grads", grads, sizes, f32, here),
-        _tensors("params", params, sizes, f32, here),
-        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here), noisy, sigma, C, seed, step,
+        arr, n, _tensors("grads", grads, arr, n, _F32, here),
+        _tensors("params", params, arr, n, _F32, here),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, arr, n, here), noisy, sigma, C, seed, step,
         scale, ctypes.byref(opt), DPSGD_ROUND_NEAREST if round_seed is None else DPSGD_ROUND_STOCHASTIC,
         0 if round_seed is None else round_seed, _stream(stream))
     _check("dpsgd_noise_adamw8_multi", st)
@@ -993,13 +993,12 @@ def dpsgd_noise_adamw8_multi(layers, grads, params, exp_avgs, exp_avg_sqs, expon
 def dpsgd_adamw8_pack_multi(layers, exp_avgs_in, exp_avg_sqs_in, exp_avgs, exp_avg_sqs, exponents,
                             stream=None):
     """float32 moments to 8 bits."""
-    lib, here, f32 = _lib or load(), _device(), _types()["f32"]
+    lib, here = _lib or load(), _device()
     arr, n = _array(layers)
-    sizes = _sizes(layers)
     st = lib.dpsgd_adamw8_pack_multi(
-        arr, n, _tensors("exp_avgs_in", exp_avgs_in, sizes, f32, here),
-        _tensors("exp_avg_sqs_in", exp_avg_sqs_in, sizes, f32, here),
-        *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here), _stream(stream))
+        arr, n, _tensors("exp_avgs_in", exp_avgs_in, arr, n, _F32, here),
+        _tensors("exp_avg_sqs_in", exp_avg_sqs_in, arr, n, _F32, here),
+        *_states8(exp_avgs, exp_avg_sqs, exponents, arr, n, here), _stream(stream))
     _check("dpsgd_adamw8_pack_multi", st)
 
 
@@ -1008,15 +1007,14 @@ def dpsgd_adamw8_unpack_multi(layers, exp_avgs, exp_avg_sqs, exponents, exp_avgs
     """The moments that 8-bit states stand for, all float32 or all bfloat16 (both exact)."""
     lib, here = _lib or load(), _device()
     arr, n = _array(layers)
-    sizes = _sizes(layers)
-    if len(exp_avgs_out) != n:
+    if len(exp_avgs_out) != n or n == 0:
         raise ValueError(f"exp_avgs_out: {n} tensors expected, not {len(exp_avgs_out)}")
-    dtype = exp_avgs_out[0].dtype
     code = _dtype_of(exp_avgs_out[0])
+    element = _BF16 if code == DPSGD_BF16 else _F32
     st = lib.dpsgd_adamw8_unpack_multi(
-        arr, n, *_states8(exp_avgs, exp_avg_sqs, exponents, sizes, here),
-        _tensors("exp_avgs_out", exp_avgs_out, sizes, dtype, here),
-        _tensors("exp_avg_sqs_out", exp_avg_sqs_out, sizes, dtype, here), code, _stream(stream))
+        arr, n, *_states8(exp_avgs, exp_avg_sqs, exponents, arr, n, here),
+        _tensors("exp_avgs_out", exp_avgs_out, arr, n, element, here),
+        _tensors("exp_avg_sqs_out", exp_avg_sqs_out, arr, n, element, here), code, _stream(stream))
     _check("dpsgd_adamw8_unpack_multi", st)
 
 

@@ -307,8 +307,6 @@ def test_binding_refuses_what_the_library_cannot_see():
     assert m[0].shape == (5, 3) and v[0].dtype == torch.uint8 and exps[0].shape == (1, 2)
     with pytest.raises(ValueError):
         dpsgd.dpsgd_adamw8_pack_multi(L, [x], [x], m, v, exps)
-    with pytest.raises(ValueError):
-        dpsgd._tensors("m", m, [15, 2], torch.uint8, -1)
 
 
 class _Elsewhere:
@@ -342,18 +340,18 @@ def test_tensors_of_another_device_are_refused():
 def test_lists_of_tensors():
     import torch
     m = dpsgd._load_marshal()
+    layers = (dpsgd.dpsgd_layer * 2)(dpsgd.shape_layer(1, 1, 3, 2), dpsgd.shape_layer(1, 1, 1, 2))
     buf = (ctypes.c_void_p * 2)()
+    none = (dpsgd.dpsgd_layer * 0)()
     cpu = [torch.zeros(6), torch.zeros(2)]
-    assert not m.addresses(cpu, [6, 2], 6, -1, buf)                    # not on a device
-    assert not m.addresses(cpu, [6], 6, -1, buf) and not m.addresses([], [6], 6, 0, buf)
-    assert not m.addresses([1, 2], [6, 2], 6, 0, buf) and m.addresses([], [], 6, 0, buf)
-    assert not m.addresses([], [1, 2, 3], 6, 0, buf) and list(buf) == [None, None]
-    for bad in ((), (1, [], 6, 0, buf), ([], 1, 6, 0, buf), ([], [], "f", 0, buf), ([], [], 6, 0, b"1"),
-                (cpu, ["a", 2], 6, 0, buf)):
+    assert not m.addresses(cpu, layers, 0, 6, -1, buf)                 # not on a device
+    assert not m.addresses(cpu[:1], layers, 0, 6, -1, buf) and not m.addresses([], layers, 0, 6, 0, buf)
+    assert not m.addresses([1, 2], layers, 0, 6, 0, buf) and m.addresses([], none, 0, 6, 0, buf)
+    assert not m.addresses(cpu, layers, 0, 6, 0, (ctypes.c_void_p * 1)()) and list(buf) == [None, None]
+    for bad in ((), (1, layers, 0, 6, 0, buf), ([], 1, 0, 6, 0, buf), ([], none, 0, "f", 0, buf),
+                ([], none, 0, 6, 0, b"1"), ([], none, 0, 6, 0)):
         with pytest.raises((TypeError, BufferError)):
             m.addresses(*bad)
-    for call in (lambda: dpsgd._tensors("x", cpu, [6, 2], torch.float32, 0),
-                 lambda: dpsgd._tensors("x", cpu, [6], torch.float32, 0),
-                 lambda: dpsgd._tensors("x", cpu, [6, 2], torch.float32, None)):
+    for tensors, here in ((cpu, 0), (cpu[:1], 0), (cpu, None), (cpu, -1)):
         with pytest.raises(ValueError):
-            call()
+            dpsgd._tensors("x", tensors, layers, 2, dpsgd._F32, here)
