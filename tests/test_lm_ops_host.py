@@ -355,3 +355,12 @@ def test_lists_of_tensors():
     for tensors, here in ((cpu, 0), (cpu[:1], 0), (cpu, None), (cpu, -1)):
         with pytest.raises(ValueError):
             dpsgd._tensors("x", tensors, layers, 2, dpsgd._F32, here)
+
+
+def test_arrays_of_descriptors():
+    Ls = [dpsgd.shape_layer(2, 3, k + 1, 5, dpsgd.DPSGD_F32, k) for k in range(4)]
+    for layers in (Ls, tuple(Ls), Ls[1], Ls[:1]):
+        (a, n), (b, m) = dpsgd._layer_array(layers), dpsgd._array(layers)
+        assert n == m and bytes(a) == bytes(b)
+    with pytest.raises(TypeError):
+        dpsgd._layer_array([Ls[0], b"x" * 56])
