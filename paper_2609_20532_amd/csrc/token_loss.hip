@@ -978,14 +978,16 @@ int64_t part_entries(int32_t dtype) {
 }
 
 // Whether rows are taken in parts: where no workgroup holds a row (sums alone need none
-// to), and for few long rows, for which a workgroup a row would leave the card idle (8
-// rows of 50257 in bf16: loss 7.4 us, 8.7 by whole rows; 64: 9.0 and 9.6; 128: 11.6
-// and 10.7). Alternatives take parts where a row would be 1024 threads and one workgroup
-// a CU (2048 rows of 131072 in bf16, k = 5: 145 us, 187 by whole rows); a loss, which
-// would read its logits twice, does not (289 and 233).
+// to), and for few rows of more than 512 threads hold, for which a workgroup a row would
+// leave the card idle. Below that a second launch costs what it saves (8 rows of 32003 in
+// float32, calls in a row: 6.0 us without alternatives, 8.5 in parts; k = 5 9.1 and 10.8;
+// loss 7.1 and 8.6; of 50257 in bf16: 6.4 and 8.7, 12.7 and 11.5, 8.9 and 8.6). Alternatives
+// take parts where a row would be 1024 threads and one workgroup a CU (2048 rows of 131072
+// in bf16, k = 5: 145 us, 187 by whole rows); a loss, which would read its logits twice, does
+// not (289 and 233).
 bool in_parts(const dpsgd_logits& d, int32_t k, bool loss) {
   const bool bf16 = d.dtype == DPSGD_BF16;
-  if (d.B * d.T <= kFewRows && d.V > 2 * part_entries(d.dtype)) return true;
+  if (d.B * d.T <= kFewRows && d.V > 8 * part_entries(d.dtype)) return true;
   if (loss) return d.V > (bf16 ? Held<uint16_t, 1024, 16>::kMost : Held<float, 1024, 16>::kMost);
   return k > 0 && d.V > (bf16 ? Held<uint16_t, 512, 16>::kMost : Held<float, 512, 16>::kMost);
 }
