@@ -474,7 +474,7 @@ __device__ __forceinline__ int32_t put_in_order(const uint64_t* keys, int32_t n,
   for (int32_t i = tid; i < n; i += NT) {
     const uint64_t own = keys[i];
     int32_t rank = 0;
-#pragma unroll 8
+#pragma unroll 4
     for (int32_t j = 0; j < n; ++j) rank += keys[j] > own ? 1 : 0;
     if (rank < k) put(rank, own);
   }
@@ -641,7 +641,7 @@ __device__ __forceinline__ void write_gradient(const Held<T, NT, NVEC>& held, co
 // workgroup. LOSS: the gradient from the same registers; else the log probabilities,
 // entropy and alternatives.
 template <class T, int NT, int NVEC, bool LOSS>
-__global__ __launch_bounds__(NT == 64 ? kThreads : NT, NVEC > 8 || (NVEC == 8 && !LOSS) ? 4 : 8) void token_row_kernel(TokenArgs a) {
+__global__ __launch_bounds__(NT == 64 ? kThreads : NT, LOSS ? (NVEC > 8 ? 4 : 8) : (NVEC > 4 ? 4 : 6)) void token_row_kernel(TokenArgs a) {
   constexpr int kTeams = NT == 64 ? kThreads / 64 : 1;
   __shared__ float red[2][NT / 64][2];
   __shared__ uint64_t red64[NT / 64];
