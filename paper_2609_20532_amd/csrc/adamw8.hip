@@ -9,6 +9,11 @@
 // that a block's exponents are maxima over one wave and nothing is shared between
 // waves.
 //
+// 52.7 million entries with stochastic rounding: 153 us (846 MB, 5.5 TB/s; the moments in
+// float32 would be 1.48 GB), read back in bf16 51-59 us (316 MB). A Philox block for four
+// entries' random bits is about a quarter of the time that the arithmetic units have. 20
+// matrices of 123 thousand entries together: 5.2 and 4.0 us.
+//
 // Codes are the upper bits of a float32: a magnitude scaled by a power of two so
 // that its block's exponent becomes 15 (m) or 31 (v) has its code in bits 20 and
 // up, with float32's subnormal numbers as the code's. Rounding is an integer

@@ -13,7 +13,13 @@
 // in registers, a fixed set of channels a thread, and takes several rows: the affine
 // parameters stay in registers, and so do the per-example sums of a backward group,
 // which are joined over a workgroup's groups in LDS and over an example's workgroups
-// by a second launch.
+// by a second launch. Rows of whole waves have wave-uniform addresses.
+//
+// [16, 1024, 4096] in bf16, RMS norms on both sides and a gate: forward 103 us (537 MB,
+// 5.2 TB/s), backward 169 us (806 MB and 25 MB of partial sums, 4.9 TB/s) and 5.5 for the
+// join. [64, 128, 768], layer norm: backward 16.8 and 3.5 us (63 MB). A backward that has
+// the next row's loads in flight while one is worked on needs 150 registers and spills in
+// rows of 512 threads (238 us in place of 169).
 #include <math.h>
 
 #include "vec.h"

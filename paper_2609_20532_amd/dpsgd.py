@@ -5,7 +5,8 @@ arithmetic of the DP-SGD step: it converts torch tensors to device pointers,
 fills ``dpsgd_layer`` descriptors, passes torch's current HIP stream, and
 raises :class:`DpsgdError` on a non-zero status. torch supplies device memory
 and streams only. The library must be built (``paper_2609_20532_amd.build``);
-loading fails loudly when it is missing.
+loading fails loudly when it is missing. The calls between and behind a model's
+blocks check their tensors through the built module ``_marshal``.
 """
 
 from __future__ import annotations
