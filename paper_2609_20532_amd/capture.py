@@ -230,6 +230,8 @@ class GPT2LoRA(nn.Module):
         and the logits' gradient (which takes the logits' place) are the library's."""
         from .text_conv import token_loss
         B, T = tokens.shape
+        if T < 2:
+            raise ValueError("no position has a next token: at least two tokens an example")
         logits = self.own_logits(tokens)
         # The token after each position; the last position has none.
         targets = torch.cat([tokens[:, 1:], tokens.new_full((B, 1), -1)], dim=1)

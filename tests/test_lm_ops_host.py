@@ -364,3 +364,13 @@ def test_arrays_of_descriptors():
         assert n == m and bytes(a) == bytes(b)
     with pytest.raises(TypeError):
         dpsgd._layer_array([Ls[0], b"x" * 56])
+
+
+def test_own_capture_refuses_rows_without_a_next_token():
+    torch = pytest.importorskip("torch")
+    from paper_2609_20532_amd import capture as cap
+    cfg = cap.GPT2Config(vocab=11, n_ctx=4, n_embd=8, n_layer=1, n_head=2, r=2)
+    model = cap.GPT2LoRA(cfg)
+    with pytest.raises(ValueError, match="two tokens"):
+        cap.capture(model, torch.zeros(3, 1, dtype=torch.int64), own=True)
+    assert model.rec.on is False and not model.rec.items
