@@ -442,11 +442,18 @@ RnPlan plan_rows(const dpsgd_residual_norm& n, int elements) {
 // Elements of a thread. Forward: the work of a row that is the same for all of its
 // threads is spread over more of them with 16 (16384 rows of 4096 in bf16: 105 us, 127
 // with 8). Backward: 16 need 208 registers and spill in rows of 1024 threads (4096 rows
-// of 8192: 110 us, 371 with 16; 175 us for 16384 rows of 4096 either way).
+// of 8192, both by 512 workgroups: 110 us, 371 with 16; 175 us for 16384 rows of 4096
+// either way).
 constexpr int kForwardElements = 16, kBackwardElements = 8;
 // Workgroups that a call is spread over. Backward: each leaves its sums, which are read
 // once more (the same rows of 4096: 175 us with 512, 196 with 1024, 200 with 256).
 constexpr int64_t kForwardWgs = 4096, kBackwardWgs = 512;
+// Of 1024 threads a CU holds one (2 x 1024 rows of 16384: 115 us with 256, 132 with 512).
+constexpr int64_t kBackwardWideWgs = 256;
+// A workgroup's sums are twice a row of bf16 for each gradient: where examples have few
+// rows, each takes at least two batches while this many workgroups are left (8 x 64 rows of
+// 4096: 17.5 us, one batch 20.9, four 18.6; 3 x 128 of 13502: 74 us, four batches 90).
+constexpr int64_t kBackwardFewWgs = 128;
 
 RnPlan plan_forward(const dpsgd_residual_norm& n) {
   RnPlan p = plan_rows(n, kForwardElements);
@@ -463,8 +470,11 @@ RnPlan plan_backward(const dpsgd_residual_norm& n) {
     p.groups /= 2;
   }
   const int64_t batches = ceil_div(n.S, p.groups);
-  const int64_t most = n.B >= kBackwardWgs ? 1 : ceil_div(kBackwardWgs, n.B);
-  p.iters = (int)ceil_div(batches, most < batches ? most : batches);
+  const int64_t most = ceil_div(p.threads > 512 ? kBackwardWideWgs : kBackwardWgs, n.B);
+  const int64_t few = ceil_div(kBackwardFewWgs, n.B), pairs = ceil_div(batches, 2);
+  const int64_t enough = pairs > few ? pairs : few;
+  const int64_t chunks = most < enough ? most : enough;
+  p.iters = (int)ceil_div(batches, chunks < batches ? chunks : batches);
   p.chunks = ceil_div(batches, p.iters);
   p.wgs = n.B * p.chunks;
   return p;

@@ -197,7 +197,8 @@ def test_rows_are_covered_once(bf16):
                 threads, groups = threads // 2, groups // 2
             assert threads >> log == groups and threads % 64 == 0
             batches = ceil_div(S, groups)
-            most = 1 if B >= 512 else ceil_div(512, B)
+            most = min(ceil_div(256 if threads > 512 else 512, B),
+                       max(ceil_div(batches, 2), ceil_div(128, B)))
             iters = ceil_div(batches, min(most, batches))
             chunks = ceil_div(batches, iters)
             s = (np.arange(chunks)[:, None, None] * iters + np.arange(iters)[:, None]) * groups + np.arange(groups)
