@@ -59,6 +59,13 @@ struct RnArgs {
   int32_t shift;
 };
 
+// Elements of a thread. Forward: the work of a row that is the same for all of its
+// threads is spread over more of them with 16 (16384 rows of 4096 in bf16: 105 us, 127
+// with 8). Backward: 16 need 208 registers and spill in rows of 1024 threads (4096 rows
+// of 8192, both by 512 workgroups: 110 us, 371 with 16; 175 us for 16384 rows of 4096
+// either way).
+constexpr int kForwardElements = 16, kBackwardElements = 8;
+
 // Sums of K values over the threads of each row, in all of them. For rows of more
 // than a wave every thread of the workgroup has to call it; `slot` goes between 0
 // and 1 from call to call, so that one barrier a call is enough.
@@ -257,6 +264,12 @@ enum BackKind : int { BARE = 0, GATED = 1, POST = 2 };
 // side has two sums, sum dR v (v: the normed block, or the block) and sum dR: gate and
 // post_gamma are constant over an example, so dgate, dpost_gamma and dpost_beta are
 // these times constants.
+// Rows of more than 8 elements a thread (8193 to 16384 channels, 1024 threads, 128 registers
+// each) are LEAN: gamma, gate and post_gamma are read again for each row (from L2), dr and the
+// block when it is their turn, and the sums of dy rh and dy are in LDS, where a thread has its
+// own places. In registers they spill 36 to 257 of them: 2 x 1024 rows of 16384 in bf16 85 us
+// (116 with spills; with only the parameters read again 90), normed on both sides 127 (311;
+// 269), 3 x 128 of 13502 with a gate 38 (74; 78). Odd widths still spill.
 template <class T, int V, int NV, int MOST, int KIND, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   extern __shared__ __align__(16) float rn_lds[];   // [groups][C], where there are several groups
@@ -268,16 +281,30 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   const int32_t chunk = (int32_t)(blockIdx.x - (uint32_t)example * (uint32_t)a.chunks);
   const float* gate = a.gate ? a.gate + (a.gate_per_example ? example * a.C : 0) : nullptr;
   int slot = 0;
+  constexpr bool LEAN = MOST == kMostThreads && NV * V > kBackwardElements;
+  static_assert(!LEAN || NV * V == 16, "places of the sums");
+  __shared__ float sums[LEAN ? 2 : 1][LEAN ? 16 * kMostThreads : 1];   // dy rh, dy
+  const auto place = [&](int j, int c) { return (j * V + c) * kMostThreads + (int)threadIdx.x; };
   float ga[NV][V], gp[NV][V];   // gamma; gate post_gamma
-  load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
-  load_affine<V, NV>(gate, 1.0f, ch, gp);
-  if constexpr (KIND == POST) {
-    float pg[NV][V];
-    load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
+  const auto load_gp = [&] {
+    load_affine<V, NV>(gate, 1.0f, ch, gp);
+    if constexpr (KIND == POST) {
+      float pg[NV][V];
+      load_affine<V, NV>(a.post_gamma, 1.0f, ch, pg);
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+#pragma unroll
+        for (int c = 0; c < V; ++c) gp[j][c] *= pg[j][c];
+    }
+  };
+  if constexpr (LEAN) {
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int c = 0; c < V; ++c) gp[j][c] *= pg[j][c];
+      for (int c = 0; c < V; ++c) sums[0][place(j, c)] = sums[1][place(j, c)] = 0.0f;
+  } else {
+    load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
+    load_gp();
   }
   constexpr int kSums = KIND == POST ? 4 : (KIND == GATED ? 3 : 2);
   float acc[kSums][NV][V] = {};   // dy rh, dy, dR v, dR
@@ -288,21 +315,29 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
     Raw<T, V> rr[NV], rb[NV], rdy[NV], rdr[NV];
     load_row<T, V, NV>(static_cast<const T*>(a.x) + at, ch, active, rr);
     load_row<T, V, NV>(static_cast<const T*>(a.dy) + at, ch, active, rdy);
-    load_row<T, V, NV>(static_cast<const T*>(a.dr) + at, ch, active && a.dr, rdr);
-    if constexpr (KIND != BARE) load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active, rb);
+    const auto load_dr = [&] {
+      load_row<T, V, NV>(static_cast<const T*>(a.dr) + at, ch, active && a.dr, rdr);
+    };
+    const auto load_block = [&] {
+      if constexpr (KIND != BARE) load_row<T, V, NV>(static_cast<const T*>(a.block) + at, ch, active, rb);
+    };
+    if constexpr (!LEAN) load_dr(), load_block();
     float4 st = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     if (active) st = reinterpret_cast<const float4*>(a.stats)[row];
     float d[NV][V], vh[NV][V];
     widen_row<T, V, NV>(rdy, d);
     widen_row<T, V, NV>(rr, vh);
     float m[2] = {0.0f, 0.0f};
+    if constexpr (LEAN) load_affine<V, NV>(a.gamma, 1.0f, ch, ga);
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
       for (int c = 0; c < V; ++c) {
         vh[j][c] = ch.has(j) ? (vh[j][c] - st.x) * st.y : 0.0f;
-        acc[0][j][c] = fmaf(d[j][c], vh[j][c], acc[0][j][c]);
-        acc[1][j][c] += d[j][c];
+        float& dg = LEAN ? sums[0][LEAN ? place(j, c) : 0] : acc[0][j][c];
+        float& db = LEAN ? sums[1][LEAN ? place(j, c) : 0] : acc[1][j][c];
+        dg = fmaf(d[j][c], vh[j][c], dg);
+        db += d[j][c];
         d[j][c] *= ga[j][c];
         m[0] += d[j][c];
         m[1] = fmaf(d[j][c], vh[j][c], m[1]);
@@ -310,6 +345,7 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
     row_sum<2>(m, a.log, lds, slot);
     m[0] = a.layer ? m[0] * a.inv_C : 0.0f;
     m[1] *= a.inv_C;
+    if constexpr (LEAN) load_dr();
     float dr[NV][V];
     widen_row<T, V, NV>(rdr, dr);
 #pragma unroll
@@ -323,6 +359,7 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
     }
     if (active && a.r) store_row<T, V, NV>(static_cast<T*>(a.r) + at, ch, d);
     if (!a.y) continue;
+    if constexpr (LEAN) load_gp(), load_block();
     if constexpr (KIND != BARE) widen_row<T, V, NV>(rb, vh);
     m[0] = m[1] = 0.0f;
 #pragma unroll
@@ -376,6 +413,8 @@ __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
                                     : f[j][c] * acc[k == 3 ? 2 : 3][j][c]);
         else
           v[j][c] = acc[k < kSums ? k : 0][j][c];
+        if constexpr (LEAN)
+          if (k < 2) v[j][c] = sums[k][place(j, c)];
       }
     }
     if (groups == 1) {
@@ -439,20 +478,15 @@ RnPlan plan_rows(const dpsgd_residual_norm& n, int elements) {
   return p;
 }
 
-// Elements of a thread. Forward: the work of a row that is the same for all of its
-// threads is spread over more of them with 16 (16384 rows of 4096 in bf16: 105 us, 127
-// with 8). Backward: 16 need 208 registers and spill in rows of 1024 threads (4096 rows
-// of 8192, both by 512 workgroups: 110 us, 371 with 16; 175 us for 16384 rows of 4096
-// either way).
-constexpr int kForwardElements = 16, kBackwardElements = 8;
 // Workgroups that a call is spread over. Backward: each leaves its sums, which are read
 // once more (the same rows of 4096: 175 us with 512, 196 with 1024, 200 with 256).
 constexpr int64_t kForwardWgs = 4096, kBackwardWgs = 512;
-// Of 1024 threads a CU holds one (2 x 1024 rows of 16384: 115 us with 256, 132 with 512).
+// Of 1024 threads a CU holds one (2 x 1024 rows of 16384, before their sums were in LDS:
+// 115 us with 256, 132 with 512).
 constexpr int64_t kBackwardWideWgs = 256;
 // A workgroup's sums are twice a row of bf16 for each gradient: where examples have few
 // rows, each takes at least two batches while this many workgroups are left (8 x 64 rows of
-// 4096: 17.5 us, one batch 20.9, four 18.6; 3 x 128 of 13502: 74 us, four batches 90).
+// 4096: 17.5 us, one batch 20.9, four 18.6; 3 x 128 of 13502, likewise: 74 us, four batches 90).
 constexpr int64_t kBackwardFewWgs = 128;
 
 RnPlan plan_forward(const dpsgd_residual_norm& n) {

@@ -228,6 +228,28 @@ def test_every_combination(dp, kind, post, gate, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("form", ["bare", "gated", "post"])
+@pytest.mark.parametrize("C", [8200, 12292, 16382, 16383, 16384])
+def test_widest_rows(dp, C, form, dtype):
+    """Rows of 1024 threads whose sums are in LDS: every vector width; three workgroups an
+    example with two rows each, the last with one."""
+    B, S = 40, 5
+    post, gate, kind = form == "post", {"bare": 0, "gated": 2, "post": 1}[form], ("layer", "rms")[C % 4 == 0]
+    c, p = _case(B, S, C, dtype, C, gate, post)
+    desc = _desc(dp, c, p, kind, post)
+    got = _forward(dp, c, desc)
+    check_forward(c, p, kind, post, got, dtype)
+    names = [n for n in AFFINE if (post or not n.startswith("post")) and (gate or n != "gate")]
+    for in_place in (False, True):
+        out = _backward(dp, c, desc, got[0], got[2], names, in_place=in_place)
+        check_backward(c, p, kind, post, got[0], out, dtype)
+    if form == "bare":
+        got = _forward(dp, c, desc, block=False)
+        out = _backward(dp, c, desc, got[0], got[2], ["gamma", "beta"], block=False, with_dr=False)
+        check_backward(c, p, kind, post, got[0], out, dtype, block=False, with_dr=False)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("B,S,C", [(2, 9, 40), (4, 33, 768), (1, 2, 5000)])
 def test_without_a_block(dp, B, S, C, dtype):
     """The first norm of a model: r is x (scaled), nothing is added."""
