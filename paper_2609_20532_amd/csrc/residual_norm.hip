@@ -269,7 +269,8 @@ enum BackKind : int { BARE = 0, GATED = 1, POST = 2 };
 // block when it is their turn, and the sums of dy rh and dy are in LDS, where a thread has its
 // own places. In registers they spill 36 to 257 of them: 2 x 1024 rows of 16384 in bf16 85 us
 // (116 with spills; with only the parameters read again 90), normed on both sides 127 (311;
-// 269), 3 x 128 of 13502 with a gate 38 (74; 78). Odd widths still spill.
+// 269), 3 x 128 of 13502 with a gate 38 (74; 78). What still
+// spills: odd widths (53 to 185 registers) and a norm of the block (6 to 99).
 template <class T, int V, int NV, int MOST, int KIND, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   extern __shared__ __align__(16) float rn_lds[];   // [groups][C], where there are several groups

@@ -167,6 +167,8 @@ def test_channels_of_a_row_are_covered_once(bf16, elements):
         V, nv, log, threads, groups = plan_rows(C, bf16, elements)
         assert threads <= 1024 and groups >= 1 and nv * V <= 16 and nv in (1, 2, 4, 8, 16)
         assert nv <= {8: 2, 4: 4, 2: 8, 1: 16}[V]          # kernels that there are
+        if nv * V > elements:
+            assert nv * V == 16 and threads == 1024         # sums in LDS: 16 places a thread
         if log < 6:
             assert nv == 1                                  # rows of less than a wave
         seen = np.zeros(C, int)
