@@ -1,11 +1,14 @@
 // Checks and addresses of tensors for the Python binding, read from the tensors
 // themselves: a call on small tensors is bound by these (0.7 us for a tensor that is
 // checked from Python, a tenth of it here). Where a check fails, the binding finds out
-// which one, and says so.
+// which one, and says so. What a tensor throws (one without storage, inside a function
+// transform, has no address) becomes the Python exception that its own method raises.
 #include <Python.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <exception>
 
 #include "dpsgd.h"
 
@@ -13,6 +16,26 @@ namespace {
 
 bool plain(const at::Tensor& v, long device) {
   return v.is_cuda() && v.get_device() == device && v.layout() == at::kStrided;
+}
+
+// The address of v, null for a tensor of no entries.
+void* address_of(const at::Tensor& v) {
+  void* p = v.data_ptr();
+  TORCH_CHECK(p || v.numel() == 0, "the tensor has no memory");
+  return p;
+}
+
+// f(); a C++ exception, which may not pass through the interpreter's frames, is set as
+// the Python error that it stands for. Whether there was none.
+template <class F>
+bool guarded(F f) {
+  try {
+    f();
+    return true;
+  } catch (...) {
+    torch::translate_exception_to_python(std::current_exception());
+    return false;
+  }
 }
 
 // addresses(tensors, layers, per_block, element, device, to): whether every tensor of
@@ -34,21 +57,24 @@ PyObject* addresses(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     if (PyObject_GetBuffer(args[5], &to, PyBUF_WRITABLE) == 0) {
       const Py_ssize_t n = PySequence_Fast_GET_SIZE(tensors);
       bool good = n * (Py_ssize_t)sizeof(dpsgd_layer) == layers.len && n * 8 <= to.len;
-      for (Py_ssize_t k = 0; good && k < n; ++k) {
-        PyObject* t = PySequence_Fast_GET_ITEM(tensors, k);
-        good = THPVariable_Check(t);
-        if (!good) break;
-        const dpsgd_layer& L = static_cast<const dpsgd_layer*>(layers.buf)[k];
-        // Sizes that the library refuses are not multiplied here.
-        const bool small = L.d_in >= 1 && L.d_out >= 1 && L.d_in < (INT64_C(1) << 31) && L.d_out < (INT64_C(1) << 31);
-        const int64_t entries = small ? L.d_in * L.d_out : -1;
-        const at::Tensor& v = THPVariable_Unpack(t);
-        good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous() &&
-               v.numel() == (per_block ? 2 * ((entries + DPSGD_STATE_BLOCK - 1) / DPSGD_STATE_BLOCK) : entries);
-        if (good) static_cast<uint64_t*>(to.buf)[k] = reinterpret_cast<uint64_t>(v.data_ptr());
-      }
+      const auto each = [&] {
+        for (Py_ssize_t k = 0; good && k < n; ++k) {
+          PyObject* t = PySequence_Fast_GET_ITEM(tensors, k);
+          good = THPVariable_Check(t);
+          if (!good) break;
+          const dpsgd_layer& L = static_cast<const dpsgd_layer*>(layers.buf)[k];
+          // Sizes that the library refuses are not multiplied here.
+          const bool small = L.d_in >= 1 && L.d_out >= 1 && L.d_in < (INT64_C(1) << 31) && L.d_out < (INT64_C(1) << 31);
+          const int64_t entries = small ? L.d_in * L.d_out : -1;
+          const at::Tensor& v = THPVariable_Unpack(t);
+          good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous() &&
+                 v.numel() == (per_block ? 2 * ((entries + DPSGD_STATE_BLOCK - 1) / DPSGD_STATE_BLOCK) : entries);
+          if (good) static_cast<uint64_t*>(to.buf)[k] = reinterpret_cast<uint64_t>(address_of(v));
+        }
+      };
+      const bool whole = guarded(each);
       PyBuffer_Release(&to);
-      answer = PyBool_FromLong(good);
+      if (whole) answer = PyBool_FromLong(good);
     }
     PyBuffer_Release(&layers);
   }
@@ -96,13 +122,14 @@ PyObject* take(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     } else {
       const long element = PyLong_AsLong(args[3 + 3 * k]);
       int good = !PyErr_Occurred() && THPVariable_Check(t);
+      address = nullptr;
       if (good) {
-        const at::Tensor& v = THPVariable_Unpack(t);
-        good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous();
-        if (good) good = fits(v, args[2 + 3 * k]);
-        address = good == 1 ? PyLong_FromVoidPtr(v.data_ptr()) : nullptr;
-      } else {
-        address = nullptr;
+        guarded([&] {
+          const at::Tensor& v = THPVariable_Unpack(t);
+          good = plain(v, device) && static_cast<long>(v.scalar_type()) == element && v.is_contiguous();
+          if (good) good = fits(v, args[2 + 3 * k]);
+          if (good == 1) address = PyLong_FromVoidPtr(address_of(v));
+        });
       }
       if (!address) {
         Py_DECREF(got);
@@ -126,14 +153,24 @@ PyObject* logits(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   const long device = PyLong_AsLong(args[0]);
   if (device == -1 && PyErr_Occurred()) return nullptr;
   if (!THPVariable_Check(args[1])) Py_RETURN_NONE;
-  const at::Tensor& v = THPVariable_Unpack(args[1]);
-  if (!plain(v, device) || v.dim() != 3 || v.numel() == 0) Py_RETURN_NONE;
-  const int64_t B = v.size(0), T = v.size(1), V = v.size(2);
-  const int64_t stride = T > 1 ? v.stride(1) : (B > 1 ? v.stride(0) : V);
-  if ((V > 1 && v.stride(2) != 1) || stride < V || (B > 1 && T > 1 && v.stride(0) != T * v.stride(1)))
-    Py_RETURN_NONE;
-  return Py_BuildValue("NLLLLi", PyLong_FromVoidPtr(v.data_ptr()), (long long)B, (long long)T,
-                       (long long)V, (long long)stride, static_cast<int>(v.scalar_type()));
+  PyObject* answer = nullptr;
+  guarded([&] {
+    const at::Tensor& v = THPVariable_Unpack(args[1]);
+    bool good = plain(v, device) && v.dim() == 3 && v.numel() != 0;
+    if (good) {
+      const int64_t B = v.size(0), T = v.size(1), V = v.size(2);
+      const int64_t stride = T > 1 ? v.stride(1) : (B > 1 ? v.stride(0) : V);
+      good = (V == 1 || v.stride(2) == 1) && stride >= V && (B == 1 || T == 1 || v.stride(0) == T * v.stride(1));
+      if (good)
+        answer = Py_BuildValue("NLLLLi", PyLong_FromVoidPtr(address_of(v)), (long long)B, (long long)T,
+                               (long long)V, (long long)stride, static_cast<int>(v.scalar_type()));
+    }
+    if (!good) {
+      Py_INCREF(Py_None);
+      answer = Py_None;
+    }
+  });
+  return answer;
 }
 
 PyMethodDef methods[] = {
