@@ -515,7 +515,9 @@ int dpsgd_token_logprobs(const dpsgd_logits* desc, const void* logits, float* lo
  *   dlogits_v = scale (p_v (grad_lse - grad_logprobs - grad_entropy (ln p_v + entropy))
  *                      + grad_logprobs [v = target])
  * lse and entropy are dpsgd_token_logprobs' (entropy is read only with
- * grad_entropy). A row whose three factors are 0 gets zeros, whatever its
+ * grad_entropy). p_v is exp(z_v - lse) where lse is within 32 of 0 (1024 in bf16),
+ * so that its rounding is lost in dtype's; beyond, m and S are formed again from
+ * the logits. A row whose three factors are 0 gets zeros, whatever its
  * logits. Row r of dlogits begins at entry r * dlogits_stride (V .. 2^31).
  * dlogits may be logits (with the same stride), and overlaps nothing else. */
 int dpsgd_token_logprobs_backward(const dpsgd_logits* desc, const void* logits, const float* lse,

@@ -884,20 +884,60 @@ __global__ __launch_bounds__(kThreads) void token_part_loss_kernel(TokenArgs a, 
   }
 }
 
+// A row's upstream gradients, and its entropy (with ge).
+struct Upstream {
+  float gp, q, ge, H;   // q: g_lse - g_logp
+};
+
+// scale (p_v (q - ge (ln p_v + H)) + gp [v = target]) of entries in registers; p and ln p
+// from the sums of their row.
+template <class T, int NT, int NVEC>
+__device__ __forceinline__ void write_backward(const Held<T, NT, NVEC>& held, const T* x, T* g, int32_t tid,
+                                               int32_t target, float scale, const Upstream& u,
+                                               const RowStats& st) {
+  const Exponents ex(scale, st.top);
+  const float f = __builtin_amdgcn_exp2f(-ex.off) / st.S;
+  write_entries(held, x, g, tid, target, scale * u.gp, [&](float v) {
+    const float t = ex.near ? ex.template at<true>(v) : ex.template at<false>(v);
+    const float p = f * __builtin_amdgcn_exp2f(t);
+    if (u.ge == 0.0f) return scale * (p * u.q);
+    const float l = fmaxf((t - ex.off) * kLn2, -256.0f) - st.log_S;   // 0 for -inf; a NaN is in p
+    return scale * (p * (u.q - u.ge * (l + u.H)));
+  });
+}
+
+// Rows whose p is formed from lse as it is stored: its rounding, half a step of lse, is then
+// at most 2^-20 of p (2^-15, a 64th of the gradient's own rounding, in bf16), and the same for
+// all p of the row. Beyond, where it would grow with the logits' common offset (0.5% of p at
+// 10^6), the row's sums are formed again, relative to its largest entry.
+template <class T>
+constexpr float kNearLse = sizeof(T) == 2 ? 1024.0f : 32.0f;
+
+// The part whose workgroup has all of a row, spread by a multiplicative hash: workgroups go to
+// the XCDs and their CUs in turn, and with the same part of every row few of them have work
+// (512 rows of 262144 in bf16 1930 us with part 0, 254 spread).
+__device__ __forceinline__ int32_t owner_of(int64_t row, int32_t parts) {
+  return (int32_t)(((uint32_t)row * 0x9E3779B1u >> 16) % (uint32_t)parts);
+}
+
 // dx_v = scale (p_v (g_lse - g_logp - g_H (ln p_v + H)) + g_logp [v = target]): rows, or
-// parts of them, one after the other.
+// parts of them, one after the other. A row in parts with its lse far from 0 is one
+// workgroup's, which reads it twice (8192 rows of 50257 in bf16: 290 us, 419 far from 0; every
+// row held in registers as in the loss: 306 and 313).
 template <class T, int NT>
 __global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, int32_t parts) {
   constexpr int kTeams = kThreads / NT;
+  __shared__ float red[2][NT / 64][2];
   const int32_t tid = NT == 64 ? (int32_t)(threadIdx.x & 63) : (int32_t)threadIdx.x;
   const int32_t team_at = NT == 64 ? __builtin_amdgcn_readfirstlane((int32_t)(threadIdx.x >> 6)) : 0;
+  Team<NT> team{red, 0};
   using H = Held<T, NT, kPartVecs>;
   for (int64_t at = (int64_t)blockIdx.x * kTeams + team_at; at < a.rows * parts; at += (int64_t)gridDim.x * kTeams) {
     const int64_t row = at / parts;
-    const int32_t first = (int32_t)(at - row * parts) * H::kMost;
+    const int32_t part = (int32_t)(at - row * parts), first = part * H::kMost;
     const int32_t n = a.V - first < H::kMost ? a.V - first : H::kMost;
-    const T* x = static_cast<const T*>(a.logits) + row * a.stride + first;
-    T* g = static_cast<T*>(a.dlogits) + row * a.grad_stride + first;
+    const T* x_row = static_cast<const T*>(a.logits) + row * a.stride;
+    T* g_row = static_cast<T*>(a.dlogits) + row * a.grad_stride;
     bool empty;
     const int32_t target = target_of(a, row, &empty);
     const float gp = empty || !a.g_logp ? 0.0f : a.g_logp[row];
@@ -906,18 +946,39 @@ __global__ __launch_bounds__(kThreads) void token_backward_kernel(TokenArgs a, i
     const bool zero = gp == 0.0f && gl == 0.0f && ge == 0.0f;
     const float lse = zero ? 0.0f : a.lse[row], H_row = ge != 0.0f ? a.entropy[row] : 0.0f;
     if (zero || lse == -INFINITY) {
-      write_zeros(g, n, tid, NT);
+      write_zeros(g_row + first, n, tid, NT);
       continue;
     }
-    H held;
-    held.load(x, n, tid);
     const float q = gl - gp;
+    H held;
+    if (fabsf(lse) > kNearLse<T>) {   // not a NaN
+      const Upstream up{gp, q, ge, H_row};
+      float top, S, E, mine;
+      if (NT == 64 || parts == 1) {
+        held.load(x_row, n, tid);
+        reduce_row(team, held, a.scale, false, top, S, E, mine);
+        write_backward(held, x_row, g_row, tid, target, a.scale, up, RowStats(a.scale, top, S, E));
+      } else if (part == owner_of(row, parts)) {
+        Running<T, NT> run;
+        run.template row<false>(x_row, a.V, tid, a.scale * kLog2e);
+        if (!run.join(team, a.scale * kLog2e)) far_sums(team, x_row, a.V, tid, a.scale, run.top, run.S, run.E);
+        const RowStats st(a.scale, run.top, run.S, run.E);
+        for (int32_t v = 0; v < a.V; v += H::kMost) {
+          held.load(x_row + v, a.V - v < H::kMost ? a.V - v : H::kMost, tid);
+          write_backward(held, x_row + v, g_row + v, tid, target - v, a.scale, up, st);
+        }
+      }
+      continue;
+    }
+    const T* x = x_row + first;
+    T* g = g_row + first;
+    held.load(x, n, tid);
     if (ge == 0.0f) {
       write_entries(held, x, g, tid, target - first, a.scale * gp,
-                    [&](float v) { return a.scale * (exp_of(a.scale * v - lse) * q); });
+                    [&](float v) { return a.scale * (exp_of(fmaf(a.scale, v, -lse)) * q); });
     } else {
       write_entries(held, x, g, tid, target - first, a.scale * gp, [&](float v) {
-        const float l = a.scale * v - lse, p = exp_of(l);
+        const float l = fmaf(a.scale, v, -lse), p = exp_of(l);
         return a.scale * (p * (q - ge * (fmaxf(l, -256.0f) + H_row)));   // 0 for -inf; a NaN is in p
       });
     }
