@@ -761,13 +761,14 @@ __device__ __forceinline__ RowStats join_parts(const TokenArgs& a, const Parts& 
   float top = -INFINITY;
   for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) top = fmaxf(top, sums[p].x);
   top = team.max(top);
-  float m = a.scale * top;
-  if (m == -INFINITY) m = 0.0f;
+  // Exponents as within a part: from rounded products the parts' shares would be off by the
+  // products' rounding, and p would not sum to 1.
+  const Exponents ex(a.scale, top);
   float S = 0.0f, E = 0.0f;
   for (int32_t p = threadIdx.x; p < parts.n; p += kThreads) {
     const float4 q = sums[p];
     if (q.y != 0.0f) {   // 0: all of the part is -inf; NaN counts
-      const float t = (a.scale * q.x - m) * kLog2e, w = __builtin_amdgcn_exp2f(t);
+      const float t = (ex.near ? ex.at<true>(q.x) : ex.at<false>(q.x)) - ex.off, w = __builtin_amdgcn_exp2f(t);
       S = fmaf(w, q.y, S);
       E += w * fmaf(q.y, fmaxf(t, -256.0f), q.z);
     }

@@ -1,6 +1,6 @@
 """The gradient of the token log probabilities where all logits of a row have a common
 offset, which the distribution does not depend on, against the float64 definition and by its
-sum over a row.
+sum over a row; and the loss's and the entropy of such rows.
 
 Bound, with u = 2^-24, d = m - z >= 0 an entry's distance from the row's largest, range the
 largest d of a row, n its length. d is off by 3 u d (the scale times log2 e is two roundings,
@@ -147,3 +147,36 @@ def test_gradient_sums_to_zero(dp, B, T, V, offset):
         p, _, _, K, _ = _row(x64[i], s, "f32")
         tol = s * U * (p * (K + 8) + 4 * (np.arange(V) == t[i]))
         assert abs(got[i].sum()) <= tol.sum() + 1e-38 * V, (i, got[i].sum(), tol.sum())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", OFFSETS)
+@pytest.mark.parametrize("B,T,V", SHAPES + [(1, 3, 300007)])
+def test_loss_and_entropy_of_rows_with_an_offset(dp, B, T, V, offset, dtype):
+    """Rows in parts among them: their join adds (3 D + 3) u to a part's share, D the distance
+    of its largest entry from the row's, so no more than 3 d u of any entry in it: on average
+    over p (3 ln n + 3) u, and 16 u of summing."""
+    import torch
+    s = 1.0 if abs(offset) > 1e5 else 0.75
+    x, x64, targets, _ = _case(B, T, V, dtype, offset, V + 1, masked=False)
+    N, t = B * T, targets.reshape(-1)
+    desc = dp.make_logits(x, torch.from_numpy(targets).cuda(), s)
+    ws = torch.empty(dp.dpsgd_token_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    dl, entropy = torch.full_like(x, 7.0), torch.empty(B, T, device="cuda")
+    dp.dpsgd_token_loss(desc, x, dl, workspace=ws)
+    dp.dpsgd_token_logprobs(desc, x, entropy=entropy, workspace=ws)
+    got, H_got = _wide(dl).reshape(N, V), _wide(entropy).reshape(N)
+    ref = lo.token_gradient(x64, t, s, -np.ones(N))
+    for i in range(N):
+        if t[i] < 0:
+            assert not got[i].any() and H_got[i] == 0.0
+            continue
+        p, _, H, K, E = _row(x64[i], s, dtype)
+        more = 3 * math.log(V) + 20
+        tol = s * U * (p * (K + more + 8) + 4 * (np.arange(V) == t[i]))
+        if dtype == "f32":
+            assert abs(got[i].sum()) <= tol.sum() + 1e-38 * V, (i, got[i].sum(), tol.sum())
+        else:
+            tol = tol + BF16 * (np.abs(ref[i]) + tol)
+        assert (np.abs(got[i] - ref[i]) <= tol + 1e-38).all(), i
+        assert abs(H_got[i] - H) <= (E + more * (2 + 2 * H)) * U, (i, H_got[i], H)
