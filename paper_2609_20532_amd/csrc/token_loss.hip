@@ -496,18 +496,27 @@ __device__ __forceinline__ int32_t put_in_order(const uint64_t* keys, int32_t n,
   return n < k ? n : k;
 }
 
-// The upper 16 bits of the k-th largest of 256 group maxima, by one wave, from the
-// highest bit down.
+// A bound on the k-th largest of 256 group maxima, by one wave: its upper 16 bits, from the
+// highest down, which is all of a bf16 logit. Of float32 ones, whose 7 bits of fraction may be
+// too coarse for the row (all logits at 1000 and more, say), the lower bits as well where more
+// than twice the groups that are needed reach the bound: with 16 bits the list of candidates
+// overflows there (2048 rows of 32003, k = 64: 66 us centred on 0; at 3000 68, with 16 bits
+// 5770).
+template <class T>
 __device__ __forceinline__ void bound_of_groups(const uint32_t* group, int32_t k, int32_t lane, uint32_t* to) {
   const uint4 g = reinterpret_cast<const uint4*>(group)[lane];
   uint32_t least = 0;
-#pragma unroll
-  for (int bit = 31; bit >= 16; --bit) {
+  int32_t reach = 256;   // groups from `least` on
+  const auto take = [&](int bit) {
     const uint32_t t = least | 1u << bit;
     const int n = __popcll(__ballot(g.x >= t)) + __popcll(__ballot(g.y >= t)) +
                   __popcll(__ballot(g.z >= t)) + __popcll(__ballot(g.w >= t));
-    if (n >= k) least = t;
-  }
+    if (n >= k) least = t, reach = n;
+  };
+#pragma unroll
+  for (int bit = 31; bit >= 16; --bit) take(bit);
+  if (sizeof(T) == 4 && reach > 2 * k)
+    for (int bit = 15; bit >= 0; --bit) take(bit);
   if (lane == 0) *to = least;
 }
 
@@ -515,8 +524,8 @@ __device__ __forceinline__ void bound_of_groups(const uint32_t* group, int32_t k
 // The entries are in 256 groups (a vector's places of one lane, the places of one, two
 // or four neighbouring lanes); at least k of the groups' largest ones are not below the
 // k-th largest of them, so entries below it are none of the k. Of V unordered entries
-// about 256 ln(256 / (256 - k)) are left, 21 for k = 20 and 74 for k = 64: they are
-// listed and put in order. `first` is added to the entries' places. Where the list is too
+// about 256 ln(256 / (256 - k)) are left, 21 for k = 20 and 74 for k = 64 (41 and 178 where
+// twice as many groups reach the bound): they are listed and put in order. `first` is added to the entries' places. Where the list is too
 // short (many equal or sorted logits) the n_row entries at x are searched once for each
 // alternative.
 template <int NT, class T, class H, class P>
@@ -541,7 +550,7 @@ __device__ __forceinline__ int32_t top_entries(Team<NT>& team, const H& held, co
   }
   if (tid == 0) lds.count = 0;
   team.barrier();
-  if (tid < 64) bound_of_groups(lds.group, k, tid, &lds.least);
+  if (tid < 64) bound_of_groups<T>(lds.group, k, tid, &lds.least);
   team.barrier();
   // Entries of -inf are none.
   const uint32_t none = order_bits(-INFINITY);
@@ -827,7 +836,7 @@ __global__ __launch_bounds__(kThreads) void token_join_kernel(TokenArgs a, Parts
       lists.group[tid] = g;
       if (tid == 0) lists.count = 0;
       __syncthreads();
-      if (tid < 64) bound_of_groups(lists.group, a.k, tid, &lists.least);
+      if (tid < 64) bound_of_groups<T>(lists.group, a.k, tid, &lists.least);
       __syncthreads();
       const uint64_t least = lists.least ? (uint64_t)lists.least << 32 : 1;
       for (int64_t i = tid; i < all; i += kThreads) {

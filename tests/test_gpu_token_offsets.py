@@ -180,3 +180,19 @@ def test_loss_and_entropy_of_rows_with_an_offset(dp, B, T, V, offset, dtype):
             tol = tol + BF16 * (np.abs(ref[i]) + tol)
         assert (np.abs(got[i] - ref[i]) <= tol + 1e-38).all(), i
         assert abs(H_got[i] - H) <= (E + more * (2 + 2 * H)) * U, (i, H_got[i], H)
+
+
+@pytest.mark.parametrize("offset", [-40.0, 1000.0, 3000.0, -2.0e5])
+@pytest.mark.parametrize("B,T,V,k", [(2, 3, 1000, 64), (2, 2, 5003, 20), (70, 1, 20011, 64), (2, 1, 40000, 5),
+                                     (1, 2, 70001, 64), (2, 1, 300007, 20), (3, 1, 700, 1)])
+def test_alternatives_of_rows_with_an_offset(dp, B, T, V, k, offset):
+    """float32 logits whose upper bits are alike, ties among them: the tokens are the exact
+    ones, in order."""
+    import torch
+    x, x64, _, _ = _case(B, T, V, "f32", offset, V + k)
+    desc = dp.make_logits(x)
+    ids = torch.full((B, T, k), 7, dtype=torch.int64, device="cuda")
+    ws = torch.empty(dp.dpsgd_token_workspace_bytes(desc, k), dtype=torch.uint8, device="cuda")
+    dp.dpsgd_token_logprobs(desc, x, top_ids=ids, workspace=ws)
+    want = [lo.alternatives(row, 1.0, k)[0] for row in x64]
+    assert np.array_equal(ids.cpu().numpy().reshape(B * T, k), np.stack(want))
