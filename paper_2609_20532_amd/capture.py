@@ -136,8 +136,7 @@ class Block(nn.Module):
 
 
 class _ResidualNorm(torch.autograd.Function):
-    """r = x + block and y = layer norm of r, with frozen parameters; without a block y
-    alone, the norm of x."""
+    """r = x + block and y = layer norm of r; without a block y alone, the norm of x."""
 
     @staticmethod
     def forward(ctx, x, block, gamma, beta, eps):
@@ -165,10 +164,15 @@ class _ResidualNorm(torch.autograd.Function):
         dblock = torch.empty_like(r) if ctx.has_block else None
         ws = torch.empty(dpsgd.dpsgd_residual_norm_workspace_bytes(ctx.desc), dtype=torch.uint8,
                          device=r.device)
+        # Per example: their sum over the batch is the parameter's gradient.
+        dgamma, dbeta = (r.new_empty(ctx.desc.B, ctx.desc.C) if ctx.needs_input_grad[k] else None
+                         for k in (2, 3))
         # Without a norm or a gate of it the block's values are not read: r stands for them.
         dpsgd.dpsgd_residual_norm_backward(ctx.desc, r if ctx.has_block else None, r, dy, dr, stats,
-                                           dx=dx, dblock=dblock, workspace=ws)
-        return dx, dblock, None, None, None
+                                           dx=dx, dblock=dblock, dgamma=dgamma, dbeta=dbeta,
+                                           workspace=ws)
+        return (dx, dblock, None if dgamma is None else dgamma.sum(0),
+                None if dbeta is None else dbeta.sum(0), None)
 
 
 class GPT2LoRA(nn.Module):
