@@ -148,27 +148,29 @@ class _ResidualNorm(torch.autograd.Function):
         y = torch.empty_like(x)
         stats = torch.empty(desc.B, desc.S, 4, device=x.device)
         dpsgd.dpsgd_residual_norm_forward(desc, x, block, r, y, stats)
-        ctx.desc, ctx.has_block = desc, block is not None
-        ctx.save_for_backward(x if r is None else r, stats)
+        ctx.eps, ctx.has_block = eps, block is not None
+        # The parameters too: one that is changed in place before the backward pass is noticed.
+        ctx.save_for_backward(x if r is None else r, stats, gamma, beta)
         ctx.set_materialize_grads(False)
         return y if r is None else (r, y)
 
     @staticmethod
     def backward(ctx, *grads):
         from . import dpsgd
-        r, stats = ctx.saved_tensors
+        r, stats, gamma, beta = ctx.saved_tensors
+        desc = dpsgd.make_residual_norm(r, "layer", gamma, beta, eps=ctx.eps)
         dr, dy = grads if ctx.has_block else (None, grads[0])
         dy = torch.zeros_like(r) if dy is None else dy.contiguous()
         dr = None if dr is None else dr.contiguous()
         dx = torch.empty_like(r) if ctx.needs_input_grad[0] else None
         dblock = torch.empty_like(r) if ctx.has_block else None
-        ws = torch.empty(dpsgd.dpsgd_residual_norm_workspace_bytes(ctx.desc), dtype=torch.uint8,
+        ws = torch.empty(dpsgd.dpsgd_residual_norm_workspace_bytes(desc), dtype=torch.uint8,
                          device=r.device)
         # Per example: their sum over the batch is the parameter's gradient.
-        dgamma, dbeta = (r.new_empty(ctx.desc.B, ctx.desc.C) if ctx.needs_input_grad[k] else None
+        dgamma, dbeta = (r.new_empty(desc.B, desc.C) if ctx.needs_input_grad[k] else None
                          for k in (2, 3))
         # Without a norm or a gate of it the block's values are not read: r stands for them.
-        dpsgd.dpsgd_residual_norm_backward(ctx.desc, r if ctx.has_block else None, r, dy, dr, stats,
+        dpsgd.dpsgd_residual_norm_backward(desc, r if ctx.has_block else None, r, dy, dr, stats,
                                            dx=dx, dblock=dblock, dgamma=dgamma, dbeta=dbeta,
                                            workspace=ws)
         return (dx, dblock, None if dgamma is None else dgamma.sum(0),

@@ -82,3 +82,13 @@ def test_gradients_of_the_first_norm(needs):
     x, _, gamma, beta = _inputs(needs)
     assert torch.autograd.gradcheck(lambda a, c, d: cap._ResidualNorm.apply(a, None, c, d, 1e-5),
                                     (x, gamma, beta))
+
+
+@pytest.mark.parametrize("which", [2, 3])
+def test_parameters_changed_before_the_backward_pass_are_noticed(which):
+    args = _inputs("xbgB")
+    r, y = cap._ResidualNorm.apply(*args, 1e-5)
+    with torch.no_grad():
+        args[which].mul_(2.0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        (r.sum() + y.square().sum()).backward()
