@@ -167,8 +167,8 @@ class _ResidualNorm(torch.autograd.Function):
         ws = torch.empty(dpsgd.dpsgd_residual_norm_workspace_bytes(desc), dtype=torch.uint8,
                          device=r.device)
         # Per example: their sum over the batch is the parameter's gradient.
-        dgamma, dbeta = (r.new_empty(desc.B, desc.C) if ctx.needs_input_grad[k] else None
-                         for k in (2, 3))
+        dgamma, dbeta = (p.new_empty(desc.B, desc.C) if need else None
+                         for p, need in zip((gamma, beta), ctx.needs_input_grad[2:4]))
         # Without a norm or a gate of it the block's values are not read: r stands for them.
         dpsgd.dpsgd_residual_norm_backward(desc, r if ctx.has_block else None, r, dy, dr, stats,
                                            dx=dx, dblock=dblock, dgamma=dgamma, dbeta=dbeta,
