@@ -35,6 +35,7 @@ from dataclasses import dataclass
 import torch
 import torch.nn as nn
 import torch.nn.functional as F
+from torch.autograd.function import once_differentiable
 
 
 @dataclass
@@ -155,6 +156,7 @@ class _ResidualNorm(torch.autograd.Function):
         return y if r is None else (r, y)
 
     @staticmethod
+    @once_differentiable   # the library's results have no graph of their own
     def backward(ctx, *grads):
         from . import dpsgd
         r, stats, gamma, beta = ctx.saved_tensors

@@ -29,6 +29,7 @@ def _forward(desc, x, block, r, y, stats):
     y.copy_(_normed(total, desc.eps)[0] * desc.gamma + desc.beta)
 
 
+@torch.no_grad()   # as the library's
 def _backward(desc, block, r, dy, dr, stats, dx=None, dblock=None, dgamma=None, dbeta=None, workspace=None):
     assert (block is None) == (dblock is None) and any(t is not None for t in (dx, dblock, dgamma, dbeta))
     vh, rstd = _normed(r, desc.eps)
@@ -92,3 +93,11 @@ def test_parameters_changed_before_the_backward_pass_are_noticed(which):
         args[which].mul_(2.0)
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         (r.sum() + y.square().sum()).backward()
+
+
+def test_a_second_derivative_is_refused():
+    x, block, gamma, beta = _inputs("xbgB")
+    _, y = cap._ResidualNorm.apply(x, block, gamma, beta, 1e-5)
+    gx, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        ((gx * gx).sum() + (x * x).sum()).backward()
