@@ -649,7 +649,7 @@ typedef enum dpsgd_rounding {
  * all 16-byte aligned and pairwise non-overlapping. round_seed is read only with
  * DPSGD_ROUND_STOCHASTIC. A launch has fewer than 2^32 threads: any 48 tensors in a
  * row have up to 2^35 entries together (less 2^18 for their ends), and calls that
- * would need more are refused. */
+ * would need more are refused, with nothing enqueued. */
 int dpsgd_noise_adamw8_multi(const dpsgd_layer* layers, int32_t n_layers,
                              const float* const* grads, float* const* params,
                              uint8_t* const* exp_avgs, uint8_t* const* exp_avg_sqs,

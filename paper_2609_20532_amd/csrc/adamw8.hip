@@ -348,6 +348,18 @@ int blocks_per_wave(const dpsgd_layer* layers, int n) {
   return blocks <= kFewBlocks ? 1 : kManyBlocks;
 }
 
+// Whether each of a call's launches can be: asked before the first, so that a call that is
+// refused has changed nothing. (Launches of few blocks a wave are small.)
+bool all_launchable(const dpsgd_layer* layers, int n_layers) {
+  for (int base = 0; base < n_layers; base += kMaxLayersPerLaunch) {
+    int64_t wgs = 0;
+    for (int l = base; l < n_layers && l < base + kMaxLayersPerLaunch; ++l)
+      wgs += wgs_of(layers[l].d_out * layers[l].d_in, kManyBlocks);
+    if (!launchable(wgs, kThreads)) return false;
+  }
+  return true;
+}
+
 }  // namespace
 
 int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* const* grads,
@@ -355,6 +367,7 @@ int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* co
                         uint8_t* const* exps, float* const* noisy, float sigma, float C,
                         uint64_t seed, uint32_t step, float scale, const dpsgd_adamw& opt,
                         int32_t rounding, uint64_t round_seed, hipStream_t stream) {
+  if (!all_launchable(layers, n_layers)) return DPSGD_ERR_INVALID_ARG;
   const double bc1 = 1.0 - pow((double)opt.beta1, (double)opt.t);
   const double bc2 = 1.0 - pow((double)opt.beta2, (double)opt.t);
   for (int base = 0; base < n_layers; base += kMaxLayersPerLaunch) {
@@ -386,7 +399,6 @@ int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* co
                          L.tensor_id, (uint32_t)wgs};
       wgs += wgs_of(L.d_out * L.d_in, per_wave);
     }
-    if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
     const dim3 grid((uint32_t)wgs), block(kThreads);
     if (rounding == DPSGD_ROUND_STOCHASTIC && per_wave == 1)
       hipLaunchKernelGGL((noise_adamw8_kernel<true, 1>), grid, block, 0, stream, args);
@@ -404,6 +416,7 @@ int launch_noise_adamw8(const dpsgd_layer* layers, int n_layers, const float* co
 int launch_adamw8_pack(const dpsgd_layer* layers, int n_layers, const float* const* ms_in,
                        const float* const* vs_in, uint8_t* const* ms, uint8_t* const* vs,
                        uint8_t* const* exps, hipStream_t stream) {
+  if (!all_launchable(layers, n_layers)) return DPSGD_ERR_INVALID_ARG;
   for (int base = 0; base < n_layers; base += kMaxLayersPerLaunch) {
     const int n = n_layers - base < kMaxLayersPerLaunch ? n_layers - base : kMaxLayersPerLaunch;
     Adam8Args args{};
@@ -415,7 +428,6 @@ int launch_adamw8_pack(const dpsgd_layer* layers, int n_layers, const float* con
                          vs[base + l], exps[base + l], nullptr, L.d_out * L.d_in, 0, (uint32_t)wgs};
       wgs += wgs_of(L.d_out * L.d_in, kManyBlocks);
     }
-    if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
     hipLaunchKernelGGL(adamw8_pack_kernel, dim3((uint32_t)wgs), dim3(kThreads), 0, stream, args);
     if (check_launch() != DPSGD_OK) return DPSGD_ERR_HIP;
   }
@@ -425,6 +437,7 @@ int launch_adamw8_pack(const dpsgd_layer* layers, int n_layers, const float* con
 int launch_adamw8_unpack(const dpsgd_layer* layers, int n_layers, const uint8_t* const* ms,
                          const uint8_t* const* vs, const uint8_t* const* exps, void* const* ms_out,
                          void* const* vs_out, int32_t out_dtype, hipStream_t stream) {
+  if (!all_launchable(layers, n_layers)) return DPSGD_ERR_INVALID_ARG;
   for (int base = 0; base < n_layers; base += kMaxLayersPerLaunch) {
     const int n = n_layers - base < kMaxLayersPerLaunch ? n_layers - base : kMaxLayersPerLaunch;
     UnpackArgs args{};
@@ -437,7 +450,6 @@ int launch_adamw8_unpack(const dpsgd_layer* layers, int n_layers, const uint8_t*
                               vs_out[base + l], L.d_out * L.d_in, (uint32_t)wgs};
       wgs += wgs_of(L.d_out * L.d_in, per_wave);
     }
-    if (!launchable(wgs, kThreads)) return DPSGD_ERR_INVALID_ARG;
     const dim3 grid((uint32_t)wgs), block(kThreads);
     if (out_dtype == DPSGD_BF16 && per_wave == 1)
       hipLaunchKernelGGL((adamw8_unpack_kernel<uint16_t, 1>), grid, block, 0, stream, args);
