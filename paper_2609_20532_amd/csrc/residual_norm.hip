@@ -464,13 +464,15 @@ struct RnPlan {
   int64_t wgs, chunks;
 };
 
+// Vectors of V elements that a thread has of rows from a wave to 1024 threads. Fewer are for
+// rows of at most a wave (256 threads a workgroup), more for those of 1024 threads.
+constexpr int usual_vectors(int elements, int V) { return elements / V > 4 ? 4 : elements / V; }
+
 RnPlan plan_rows(const dpsgd_residual_norm& n, int elements) {
   RnPlan p{};
   p.V = vec_width(n.C, n.dtype == DPSGD_BF16 ? 8 : 4);
   const int64_t units = n.C / p.V;
-  // As many vectors a thread as the elements hold, if that leaves a wave or more; more of
-  // them where a row would be more than 1024 threads.
-  p.nv = elements / p.V > 4 ? 4 : elements / p.V;
+  p.nv = usual_vectors(elements, p.V);
   while (p.nv > 1 && units <= 64 * (p.nv / 2)) p.nv /= 2;
   while (units > (int64_t)p.nv * kMostThreads) p.nv *= 2;
   while (((int64_t)p.nv << p.log) < units) ++p.log;
@@ -542,38 +544,46 @@ RnArgs common_args(const dpsgd_residual_norm& n, const RnPlan& p) {
 constexpr int FORWARD = -1;
 
 template <class T, int V, int NV, int MOST, bool WIDE, int KIND>
-void run(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+int run(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
   const dim3 grid((uint32_t)p.wgs), block(p.threads);
   if constexpr (KIND == FORWARD)
     hipLaunchKernelGGL((rn_forward_kernel<T, V, NV, MOST, WIDE>), grid, block, 0, stream, a);
   else
     hipLaunchKernelGGL((rn_backward_kernel<T, V, NV, MOST, KIND, WIDE>), grid, block, lds, stream, a);
+  return check_launch();
 }
 
+// The kernels that a plan can ask for, and no others.
 template <class T, int V, int NV, int KIND>
-void pick_threads(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
-  if (p.threads > 512) return run<T, V, NV, kMostThreads, true, KIND>(p, a, lds, stream);
-  if (p.threads > kThreads) return run<T, V, NV, 512, true, KIND>(p, a, lds, stream);
+int pick_threads(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+  constexpr int kUsual = usual_vectors(KIND == FORWARD ? kForwardElements : kBackwardElements, V);
+  if constexpr (NV >= kUsual)
+    if (p.threads > 512) return run<T, V, NV, kMostThreads, true, KIND>(p, a, lds, stream);
+  if constexpr (NV == kUsual)
+    if (p.threads > kThreads && p.threads <= 512) return run<T, V, NV, 512, true, KIND>(p, a, lds, stream);
   if constexpr (NV == 1)   // rows of less than a wave have one vector a thread
     if (p.log < 6) return run<T, V, NV, kThreads, false, KIND>(p, a, lds, stream);
-  return run<T, V, NV, kThreads, true, KIND>(p, a, lds, stream);
+  if constexpr (NV <= kUsual)
+    if (p.threads <= kThreads) return run<T, V, NV, kThreads, true, KIND>(p, a, lds, stream);
+  return DPSGD_ERR_UNSUPPORTED;
 }
 
 template <class T, int V, int KIND>
-void pick_vectors(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
+int pick_vectors(const RnPlan& p, const RnArgs& a, size_t lds, hipStream_t stream) {
   switch (p.nv) {
     case 1: return pick_threads<T, V, 1, KIND>(p, a, lds, stream);
     case 2: return pick_threads<T, V, 2, KIND>(p, a, lds, stream);
     case 4:
       if constexpr (V <= 4) return pick_threads<T, V, 4, KIND>(p, a, lds, stream);
-      return;
+      break;
     case 8:
       if constexpr (V <= 2) return pick_threads<T, V, 8, KIND>(p, a, lds, stream);
-      return;
+      break;
     case 16:
       if constexpr (V <= 1) return pick_threads<T, V, 16, KIND>(p, a, lds, stream);
-      return;
+      break;
   }
+  return DPSGD_ERR_UNSUPPORTED;
 }
 
 template <int KIND>
@@ -582,19 +592,17 @@ int launch(const dpsgd_residual_norm& n, const RnPlan& p, const RnArgs& a, size_
   if (!launchable(p.wgs, p.threads)) return DPSGD_ERR_INVALID_ARG;
   if (n.dtype == DPSGD_BF16) {
     switch (p.V) {
-      case 8: pick_vectors<uint16_t, 8, KIND>(p, a, lds, stream); break;
-      case 4: pick_vectors<uint16_t, 4, KIND>(p, a, lds, stream); break;
-      case 2: pick_vectors<uint16_t, 2, KIND>(p, a, lds, stream); break;
-      default: pick_vectors<uint16_t, 1, KIND>(p, a, lds, stream); break;
-    }
-  } else {
-    switch (p.V) {
-      case 4: pick_vectors<float, 4, KIND>(p, a, lds, stream); break;
-      case 2: pick_vectors<float, 2, KIND>(p, a, lds, stream); break;
-      default: pick_vectors<float, 1, KIND>(p, a, lds, stream); break;
+      case 8: return pick_vectors<uint16_t, 8, KIND>(p, a, lds, stream);
+      case 4: return pick_vectors<uint16_t, 4, KIND>(p, a, lds, stream);
+      case 2: return pick_vectors<uint16_t, 2, KIND>(p, a, lds, stream);
+      default: return pick_vectors<uint16_t, 1, KIND>(p, a, lds, stream);
     }
   }
-  return check_launch();
+  switch (p.V) {
+    case 4: return pick_vectors<float, 4, KIND>(p, a, lds, stream);
+    case 2: return pick_vectors<float, 2, KIND>(p, a, lds, stream);
+    default: return pick_vectors<float, 1, KIND>(p, a, lds, stream);
+  }
 }
 
 }  // namespace
