@@ -10,16 +10,17 @@
 //
 // Bound by memory traffic: forward 4 rows of C elements (x, block, r, y), backward
 // 6 (r, block, dy, dr, dx, dblock), each touched once. A group of threads has a row
-// in registers, a fixed set of channels a thread, and takes several rows: the affine
-// parameters stay in registers, and so do the per-example sums of a backward group,
-// which are joined over a workgroup's groups in LDS and over an example's workgroups
+// in registers, a fixed set of channels a thread, and takes several rows: up to 8192
+// channels the affine parameters stay in registers, and so do the per-example sums of a
+// backward group, which are joined over a workgroup's groups in LDS and over an example's workgroups
 // by a second launch. Rows of whole waves have wave-uniform addresses.
 //
 // [16, 1024, 4096] in bf16, RMS norms on both sides and a gate: forward 103 us (537 MB,
 // 5.2 TB/s), backward 169 us (806 MB and 25 MB of partial sums, 4.9 TB/s) and 5.5 for the
 // join. [64, 128, 768], layer norm: backward 16.8 and 3.5 us (63 MB). A backward that has
-// the next row's loads in flight while one is worked on needs 150 registers and spills in
-// rows of 512 threads (238 us in place of 169).
+// the next row's loads in flight while one is worked on needs 150 registers, so that a CU
+// holds one workgroup of 512 threads in place of two (238 us in place of 169); for rows of
+// fewer threads it was not tried. float32, [16, 1024, 4096]: forward 207 us (5.2 TB/s).
 #include <math.h>
 
 #include "vec.h"
@@ -196,6 +197,9 @@ __device__ __forceinline__ int group_of(int log) {
   return WIDE ? __builtin_amdgcn_readfirstlane(g) : g;
 }
 
+// The five parameter arrays and two rows are in registers also above 8192 channels, where
+// they spill: vectors of 4 elements 2 (bf16) and 14, of 2 39 and 46, of 1 154 (4 x 1024 rows of
+// 12288 in float32: 203 us, 4.0 TB/s).
 template <class T, int V, int NV, int MOST, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_forward_kernel(RnArgs a) {
   __shared__ float lds[2][kWaves][2];
@@ -270,7 +274,9 @@ enum BackKind : int { BARE = 0, GATED = 1, POST = 2 };
 // own places. In registers they spill 36 to 257 of them: 2 x 1024 rows of 16384 in bf16 85 us
 // (116 with spills; with only the parameters read again 90), normed on both sides 127 (311;
 // 269), 3 x 128 of 13502 with a gate 38 (74; 78). What still
-// spills: odd widths (53 to 185 registers) and a norm of the block (6 to 99).
+// spills above 8192 channels: a norm of the block (vectors of 8, 4, 2 and 1 elements: 6, 23 to
+// 27, 81 to 99 and 164 to 185 registers), a gate (vectors of 2 and 1: 21 to 23 and 66), neither
+// (1 to 2 and 53 to 57), and one register in odd widths of 4097 to 8192 with a norm of the block.
 template <class T, int V, int NV, int MOST, int KIND, bool WIDE>
 __global__ __launch_bounds__(MOST) void rn_backward_kernel(RnArgs a) {
   extern __shared__ __align__(16) float rn_lds[];   // [groups][C], where there are several groups

@@ -20,7 +20,10 @@
 //    which the last-level cache holds a part (held rows took 116).
 //  - Alternatives: rows held, candidates by a bound (top_entries): 54 us for 5 of the same
 //    rows' entries, 64 us for 64 (reading the row once for each took 1616 us for 20).
-//  - Rows that no workgroup holds, or few long ones: in parts, joined by a second launch.
+//  - Rows that no workgroup holds, or few long ones: in parts, joined by a second launch
+//    (loss of 1024 rows of 128256 in float32: 302 us, its logits read twice).
+//  - The gradient of log probabilities: parts of rows, p from lse, 290 us for 8192 rows of
+//    50257 in bf16 (5.7 TB/s); rows whose lse is far from 0 by one workgroup each.
 #include <math.h>
 
 #include "vec.h"
@@ -57,7 +60,8 @@ struct TokenArgs {
   float scale;
 };
 
-// e^d for d <= 0: exactly 0 for -inf.
+// e^d for d <= 0: exactly 0 for -inf, else within (2 |d| + 2) 2^-24 of itself (the rounding of
+// d log2 e, and the instruction's).
 __device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
 
 // The target of a row, -1 for an empty position; *empty: there is none.
@@ -918,7 +922,7 @@ __device__ __forceinline__ void write_backward(const Held<T, NT, NVEC>& held, co
 
 // Rows whose p is formed from lse as it is stored: its rounding, half a step of lse, is then
 // at most 2^-20 of p (2^-15, a 64th of the gradient's own rounding, in bf16), and the same for
-// all p of the row. Beyond, where it would grow with the logits' common offset (0.5% of p at
+// all p of the row. Beyond, where it would grow with the logits' common offset (to 3% of p at
 // 10^6), the row's sums are formed again, relative to its largest entry.
 template <class T>
 constexpr float kNearLse = sizeof(T) == 2 ? 1024.0f : 32.0f;
