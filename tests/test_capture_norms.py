@@ -101,3 +101,9 @@ def test_a_second_derivative_is_refused():
     gx, = torch.autograd.grad(y.square().sum(), x, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         ((gx * gx).sum() + (x * x).sum()).backward()
+
+
+@pytest.mark.parametrize("used", [0, 1])
+def test_one_output_alone(used):
+    """The gradient of the output that nothing uses is none."""
+    assert torch.autograd.gradcheck(lambda *a: cap._ResidualNorm.apply(*a, 1e-5)[used], _inputs("xbgB"))
